@@ -368,6 +368,99 @@ hdt_status_t hdt_hpe_table(float *d_table, int32_t rows, int32_t d_model, void *
 hdt_status_t hdt_hpe_add(const int32_t *d_p, int32_t batch, int32_t n_pos, int32_t n_levels, const float *d_table,
                          int32_t table_rows, void *x, int32_t d_model, hdt_dtype_t dt, void *stream);
 
+/*
+ * Self-attention with a learned relative position bias by buckets (the decoder of Sec. 3.2, "T5-style": causal, one scalar per
+ * bucket of distances and head), and its gradient:
+ *     A_ij = softmax_scale q_i . k_j + bias[table[clamp(j - p_i, -max_distance, max_distance) + max_distance]][head]
+ *     O = softmax over the visible j of A, times V;   p_i = d_q_start[sample] + i is the position query i stands at
+ * Key j of a sample is visible to query i iff j < d_lengths[sample] and, with `causal`, j <= p_i.  A query is real iff its position
+ * lies in [0, d_lengths[sample]): the queries are a window of the sequence whose keys are given.  A training step has the whole of
+ * it (d_q_start NULL: 0), a step of generation its last n_q positions (d_q_start = length - n_q, the new keys already in the cache).
+ * Rows that are not real get O = 0, LSE = -inf and gradients of 0, and so do keys from the length on; what such rows of Q, K, V,
+ * O, dO hold may be anything, NaN included.  A non-finite value in a REAL row reaches the rows that see it, and may also reach rows
+ * of its tile of 128 x 64 pairs that the causal mask hides it from (zero weights are applied by multiplication).
+ *
+ *   heads, kv_heads   kv_heads divides heads: key head g serves the heads [g heads / kv_heads, (g + 1) heads / kv_heads), and
+ *                     dk, dv are the sums over them
+ *   d_bias            device, [n_buckets][heads], bias_dtype.  Values from -1e6 down (-inf, the type's lowest) hide a bucket: its pairs
+ *                     are not visible, and a query that sees nothing else has O = 0, LSE = -inf; values from 1e6 up count as 1e6
+ *   d_table           device, int32 [2 max_distance + 1], of hdt_rel_table or the caller's own; entries outside [0, n_buckets)
+ *                     count as the nearest one inside; max_distance 1 .. 1024, n_buckets 1 .. 4096
+ *   d_lengths, d_q_start  device, int32 [batch], or NULL (n_kv; 0).  Read by the kernels: they may change between replays of a
+ *                     captured graph.  Lengths outside [0, n_kv] count as the nearest one inside.
+ *   strides           in elements, rows of head_dim consecutive values, multiples of 16 bytes; all zero: dense [batch][heads][rows]
+ *                     [head_dim].  A row stride is at most 2^20.  Inputs may be broadcast (stride 0 over batch or heads), the rows
+ *                     of an output must not overlap.
+ *   head_dim 64 or 128; n_q, n_kv up to 2^24; every size may be 0.  Tensor pointers 16-byte aligned.
+ */
+typedef struct {
+    int64_t batch, head, row;
+} hdt_strides_t;
+
+typedef struct {
+    int32_t batch, heads, kv_heads, n_q, n_kv, head_dim;
+    int32_t causal; /* 1: a position sees itself and what stands before it, 0: the whole sequence */
+    int32_t n_buckets, max_distance;
+    hdt_dtype_t dtype, bias_dtype;
+    float softmax_scale;
+    const void *d_bias;
+    const int32_t *d_table, *d_lengths, *d_q_start;
+    hdt_strides_t q, k, v, o;          /* dense if all three are 0 */
+    hdt_strides_t d_o, dq, dk, dv;     /* the backward's */
+} hdt_rel_attn_t;
+
+/* The buckets of T5: table[d + max_distance], d = key position - query position.  One way (both_ways = 0, for causal attention): the
+ * first half of the buckets are the distances 0, 1, 2, ... back, the others ranges that grow with the logarithm up to max_distance
+ * (a border counts as reached from 1e-9 below on), all beyond in the last bucket; positions ahead share bucket 0.  Both ways: the
+ * same with half of the buckets for each direction, those for positions ahead second.  Enqueues one kernel on `stream`.
+ * Errors: INVALID_ARG, SHAPE (fewer than 2 buckets a direction, max_distance not beyond the exact half or above 1024), HDT_ERR_HIP. */
+hdt_status_t hdt_rel_table(int32_t n_buckets, int32_t max_distance, int32_t both_ways, int32_t *d_table, void *stream);
+
+/*
+ * hdt_rel_attn_fwd -- q [batch][heads][n_q][head_dim], k, v [batch][kv_heads][n_kv][head_dim] -> o like q, lse [batch][heads][n_q]
+ * float (dense).  Where there are few rows and many keys, the keys are divided among workgroups whose results a second kernel
+ * joins in a fixed order; that takes a workspace of hdt_rel_attn_fwd_workspace_bytes (0: none needed), and with less, or NULL, the
+ * keys stay together, which is slower.  Only enqueues work on `stream`.
+ * hdt_rel_attn_bwd -- o, lse of the forward and d_o -> dq, dk, dv, and d_bias_grad [n_buckets][heads] of bias_dtype: the sum of
+ *   dS over the pairs of a bucket.  Every output is written whole.  `workspace`: hdt_rel_attn_bwd_workspace_bytes bytes, scratch only.
+ * Both give the same bits every time.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED (dtype, head_dim), HDT_ERR_HIP.
+ */
+size_t hdt_rel_attn_fwd_workspace_bytes(const hdt_rel_attn_t *h_call);
+hdt_status_t hdt_rel_attn_fwd(const hdt_rel_attn_t *h_call, const void *q, const void *k, const void *v, void *o, float *lse,
+                              void *workspace, size_t workspace_bytes, void *stream);
+size_t hdt_rel_attn_bwd_workspace_bytes(const hdt_rel_attn_t *h_call);
+hdt_status_t hdt_rel_attn_bwd(const hdt_rel_attn_t *h_call, const void *q, const void *k, const void *v, const void *o, const float *lse,
+                              const void *d_o, void *dq, void *dk, void *dv, void *d_bias_grad, void *workspace, size_t workspace_bytes,
+                              void *stream);
+
+/*
+ * What stands between the attention calls of a pre-norm block (Sec. 3.2; dropout 0.1 in App. A.2): dropout whose mask is never stored,
+ * the residual, layer norm.  The mask m of n elements comes from a counter: elements 8g .. 8g + 7 of a call share one block of
+ * Philox4x32-10 (Salmon et al., SC 2011) with counter (g, site, step, step >> 32) and key (seed, seed >> 32), 16 bits each, the lowest
+ * of the first word first; an element is kept iff its bits are at least t = round(65536 p), times 65536 / (65536 - t).
+ * d_rng: device, int64 [2] = (seed, step), 8-byte aligned.  The kernels read it, so a captured graph that increments the step drops others
+ * at every replay; a backward needs the values its forward had.  `site` tells calls with the same seed and step apart.  p = 0 drops
+ * nothing and needs no d_rng.  Tensors are dense; at most 2^35 elements.
+ *
+ * hdt_dropout_add -- out = x + y o m on n elements; x may be NULL (dropout by itself, and its gradient: the same call on the gradient);
+ *   out may be x or y.
+ * hdt_add_norm_fwd -- h = x + y o m, n = (h - mean) rstd weight + bias over rows of `width`, rstd = 1 / sqrt(variance + eps).  y may be
+ *   NULL (h is x then and not written, h may be NULL), bias too.  mean, rstd: [rows] float.  Statistics are those of the unrounded h.
+ * hdt_add_norm_bwd -- from dn, the gradient of n, and dh, that of h from elsewhere (may be NULL): dx, the gradient of x (and of h); dy = dx o m,
+ *   only where something is dropped (else dy may be NULL: it is dx); d_weight, d_bias (may be NULL) [width] of weight_dt.  `h`: the
+ *   forward's h (its x where y was NULL).  `workspace`: hdt_add_norm_bwd_workspace_bytes bytes, scratch only.  Sums in a fixed order.
+ * width 1 .. 32768.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED (dtype), HDT_ERR_HIP.
+ */
+hdt_status_t hdt_dropout_add(const void *y, const void *x, void *out, int64_t n, double p, const int64_t *d_rng, uint32_t site,
+                             hdt_dtype_t dt, void *stream);
+hdt_status_t hdt_add_norm_fwd(const void *x, const void *y, const void *weight, const void *bias, int64_t rows, int32_t width, float eps,
+                              double p, const int64_t *d_rng, uint32_t site, void *h, void *n, float *mean, float *rstd, hdt_dtype_t dt,
+                              hdt_dtype_t weight_dt, void *stream);
+size_t hdt_add_norm_bwd_workspace_bytes(int64_t rows, int32_t width);
+hdt_status_t hdt_add_norm_bwd(const void *dn, const void *dh, const void *h, const void *weight, const float *mean, const float *rstd,
+                              int64_t rows, int32_t width, double p, const int64_t *d_rng, uint32_t site, void *dx, void *dy, void *d_weight,
+                              void *d_bias, hdt_dtype_t dt, hdt_dtype_t weight_dt, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Text of a status code / of the last error on this thread (never NULL). */
 const char *hdt_status_string(hdt_status_t status);
 const char *hdt_last_error(void);

@@ -26,6 +26,8 @@ EXPORTED_SYMBOLS = [
     "hdt_attn_fwd", "hdt_attn_fwd_ws", "hdt_attn_fwd_workspace_bytes", "hdt_attn_bwd_workspace_bytes", "hdt_attn_bwd", "hdt_attn_bwd_no_alloc", "hdt_status_string", "hdt_last_error",
     "hdt_timing_enable", "hdt_timing_reset", "hdt_timing_read", "hdt_probe_mfma_bf16", "hdt_release_cached_memory",
     "hdt_parents_from_levels", "hdt_index_vectors_workspace_bytes", "hdt_index_vectors", "hdt_hpe_table", "hdt_hpe_add",
+    "hdt_rel_table", "hdt_rel_attn_fwd_workspace_bytes", "hdt_rel_attn_fwd", "hdt_rel_attn_bwd_workspace_bytes", "hdt_rel_attn_bwd",
+    "hdt_dropout_add", "hdt_add_norm_fwd", "hdt_add_norm_bwd_workspace_bytes", "hdt_add_norm_bwd",
 ]
 
 
@@ -48,6 +50,18 @@ class _Info(ctypes.Structure):
                 ("windowed", ctypes.c_int32), ("edges", ctypes.c_int32), ("n_tiles", ctypes.c_int64),
                 ("nnz", ctypes.c_int64), ("device_bytes", ctypes.c_int64), ("n_kv", ctypes.c_int32),
                 ("cross", ctypes.c_int32), ("cross_level_mask", ctypes.c_uint32), ("compact_rows", ctypes.c_int32)]
+
+
+class _Strides(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("head", ctypes.c_int64), ("row", ctypes.c_int64)]
+
+
+class _RelAttn(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in ("batch", "heads", "kv_heads", "n_q", "n_kv", "head_dim", "causal", "n_buckets",
+                                              "max_distance")]
+    _fields_ += [("dtype", ctypes.c_int), ("bias_dtype", ctypes.c_int), ("softmax_scale", ctypes.c_float)]
+    _fields_ += [(f, ctypes.c_void_p) for f in ("d_bias", "d_table", "d_lengths", "d_q_start")]
+    _fields_ += [(f, _Strides) for f in ("q", "k", "v", "o", "d_o", "dq", "dk", "dv")]
 
 
 def library_path() -> str:
@@ -145,6 +159,20 @@ def load_library():
     lib.hdt_hpe_table.restype = ctypes.c_int
     lib.hdt_hpe_add.argtypes = [vp, i32, i32, i32, vp, i32, vp, i32, ctypes.c_int, vp]
     lib.hdt_hpe_add.restype = ctypes.c_int
+    desc, size, code, f64 = ctypes.POINTER(_RelAttn), ctypes.c_size_t, ctypes.c_int, ctypes.c_double
+    lib.hdt_rel_table.argtypes = [i32, i32, i32, vp, vp]
+    lib.hdt_rel_attn_fwd_workspace_bytes.argtypes = [desc]
+    lib.hdt_rel_attn_fwd.argtypes = [desc, vp, vp, vp, vp, vp, vp, size, vp]
+    lib.hdt_rel_attn_bwd_workspace_bytes.argtypes = [desc]
+    lib.hdt_rel_attn_bwd.argtypes = [desc] + [vp] * 11 + [size, vp]
+    lib.hdt_dropout_add.argtypes = [vp, vp, vp, i64, f64, vp, ctypes.c_uint32, code, vp]
+    lib.hdt_add_norm_fwd.argtypes = [vp, vp, vp, vp, i64, i32, f32, f64, vp, ctypes.c_uint32, vp, vp, vp, vp, code, code, vp]
+    lib.hdt_add_norm_bwd_workspace_bytes.argtypes = [i64, i32]
+    lib.hdt_add_norm_bwd.argtypes = [vp] * 6 + [i64, i32, f64, vp, ctypes.c_uint32] + [vp] * 4 + [code, code, vp, size, vp]
+    for f in (lib.hdt_rel_table, lib.hdt_rel_attn_fwd, lib.hdt_rel_attn_bwd, lib.hdt_dropout_add, lib.hdt_add_norm_fwd, lib.hdt_add_norm_bwd):
+        f.restype = code
+    for f in (lib.hdt_rel_attn_fwd_workspace_bytes, lib.hdt_rel_attn_bwd_workspace_bytes, lib.hdt_add_norm_bwd_workspace_bytes):
+        f.restype = size
     _calls = _native_calls(lib, str(torch.__version__))
     _lib = lib  # the last step: whoever sees it, in another thread too, uses _calls
     return lib
@@ -494,3 +522,186 @@ def hdt_hpe_add(p, table, x, stream=None):
     _check(load_library().hdt_hpe_add(_ptr(p), B, N, L, _ptr(table) if rows else None, rows, _ptr(x), x.shape[2],
                                       _dtype_code(x), _stream_ptr(stream)))
     return x
+
+
+def hdt_rel_table(n_buckets: int, max_distance: int, both_ways: bool = False, device="cuda", stream=None):
+    """int32 device tensor [2 max_distance + 1]: T5's bucket of every distance key - query; ``both_ways`` for attention that is
+    not causal."""
+    import torch
+    table = torch.empty(2 * max(int(max_distance), 0) + 1, dtype=torch.int32, device=device)
+    _check(load_library().hdt_rel_table(int(n_buckets), int(max_distance), int(both_ways), _ptr(table), _stream_ptr(stream)))
+    return table
+
+
+def _same_device(ts):
+    """One device for all of them (the current one: kernels go to its streams)."""
+    import torch
+    for t in ts:
+        if t is not None and not (t.is_cuda and t.get_device() == torch.cuda.current_device()):
+            raise ValueError("tensors must be on the current device")
+
+
+def _rel_attn_call(q, k, v, bias, table, softmax_scale, causal, lengths, q_start, **others):
+    """The description of a call; ``others``: name of a strided tensor -> the tensor (shaped like q or k)."""
+    import torch
+    if q.dim() != 4 or k.dim() != 4 or k.shape != v.shape:
+        raise ValueError("q must be [batch][heads][n_q][head_dim], k and v [batch][kv_heads][n_kv][head_dim]")
+    (B, H, nq, D), (KV, nk) = q.shape, k.shape[1:3]
+    if k.shape[0] != B or k.shape[3] != D:
+        raise ValueError(f"k {tuple(k.shape)} does not fit q {tuple(q.shape)}")
+    if bias.dim() != 2 or bias.shape[1] != H or not bias.is_contiguous():
+        raise ValueError("bias must be a contiguous [n_buckets][heads] tensor")
+    if table.dim() != 1 or table.numel() % 2 == 0 or table.dtype != torch.int32 or not table.is_contiguous():
+        raise ValueError("table must be a contiguous int32 tensor of 2 max_distance + 1 entries")
+    for name, t in (("lengths", lengths), ("q_start", q_start)):
+        if t is not None and (t.dtype != torch.int32 or t.shape != (B,) or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous int32 tensor [batch]")
+    c = _RelAttn(B, H, KV, nq, nk, D, int(causal), bias.shape[0], table.numel() // 2, _dtype_code(q), _dtype_code(bias), float(softmax_scale),
+                 _ptr(bias), _ptr(table), _ptr(lengths), _ptr(q_start))
+    for name, t in dict(others, q=q, k=k, v=v).items():
+        shape = k.shape if name in ("k", "v", "dk", "dv") else q.shape
+        if t.shape != shape or t.dtype != q.dtype:
+            raise ValueError(f"{name} must be {tuple(shape)} of {q.dtype}")
+        if t.stride(3) != 1 and t.numel() > 0:
+            raise ValueError(f"{name}: the values of a row must be consecutive")
+        if not t.is_contiguous():  # (a stride of a dimension of one element says nothing)
+            dense = (shape[1] * shape[2] * D, shape[2] * D, D)
+            setattr(c, name, _Strides(*(t.stride(i) if shape[i] > 1 else dense[i] for i in range(3))))
+    _same_device((q, k, v, bias, table, lengths, q_start, *others.values()))
+    return c
+
+
+def hdt_rel_attn_fwd(q, k, v, bias, table, softmax_scale: float, causal: bool = True, lengths=None, q_start=None, o=None, lse=None,
+                     workspace=None, stream=None):
+    """Self-attention with a relative position bias (hdt_rel_attn_fwd in include/hdt.h).  q [batch][heads][n_q][head_dim], k, v
+    [batch][kv_heads][n_kv][head_dim], of any strides with consecutive row values; bias [n_buckets][heads]; table: of
+    hdt_rel_table; lengths, q_start: int32 device tensors [batch] or None.  Returns (o, lse)."""
+    import torch
+    lib = load_library()
+    if o is None:
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
+    c = _rel_attn_call(q, k, v, bias, table, softmax_scale, causal, lengths, q_start, o=o)
+    if lse.shape != q.shape[:3] or lse.dtype != torch.float32 or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous float32 tensor [batch][heads][n_q]")
+    _same_device((lse, workspace))
+    if workspace is None:
+        need = lib.hdt_rel_attn_fwd_workspace_bytes(ctypes.byref(c))
+        workspace = _scratch(need, q.device, stream) if need else None
+    nbytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _check(lib.hdt_rel_attn_fwd(ctypes.byref(c), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(workspace), nbytes, _stream_ptr(stream)))
+    return o, lse
+
+
+def hdt_rel_attn_bwd(q, k, v, bias, table, o, lse, d_o, softmax_scale: float, causal: bool = True, lengths=None, q_start=None, dq=None,
+                     dk=None, dv=None, dbias=None, workspace=None, stream=None):
+    """The gradients of hdt_rel_attn_fwd: (dq, dk, dv, dbias), dbias like bias."""
+    import torch
+    lib = load_library()
+    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
+    dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dk is None else dk
+    dv = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dv is None else dv
+    dbias = torch.empty_like(bias) if dbias is None else dbias
+    c = _rel_attn_call(q, k, v, bias, table, softmax_scale, causal, lengths, q_start, o=o, d_o=d_o, dq=dq, dk=dk, dv=dv)
+    if lse.shape != q.shape[:3] or lse.dtype != torch.float32 or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous float32 tensor [batch][heads][n_q]")
+    if dbias.shape != bias.shape or dbias.dtype != bias.dtype or not dbias.is_contiguous():
+        raise ValueError("dbias must be like bias")
+    _same_device((lse, dbias, workspace))
+    if workspace is None:
+        workspace = _scratch(lib.hdt_rel_attn_bwd_workspace_bytes(ctypes.byref(c)), q.device, stream)
+    _check(lib.hdt_rel_attn_bwd(ctypes.byref(c), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(d_o), _ptr(dq), _ptr(dk), _ptr(dv),
+                                _ptr(dbias), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+    return dq, dk, dv, dbias
+
+
+def _check_rng(rng, p):
+    import torch
+    if rng is None:
+        if p > 0:
+            raise ValueError("dropout needs rng: an int64 device tensor (seed, step)")
+    elif rng.dtype != torch.int64 or rng.shape != (2,) or not (rng.is_cuda and rng.is_contiguous()):
+        raise ValueError("rng must be an int64 device tensor (seed, step)")
+
+
+def _check_like(t, ts):
+    for x in ts:
+        if x is not None and (x.shape != t.shape or x.dtype != t.dtype or not (x.is_cuda and x.is_contiguous())):
+            raise ValueError(f"tensors must be contiguous device tensors {tuple(t.shape)} of {t.dtype}")
+
+
+def hdt_dropout_add(y, p: float, rng=None, site: int = 0, x=None, out=None, stream=None):
+    """x + dropout(y) (x = None: dropout alone; on a gradient: its backward).  ``rng``: int64 device tensor (seed, step); ``site``: which
+    of the calls with that seed and step.  ``out`` may be x or y.  Returns out."""
+    import torch
+    out = torch.empty_like(y) if out is None else out
+    _check_like(y, (y, x, out))
+    _check_rng(rng, p)
+    _same_device((y, x, out, rng))
+    _check(load_library().hdt_dropout_add(_ptr(y), _ptr(x), _ptr(out), y.numel(), float(p), _ptr(rng), int(site), _dtype_code(y), _stream_ptr(stream)))
+    return out
+
+
+def _check_norm(x, weight, vectors, statistics):
+    import torch
+    rows = x.shape[:-1].numel()
+    for w in (weight, *vectors):
+        if w is not None and (w.shape != x.shape[-1:] or w.dtype != weight.dtype or not (w.is_cuda and w.is_contiguous())):
+            raise ValueError("weight and bias must be contiguous device tensors [width] of one dtype")
+    for s in statistics:
+        if s.numel() != rows or s.dtype != torch.float32 or not (s.is_cuda and s.is_contiguous()):
+            raise ValueError("mean and rstd must be contiguous float32 device tensors with one value a row")
+    return rows
+
+
+def hdt_add_norm_fwd(x, weight, bias=None, eps: float = 1e-5, y=None, p: float = 0.0, rng=None, site: int = 0, h=None, n=None, mean=None,
+                     rstd=None, stream=None):
+    """h = x + dropout(y), n = layer norm of h over the last dimension.  Returns (n, h, mean, rstd); h is x where y is None."""
+    import torch
+    if x.dim() < 1:
+        raise ValueError("x must have a last dimension")
+    n = torch.empty_like(x) if n is None else n
+    if y is None:
+        h = x
+    elif h is None:
+        h = torch.empty_like(x)
+    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if mean is None else mean
+    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if rstd is None else rstd
+    _check_like(x, (x, y, h, n))
+    rows = _check_norm(x, weight, (bias,), (mean, rstd))
+    _check_rng(rng, p if y is not None else 0.0)
+    _same_device((x, y, h, n, weight, bias, mean, rstd, rng))
+    if y is None:
+        p = 0.0
+    _check(load_library().hdt_add_norm_fwd(_ptr(x), _ptr(y), _ptr(weight), _ptr(bias), rows, x.shape[-1], float(eps), float(p), _ptr(rng),
+                                           int(site), _ptr(h) if y is not None else None, _ptr(n), _ptr(mean), _ptr(rstd), _dtype_code(x),
+                                           _dtype_code(weight), _stream_ptr(stream)))
+    return n, h, mean, rstd
+
+
+def hdt_add_norm_bwd(dn, h, weight, mean, rstd, dh=None, p: float = 0.0, rng=None, site: int = 0, bias: bool = True, dx=None, dy=None,
+                     dweight=None, dbias=None, workspace=None, stream=None):
+    """Gradients of hdt_add_norm_fwd from dn (that of n) and dh (that of h from elsewhere, or None).  Returns (dx, dy, dweight, dbias):
+    dy is dx itself where nothing is dropped, dbias None with ``bias=False``."""
+    import torch
+    lib = load_library()
+    dx = torch.empty_like(h) if dx is None else dx
+    dropped = int(float(p) * 65536 + 0.5) > 0
+    if not dropped:
+        dy = dx
+    elif dy is None:
+        dy = torch.empty_like(h)
+    dweight = torch.empty_like(weight) if dweight is None else dweight
+    if bias and dbias is None:
+        dbias = torch.empty_like(weight)
+    _check_like(h, (h, dn, dh, dx, dy))
+    rows = _check_norm(h, weight, (dweight, dbias), (mean, rstd))
+    _check_rng(rng, p)
+    _same_device((h, dn, dh, dx, dy, weight, dweight, dbias, mean, rstd, rng, workspace))
+    if workspace is None:
+        workspace = _scratch(lib.hdt_add_norm_bwd_workspace_bytes(rows, h.shape[-1]), h.device, stream)
+    _check(lib.hdt_add_norm_bwd(_ptr(dn), _ptr(dh), _ptr(h), _ptr(weight), _ptr(mean), _ptr(rstd), rows, h.shape[-1], float(p), _ptr(rng),
+                                int(site), _ptr(dx), _ptr(dy) if dropped else None, _ptr(dweight), _ptr(dbias), _dtype_code(h), _dtype_code(weight),
+                                _ptr(workspace), workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+    return dx, dy, dweight, dbias

@@ -13,7 +13,8 @@ CSRC = os.path.join(_PKG, "csrc")
 LIB = os.path.join(_PKG, "libhdt.so")
 # compiled for one Python (the suffix says which) and one torch; libhdt.so takes any of both
 PYCALL = os.path.join(_PKG, "_hdt_pycall" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
-SOURCES = ["hdt_api.hip", "hdt_layout.hip", "hdt_f32.hip", "hdt_fwd.hip", "hdt_bwd.hip", "hdt_hpe.hip", "hdt_cross.hip", "hdt_probe.hip"]
+SOURCES = ["hdt_api.hip", "hdt_layout.hip", "hdt_f32.hip", "hdt_fwd.hip", "hdt_bwd.hip", "hdt_hpe.hip", "hdt_cross.hip", "hdt_probe.hip", "hdt_rel.hip",
+           "hdt_rel_fwd.hip", "hdt_rel_bwd.hip", "hdt_norm.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",

@@ -155,6 +155,13 @@ hdt_status_t hdt_fail(hdt_status_t st, const char *fmt, ...);
                             #expr, hipGetErrorString(_e));                                    \
     } while (0)
 
+// neither infinite nor NaN, by the bits: the sources are compiled on the assumption that comparisons meet no NaN
+inline bool hdt_finite(double x)
+{
+    uint64_t u;
+    __builtin_memcpy(&u, &x, sizeof(u));
+    return (u >> 52 & 0x7ffu) != 0x7ffu;
+}
 bool hdt_layout_ok(const hdt_layout_t *l);
 // Reads the report of a deferred build: with `wait` it returns once the report is in (it waits for the build
 // kernel, not for the stream), without it only looks.  Returns the build's status as far as it is known (HDT_OK

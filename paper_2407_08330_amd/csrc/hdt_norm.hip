@@ -1,0 +1,530 @@
+// What stands between the attention calls of a pre-norm block: dropout from a counter-based generator, the residual, layer norm.
+//
+//   hdt_dropout_add   out = x + y o m                       (x may be missing; the gradient of y is the same call on the gradient)
+//   hdt_add_norm_fwd  h = x + y o m,  n = (h - mean) rstd w + b
+//   hdt_add_norm_bwd  g = dn w,  dx = dh + rstd (g - mean(g) - xhat mean(g xhat)),  dy = dx o m,  dw = sum dn xhat,  db = sum dn
+//
+// The mask m is never stored: both passes compute it from (seed, step, site, element).  Eight elements share one block of
+// Philox4x32-10 (Salmon, Moraes, Dror and Shaw, SC 2011), 16 bits each; an element is kept iff its 16 bits are at least
+// t = round(65536 p), and what is kept is multiplied by 65536 / (65536 - t), the inverse of the probability that 16 bits really give.
+//
+// All of it is bound by memory: a row is read once, held in registers between its statistics and its result, and written once.
+// Sums and statistics are in fp32; h is rounded once, when it is written (the norm is taken of the unrounded sum).
+#include "hdt_internal.h"
+#include "hdt_mfma.h"
+
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
+struct Drop {
+    const long long *rng;  // device: seed, step
+    uint32_t site, threshold;  // threshold 0: nothing is dropped
+    float keep_scale;
+};
+struct Key {
+    uint32_t seed_lo, seed_hi, step_lo, step_hi;
+};
+__device__ __forceinline__ Key key_of(const Drop &d)
+{
+    if (d.threshold == 0) return {};
+    const unsigned long long seed = (unsigned long long)d.rng[0], step = (unsigned long long)d.rng[1];
+    return {(uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)step, (uint32_t)(step >> 32)};
+}
+
+struct Block {
+    uint32_t w[4];
+};
+__device__ __forceinline__ Block philox(uint32_t block, uint32_t site, const Key &k)
+{
+    uint32_t c0 = block, c1 = site, c2 = k.step_lo, c3 = k.step_hi, k0 = k.seed_lo, k1 = k.seed_hi;
+#pragma unroll
+    for (int i = 0; i < 10; i++) {
+        const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
+        c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+        c1 = (uint32_t)b;
+        c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+        c3 = (uint32_t)a;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return {{c0, c1, c2, c3}};
+}
+// the 16-bit numbers of elements at .. at + 7
+__device__ __forceinline__ Block numbers(unsigned long long at, const Drop &d, const Key &k)
+{
+    const uint32_t block = (uint32_t)(at >> 3), off = (uint32_t)at & 7u;
+    Block a = philox(block, d.site, k);
+    if (off == 0) return a;
+    const Block b = philox(block + 1, d.site, k);
+    uint32_t w[8] = {a.w[0], a.w[1], a.w[2], a.w[3], b.w[0], b.w[1], b.w[2], b.w[3]};
+#pragma unroll
+    for (int s = 4; s >= 1; s >>= 1) {
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            if (i + s < 8) w[i] = (off >> 1) & s ? w[i + s] : w[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++) a.w[i] = off & 1 ? (w[i] >> 16) | (w[i + 1] << 16) : w[i];
+    return a;
+}
+// the factors of elements e of a block
+__device__ __forceinline__ float factor(const Block &b, int e, const Drop &d)
+{
+    const uint32_t u = e & 1 ? b.w[e >> 1] >> 16 : b.w[e >> 1] & 0xffffu;
+    return u >= d.threshold ? d.keep_scale : 0.f;
+}
+
+// 8 consecutive elements; `left` of them exist.  The address is aligned to an element only.
+typedef bf16x8 __attribute__((aligned(2))) bf16x8_any;
+typedef f32x4 __attribute__((aligned(4))) f32x4_any;
+struct Eight {
+    float x[8];
+};
+__device__ __forceinline__ Eight load8(const __bf16 *p, int left)
+{
+    Eight r;
+    if (left >= 8) {
+        const bf16x8 v = *reinterpret_cast<const bf16x8_any *>(p);
+#pragma unroll
+        for (int e = 0; e < 8; e++) r.x[e] = (float)v[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) r.x[e] = e < left ? (float)p[e] : 0.f;
+    }
+    return r;
+}
+__device__ __forceinline__ Eight load8(const float *p, int left)
+{
+    Eight r;
+    if (left >= 8) {
+        const f32x4 a = *reinterpret_cast<const f32x4_any *>(p), b = *reinterpret_cast<const f32x4_any *>(p + 4);
+#pragma unroll
+        for (int e = 0; e < 4; e++) r.x[e] = a[e], r.x[4 + e] = b[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) r.x[e] = e < left ? p[e] : 0.f;
+    }
+    return r;
+}
+__device__ __forceinline__ void store8(__bf16 *p, const Eight &r, int left)
+{
+    if (left >= 8) {
+        bf16x8 v;
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] = (__bf16)r.x[e];
+        *reinterpret_cast<bf16x8_any *>(p) = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            if (e < left) p[e] = (__bf16)r.x[e];
+    }
+}
+__device__ __forceinline__ void store8(float *p, const Eight &r, int left)
+{
+    if (left >= 8) {
+        *reinterpret_cast<f32x4_any *>(p) = f32x4{r.x[0], r.x[1], r.x[2], r.x[3]};
+        *reinterpret_cast<f32x4_any *>(p + 4) = f32x4{r.x[4], r.x[5], r.x[6], r.x[7]};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            if (e < left) p[e] = r.x[e];
+    }
+}
+__device__ __forceinline__ Eight load_weight(const void *p, int bf16, long long at, int left)
+{
+    return bf16 ? load8((const __bf16 *)p + at, left) : load8((const float *)p + at, left);
+}
+
+// ------------------------------------------------------------------------------------------ dropout + residual
+template <typename T>
+__global__ __launch_bounds__(256) void k_dropout_add(const T *y, const T *x, T *out, unsigned long long n, Drop d)
+{
+    const Key k = key_of(d);
+    const unsigned long long at = ((unsigned long long)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (at >= n) return;
+    const int left = (int)min(n - at, 8ull);
+    Eight v = load8(y + at, left);
+    if (d.threshold) {
+        const Block b = philox((uint32_t)(at >> 3), d.site, k);
+#pragma unroll
+        for (int e = 0; e < 8; e++) v.x[e] *= factor(b, e, d);
+    }
+    if (x) {
+        const Eight r = load8(x + at, left);
+#pragma unroll
+        for (int e = 0; e < 8; e++) v.x[e] += r.x[e];
+    }
+    store8(out + at, v, left);
+}
+
+// ------------------------------------------------------------------------------------------ sums over a row
+// the sum over the threads of a row: a wave, or (TPR > 64) the whole workgroup
+template <int TPR>
+__device__ __forceinline__ float row_sum(float x, float *lds)
+{
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
+    if (TPR > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+        __syncthreads();
+        x = 0.f;
+#pragma unroll
+        for (int i = 0; i < TPR / 64; i++) x += lds[i];
+    }
+    return x;
+}
+
+struct NormArgs {
+    const void *x, *y, *weight, *bias, *dn, *dh, *h;
+    void *h_out, *n, *dx, *dy, *d_weight, *d_bias;
+    float *mean, *rstd, *parts;
+    int rows, width, weight_bf16;
+    float eps, inv_width;
+    Drop drop;
+};
+
+// a row's threads hold its 16-byte chunks c = thread + TPR u, u < NCH
+template <typename T, int TPR, int NCH>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_add_norm_fwd(NormArgs a)
+{
+    constexpr int PER = (TPR < 256 ? 256 : TPR) / TPR;
+    __shared__ float lds[16];
+    const int row = blockIdx.x * PER + threadIdx.x / TPR, t = threadIdx.x % TPR;
+    if (row >= a.rows) return;  // (whole waves; with several waves a row there is one row per workgroup)
+    const Key k = key_of(a.drop);
+    const size_t at = (size_t)row * a.width;
+    Eight h[NCH];
+    float sum = 0.f;
+#pragma unroll
+    for (int u = 0; u < NCH; u++) {
+        const int c = (t + TPR * u) * 8, left = a.width - c;
+        if (left <= 0) {
+#pragma unroll
+            for (int e = 0; e < 8; e++) h[u].x[e] = 0.f;
+            continue;
+        }
+        h[u] = load8((const T *)a.x + at + c, left);
+        if (a.y) {
+            Eight y = load8((const T *)a.y + at + c, left);
+            if (a.drop.threshold) {
+                const Block b = numbers(at + c, a.drop, k);
+#pragma unroll
+                for (int e = 0; e < 8; e++) y.x[e] *= factor(b, e, a.drop);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; e++) h[u].x[e] += y.x[e];
+            store8((T *)a.h_out + at + c, h[u], left);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e++) sum += h[u].x[e];
+    }
+    const float mean = row_sum<TPR>(sum, lds) * a.inv_width;
+    float sq = 0.f;
+#pragma unroll
+    for (int u = 0; u < NCH; u++) {
+        const int left = a.width - (t + TPR * u) * 8;
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            h[u].x[e] = e < left ? h[u].x[e] - mean : 0.f;
+            sq = fmaf(h[u].x[e], h[u].x[e], sq);
+        }
+    }
+    const float rstd = 1.f / sqrtf(row_sum<TPR>(sq, lds) * a.inv_width + a.eps);
+#pragma unroll
+    for (int u = 0; u < NCH; u++) {
+        const int c = (t + TPR * u) * 8, left = a.width - c;
+        if (left <= 0) continue;
+        const Eight w = load_weight(a.weight, a.weight_bf16, c, left);
+        Eight b = {};
+        if (a.bias) b = load_weight(a.bias, a.weight_bf16, c, left);
+#pragma unroll
+        for (int e = 0; e < 8; e++) h[u].x[e] = fmaf(h[u].x[e] * rstd, w.x[e], b.x[e]);
+        store8((T *)a.n + at + c, h[u], left);
+    }
+    if (t == 0) {
+        a.mean[row] = mean;
+        a.rstd[row] = rstd;
+    }
+}
+
+// Rows blockIdx, blockIdx + gridDim, ... of a workgroup's wave (or of the workgroup), the columns' sums of dn xhat and dn in
+// registers throughout; at the end a row of the workgroup's sums: parts[workgroup][2][width]
+template <typename T, int TPR, int NCH>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_add_norm_bwd(NormArgs a)
+{
+    constexpr int PER = (TPR < 256 ? 256 : TPR) / TPR;
+    extern __shared__ __attribute__((aligned(16))) float lds[];  // 32, then (PER > 1) PER rows of `width` up to whole chunks
+    const int sub = threadIdx.x / TPR, t = threadIdx.x % TPR;
+    const Key k = key_of(a.drop);
+    Eight w[NCH], sw[NCH] = {}, sb[NCH] = {};
+#pragma unroll
+    for (int u = 0; u < NCH; u++) {
+        const int c = (t + TPR * u) * 8;
+        if (c < a.width) w[u] = load_weight(a.weight, a.weight_bf16, c, a.width - c);
+    }
+    for (int row = blockIdx.x * PER + sub; row < a.rows; row += gridDim.x * PER) {
+        const size_t at = (size_t)row * a.width;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        Eight hat[NCH], g[NCH];
+        float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+        for (int u = 0; u < NCH; u++) {
+            const int c = (t + TPR * u) * 8, left = a.width - c;
+            if (left <= 0) continue;
+            hat[u] = load8((const T *)a.h + at + c, left);
+            g[u] = load8((const T *)a.dn + at + c, left);
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                hat[u].x[e] = e < left ? (hat[u].x[e] - mean) * rstd : 0.f;
+                sw[u].x[e] = fmaf(g[u].x[e], hat[u].x[e], sw[u].x[e]);
+                sb[u].x[e] += g[u].x[e];
+                g[u].x[e] *= w[u].x[e];
+                s0 += g[u].x[e];
+                s1 = fmaf(g[u].x[e], hat[u].x[e], s1);
+            }
+        }
+        s0 = row_sum<TPR>(s0, lds) * a.inv_width;
+        s1 = row_sum<TPR>(s1, lds + 16) * a.inv_width;
+#pragma unroll
+        for (int u = 0; u < NCH; u++) {
+            const int c = (t + TPR * u) * 8, left = a.width - c;
+            if (left <= 0) continue;
+            Eight d = {};
+            if (a.dh) d = load8((const T *)a.dh + at + c, left);
+#pragma unroll
+            for (int e = 0; e < 8; e++) d.x[e] = fmaf(rstd, g[u].x[e] - s0 - hat[u].x[e] * s1, d.x[e]);
+            store8((T *)a.dx + at + c, d, left);
+            if (a.drop.threshold) {
+                const Block b = numbers(at + c, a.drop, k);
+#pragma unroll
+                for (int e = 0; e < 8; e++) d.x[e] *= factor(b, e, a.drop);
+                store8((T *)a.dy + at + c, d, left);
+            }
+        }
+    }
+    float *out = a.parts + (size_t)blockIdx.x * 2 * a.width;
+    if (PER == 1) {
+#pragma unroll
+        for (int u = 0; u < NCH; u++) {
+            const int c = (t + TPR * u) * 8;
+            if (c >= a.width) continue;
+            store8(out + c, sw[u], a.width - c);
+            store8(out + a.width + c, sb[u], a.width - c);
+        }
+        return;
+    }
+    const int whole = (a.width + 7) & ~7;
+#pragma unroll
+    for (int which = 0; which < 2; which++) {
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < NCH; u++) {
+            const int c = (t + TPR * u) * 8;
+            if (c < a.width) store8(lds + 32 + (size_t)sub * whole + c, which ? sb[u] : sw[u], 8);
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < a.width; c += TPR * PER) {
+            float sum = 0.f;
+#pragma unroll
+            for (int u = 0; u < PER; u++) sum += lds[32 + (size_t)u * whole + c];
+            out[which * a.width + c] = sum;
+        }
+    }
+}
+
+// the workgroups' sums added up in a fixed order: 64 columns a workgroup, 16 runs of parts
+__global__ __launch_bounds__(1024) void k_norm_parts(NormArgs a, int parts)
+{
+    __shared__ float lds[16][64];
+    const int lane = threadIdx.x & 63, run = threadIdx.x >> 6, x = blockIdx.x * 64 + lane;
+    float sum = 0.f;
+    if (x < 2 * a.width)
+        for (int p = run; p < parts; p += 16) sum += a.parts[(size_t)p * 2 * a.width + x];
+    lds[run][lane] = sum;
+    __syncthreads();
+    if (run != 0 || x >= 2 * a.width) return;
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; i++) sum += lds[i][lane];
+    void *out = x < a.width ? a.d_weight : a.d_bias;
+    const int c = x < a.width ? x : x - a.width;
+    if (!out) return;
+    if (a.weight_bf16)
+        ((__bf16 *)out)[c] = (__bf16)sum;
+    else
+        ((float *)out)[c] = sum;
+}
+
+constexpr int kMostWidth = 32768, kMostParts = 1024;
+constexpr long long kMostElements = 1ll << 35;  // 2^32 blocks of eight
+
+// threads a row and chunks a thread: a wave up to 2048 columns, then a workgroup of 256 or 1024
+struct RowShape {
+    int tpr, nch;
+};
+RowShape row_shape(int width)
+{
+    const int chunks = (width + 7) / 8;
+    if (chunks <= 64) return {64, 1};
+    if (chunks <= 128) return {64, 2};
+    if (chunks <= 256) return {64, 4};
+    return chunks <= 1024 ? RowShape{256, 4} : RowShape{1024, 4};
+}
+int norm_parts(int rows, int width)
+{
+    const int per = row_shape(width).tpr == 64 ? 4 : 1, groups = (rows + per - 1) / per;
+    return groups < kMostParts ? groups : kMostParts;
+}
+
+template <typename T, int TPR, int NCH>
+void launch_fwd(const NormArgs &a, hipStream_t st)
+{
+    constexpr int THREADS = TPR < 256 ? 256 : TPR, PER = THREADS / TPR;
+    hipLaunchKernelGGL((k_add_norm_fwd<T, TPR, NCH>), dim3((unsigned)((a.rows + PER - 1) / PER)), dim3(THREADS), 0, st, a);
+}
+template <typename T, int TPR, int NCH>
+void launch_bwd(const NormArgs &a, hipStream_t st)
+{
+    constexpr int THREADS = TPR < 256 ? 256 : TPR, PER = THREADS / TPR;
+    const size_t lds = (32 + (PER > 1 ? (size_t)PER * ((a.width + 7) & ~7) : 0)) * sizeof(float);
+    hipLaunchKernelGGL((k_add_norm_bwd<T, TPR, NCH>), dim3((unsigned)norm_parts(a.rows, a.width)), dim3(THREADS), lds, st, a);
+}
+template <typename T>
+void launch(const NormArgs &a, bool bwd, hipStream_t st)
+{
+    const RowShape s = row_shape(a.width);
+#define HDT_ROWS(TPR, NCH)                                                                     \
+    if (s.tpr == TPR && s.nch == NCH) {                                                        \
+        bwd ? launch_bwd<T, TPR, NCH>(a, st) : launch_fwd<T, TPR, NCH>(a, st);                 \
+        return;                                                                                \
+    }
+    HDT_ROWS(64, 1)
+    HDT_ROWS(64, 2)
+    HDT_ROWS(64, 4)
+    HDT_ROWS(256, 4)
+    HDT_ROWS(1024, 4)
+#undef HDT_ROWS
+}
+
+bool misaligned(const void *p) { return ((uintptr_t)p & 15u) != 0; }
+
+// any: there is an element to drop
+hdt_status_t drop_of(const char *fn, double p, bool any, const int64_t *rng, uint32_t site, Drop *d)
+{
+    if (!hdt_finite(p) || p < 0. || p >= 1.) return hdt_fail(HDT_ERR_INVALID_ARG, "%s: p = %g outside [0, 1)", fn, p);
+    const uint32_t t = (uint32_t)(p * 65536. + 0.5);
+    if (t > 65535) return hdt_fail(HDT_ERR_INVALID_ARG, "%s: p = %g rounds to 1 in steps of 1/65536", fn, p);
+    if (t > 0 && any && !rng) return hdt_fail(HDT_ERR_INVALID_ARG, "%s: NULL generator state", fn);
+    if ((uintptr_t)rng & 7u) return hdt_fail(HDT_ERR_INVALID_ARG, "%s: the generator's state must be 8-byte aligned", fn);
+    *d = {(const long long *)rng, site, t, (float)(65536. / (65536. - t))};
+    return HDT_OK;
+}
+hdt_status_t check_norm(const char *fn, int64_t rows, int32_t width, hdt_dtype_t dt, hdt_dtype_t wdt)
+{
+    if (rows < 0 || width < 0) return hdt_fail(HDT_ERR_INVALID_ARG, "%s: negative size", fn);
+    if (dt != HDT_BF16 && dt != HDT_F32) return hdt_fail(HDT_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, (int)dt);
+    if (wdt != HDT_BF16 && wdt != HDT_F32) return hdt_fail(HDT_ERR_UNSUPPORTED, "%s: unknown dtype %d of the weight", fn, (int)wdt);
+    if (width < 1 || width > kMostWidth) return hdt_fail(HDT_ERR_SHAPE, "%s: width %d outside [1, %d]", fn, width, kMostWidth);
+    if (rows > INT32_MAX || rows * width > kMostElements) return hdt_fail(HDT_ERR_SHAPE, "%s: more than 2^31 rows or 2^35 elements", fn);
+    return HDT_OK;
+}
+
+#define HDT_EXPORT extern "C" __attribute__((visibility("default")))
+
+}  // namespace
+
+HDT_EXPORT hdt_status_t hdt_dropout_add(const void *y, const void *x, void *out, int64_t n, double p, const int64_t *d_rng, uint32_t site,
+                                        hdt_dtype_t dt, void *stream)
+{
+    const char *fn = "hdt_dropout_add";
+    if (n < 0) return hdt_fail(HDT_ERR_INVALID_ARG, "%s: negative size", fn);
+    if (n > kMostElements) return hdt_fail(HDT_ERR_SHAPE, "%s: more than 2^35 elements", fn);
+    if (dt != HDT_BF16 && dt != HDT_F32) return hdt_fail(HDT_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, (int)dt);
+    Drop d;
+    const bool any = n > 0;
+    if (hdt_status_t st = drop_of(fn, p, any, d_rng, site, &d)) return st;
+    if (n == 0) return HDT_OK;
+    if (!y || !out) return hdt_fail(HDT_ERR_INVALID_ARG, "%s: NULL pointer", fn);
+    if (misaligned(y) || misaligned(x) || misaligned(out)) return hdt_fail(HDT_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", fn);
+    hipStream_t st = (hipStream_t)stream;
+    HdtTimer t("hdt_dropout_add", st);
+    const dim3 grid((unsigned)((n + 2047) / 2048)), block(256);
+    if (dt == HDT_BF16)
+        hipLaunchKernelGGL(k_dropout_add<__bf16>, grid, block, 0, st, (const __bf16 *)y, (const __bf16 *)x, (__bf16 *)out, (unsigned long long)n, d);
+    else
+        hipLaunchKernelGGL(k_dropout_add<float>, grid, block, 0, st, (const float *)y, (const float *)x, (float *)out, (unsigned long long)n, d);
+    HDT_HIP_TRY(hipGetLastError());
+    return HDT_OK;
+}
+
+HDT_EXPORT hdt_status_t hdt_add_norm_fwd(const void *x, const void *y, const void *weight, const void *bias, int64_t rows, int32_t width,
+                                         float eps, double p, const int64_t *d_rng, uint32_t site, void *h, void *n, float *mean, float *rstd,
+                                         hdt_dtype_t dt, hdt_dtype_t weight_dt, void *stream)
+{
+    const char *fn = "hdt_add_norm_fwd";
+    if (hdt_status_t st = check_norm(fn, rows, width, dt, weight_dt)) return st;
+    if (!hdt_finite(eps) || eps < 0.f) return hdt_fail(HDT_ERR_INVALID_ARG, "%s: eps = %g", fn, (double)eps);
+    NormArgs a = {};
+    const bool any = rows > 0;
+    if (hdt_status_t st = drop_of(fn, p, any, d_rng, site, &a.drop)) return st;
+    if (rows == 0) return HDT_OK;
+    if (!x || !weight || !n || !mean || !rstd || (y && !h)) return hdt_fail(HDT_ERR_INVALID_ARG, "%s: NULL pointer", fn);
+    for (const void *q : {x, y, weight, bias, (const void *)h, (const void *)n})
+        if (misaligned(q)) return hdt_fail(HDT_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", fn);
+    if (n == x || n == y || (y && (h == x || h == y || h == n))) return hdt_fail(HDT_ERR_INVALID_ARG, "%s: output aliases an input or the other output", fn);
+    if (!y) a.drop.threshold = 0;
+    a.x = x, a.y = y, a.weight = weight, a.bias = bias, a.h_out = h, a.n = n, a.mean = mean, a.rstd = rstd;
+    a.rows = (int)rows, a.width = width, a.weight_bf16 = weight_dt == HDT_BF16, a.eps = eps, a.inv_width = 1.f / (float)width;
+    hipStream_t st = (hipStream_t)stream;
+    HdtTimer t("hdt_add_norm_fwd", st);
+    dt == HDT_BF16 ? launch<__bf16>(a, false, st) : launch<float>(a, false, st);
+    HDT_HIP_TRY(hipGetLastError());
+    return HDT_OK;
+}
+
+HDT_EXPORT size_t hdt_add_norm_bwd_workspace_bytes(int64_t rows, int32_t width)
+{
+    if (rows <= 0 || rows > INT32_MAX || width < 1 || width > kMostWidth) return 0;
+    return (size_t)norm_parts((int)rows, width) * 2 * width * sizeof(float);
+}
+
+HDT_EXPORT hdt_status_t hdt_add_norm_bwd(const void *dn, const void *dh, const void *h, const void *weight, const float *mean,
+                                         const float *rstd, int64_t rows, int32_t width, double p, const int64_t *d_rng, uint32_t site,
+                                         void *dx, void *dy, void *d_weight, void *d_bias, hdt_dtype_t dt, hdt_dtype_t weight_dt,
+                                         void *workspace, size_t workspace_bytes, void *stream)
+{
+    const char *fn = "hdt_add_norm_bwd";
+    if (hdt_status_t st = check_norm(fn, rows, width, dt, weight_dt)) return st;
+    NormArgs a = {};
+    const bool any = rows > 0;
+    if (hdt_status_t st = drop_of(fn, p, any, d_rng, site, &a.drop)) return st;
+    if (!d_weight) return hdt_fail(HDT_ERR_INVALID_ARG, "%s: NULL pointer", fn);
+    if (rows > 0) {
+        if (!dn || !h || !weight || !mean || !rstd || !dx || (a.drop.threshold && !dy)) return hdt_fail(HDT_ERR_INVALID_ARG, "%s: NULL pointer", fn);
+        const void *in[] = {dn, dh, h, weight, mean, rstd}, *out[] = {dx, a.drop.threshold ? dy : nullptr};
+        for (const void *q : {dn, dh, h, weight, (const void *)dx, (const void *)dy})
+            if (misaligned(q)) return hdt_fail(HDT_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", fn);
+        for (const void *o : out)
+            for (const void *q : in)
+                if (o && o == q) return hdt_fail(HDT_ERR_INVALID_ARG, "%s: output aliases an input", fn);
+        if (out[0] == out[1]) return hdt_fail(HDT_ERR_INVALID_ARG, "%s: outputs alias each other", fn);
+        const size_t need = hdt_add_norm_bwd_workspace_bytes(rows, width);
+        if (!workspace || workspace_bytes < need || misaligned(workspace))
+            return hdt_fail(HDT_ERR_INVALID_ARG, "%s: a 16-byte aligned workspace of %zu bytes needed, %zu given", fn, need, workspace ? workspace_bytes : (size_t)0);
+    }
+    a.dn = dn, a.dh = dh, a.h = h, a.weight = weight, a.mean = (float *)mean, a.rstd = (float *)rstd, a.dx = dx, a.dy = dy;
+    a.d_weight = d_weight, a.d_bias = d_bias, a.parts = (float *)workspace;
+    a.rows = (int)rows, a.width = width, a.weight_bf16 = weight_dt == HDT_BF16, a.inv_width = 1.f / (float)width;
+    hipStream_t st = (hipStream_t)stream;
+    if (rows > 0) {
+        HdtTimer t("hdt_add_norm_bwd", st);
+        dt == HDT_BF16 ? launch<__bf16>(a, true, st) : launch<float>(a, true, st);
+        HDT_HIP_TRY(hipGetLastError());
+    }
+    HdtTimer t("hdt_norm_parts", st);
+    hipLaunchKernelGGL(k_norm_parts, dim3((unsigned)((2 * width + 63) / 64)), dim3(1024), 0, st, a, rows > 0 ? norm_parts((int)rows, width) : 0);
+    HDT_HIP_TRY(hipGetLastError());
+    return HDT_OK;
+}

@@ -1,0 +1,171 @@
+// Pieces shared by the kernels of self-attention with a relative position bias (hdt_rel_fwd.hip, hdt_rel_bwd.hip).
+//
+//     A_ij = scale q_i . k_j + bias[bucket(j - p_i)][head],   P = softmax over the visible j,   O = P V
+//
+// p_i = start + i is the position query i stands at; it is real iff 0 <= p_i < length; key j is visible to it iff j < length and,
+// in the causal form, j <= p_i.  The bias depends on the distance j - p_i alone and is constant from max_distance on, so of the
+// 32 x 32 blocks of pairs that a wave works on
+//   * most are "far": one constant for the whole block, which joins the exponent's own constant and costs nothing;
+//   * the few within max_distance of the diagonal are "near": the accumulators of Q K^T start from the head's bias by distance
+//     (bias / scale, in LDS) instead of zero, so that they cost LDS reads but no arithmetic.  The causal mask is part of that
+//     table: minus infinity at positive distances.  Every block that the diagonal crosses is a near one.
+// Accumulators hold pairs with one side along the lanes (column l % 32) and the other along the registers (rows of C, hdt_mfma.h).
+//
+// bf16 tensors go through v_mfma_f32_32x32x16_bf16, fp32 ones through v_mfma_f32_32x32x2_f32, whose C layout is the same; a lane's
+// 16 bytes of a row are 8 contraction values of one instruction in bf16 and one value of each of four in fp32 (Op<T>).
+#pragma once
+
+#include "hdt_internal.h"
+#include "hdt_mfma.h"
+#include "hdt_tile.h"
+
+namespace hdt_rel {
+
+using namespace hdt_tile;
+
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
+constexpr int kPad = 64;              // distances the table goes on beyond the last one that matters
+constexpr float kHidden = 1e6f;       // a bias from -1e6 down hides a bucket, one from 1e6 up counts as 1e6
+
+// one row-side operand fragment (16 bytes of a row) and the contractions it takes part in
+template <typename T>
+struct Op;
+template <>
+struct Op<__bf16> {
+    typedef bf16x8 Frag;
+    static constexpr int PER_STEP = 16;  // values of the contraction a step covers
+    static __device__ __forceinline__ Frag zero() { return zero_bf16x8(); }
+    static __device__ __forceinline__ f32x16 mma(Frag a, Frag b, f32x16 c) { return mfma_32x32x16(a, b, c); }
+};
+template <>
+struct Op<float> {
+    typedef f32x4 Frag;
+    static constexpr int PER_STEP = 8;
+    static __device__ __forceinline__ Frag zero() { return f32x4{0.f, 0.f, 0.f, 0.f}; }
+    static __device__ __forceinline__ f32x16 mma(Frag a, Frag b, f32x16 c)
+    {
+#pragma unroll
+        for (int e = 0; e < 4; e++) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+        return c;
+    }
+};
+
+// What a kernel does with blocks of 32 x 32 held in C fragments (P, dS) as the B operand of the next contraction
+template <typename T>
+struct Weights;
+template <>
+struct Weights<__bf16> {  // rounded to bf16: the operand type of the fast contraction; its sum is taken before
+    bf16x8 lo, hi;
+    __device__ __forceinline__ explicit Weights(const f32x16 &p) : lo(pack_bf16x8(p, 0)), hi(pack_bf16x8(p, 8)) {}
+};
+template <>
+struct Weights<float> {
+    f32x16 p;
+    __device__ __forceinline__ explicit Weights(const f32x16 &x) : p(x) {}
+};
+
+// Rows of a [.][D] tensor in LDS: tiles of R rows, 16-byte chunks permuted within a row against bank conflicts (swz).
+template <typename T, int D>
+struct Rows {
+    static constexpr int ROWB = D * (int)sizeof(T), CPR = ROWB / 16, RPI = 1024 / ROWB;  // rows per wave-level load
+    static constexpr int STEPS = D / Op<T>::PER_STEP, BLOCKS = D / 32;
+    typedef typename Op<T>::Frag Frag;
+
+    // 16 bytes of row r0 + l % 32: step st
+    static __device__ __forceinline__ Frag read(const char *tile, const RowLane &r, int r0, int st)
+    {
+        return *reinterpret_cast<const Frag *>(tile + (r0 + r.row) * ROWB + ((((st << 1) ^ r.x)) << 4));
+    }
+    // acc += (rows r0 .. r0 + 31 of the tile, columns 32 j ..)^T times the weights of those rows
+    static __device__ __forceinline__ f32x16 weigh(const char *tile, const TrLane &t, int lane, int r0, int j, const Weights<T> &w, f32x16 acc)
+    {
+        if constexpr (sizeof(T) == 2) {
+            acc = mfma_32x32x16(read_tr<ROWB>(tile, t, r0, j), w.lo, acc);
+            acc = mfma_32x32x16(read_tr<ROWB>(tile, t, r0 + 16, j), w.hi, acc);
+        } else {
+            const int c = 8 * j + ((lane & 31) >> 2), hf = lane >> 5;
+#pragma unroll
+            for (int v = 0; v < 16; v++) {
+                const int r = r0 + 8 * (v >> 2) + (v & 3) + 4 * hf;
+                const float a = *reinterpret_cast<const float *>(tile + r * ROWB + ((c ^ swz<CPR>(r & 31)) << 4) + (lane & 3) * 4);
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w.p[v], acc, 0, 0, 0);
+            }
+        }
+        return acc;
+    }
+    // Starts loading R rows of a tensor from `base` on into a tile, this wave's share of NW.  Rows in front of row `low` or behind row
+    // `last` (of the R) are not read: copies of those two stand in their place.
+    template <int R, int NW>
+    static __device__ __forceinline__ void load(const void *base, uint32_t stride_bytes, int low, int last, uint32_t lds, int wave, int lane)
+    {
+        constexpr int NI = R / RPI / NW;
+        static_assert(NI >= 1 && R % (RPI * NW) == 0, "a wave loads whole instructions");
+        const int lr = lane / CPR, c = lane % CPR;
+#pragma unroll
+        for (int i = 0; i < NI; i++) {
+            const int r = (wave * NI + i) * RPI + lr;
+            dma16(base, (uint32_t)min(max(r, low), last) * stride_bytes + (uint32_t)((c ^ swz<CPR>(r & 31)) << 4),
+                  lds + (uint32_t)((wave * NI + i) * 1024));
+        }
+    }
+};
+
+// The rows of a sample that stand for positions, and its keys
+struct Sample {
+    int start, length;  // position of query 0; keys
+    int lo, hi;         // queries [lo, hi) are real
+};
+__device__ __forceinline__ Sample sample_of(const int32_t *lengths, const int32_t *starts, int b, int n_q, int n_kv)
+{
+    Sample s;
+    s.length = lengths ? min(max(as_const(lengths)[b], 0), n_kv) : n_kv;
+    const int64_t start = starts ? as_const(starts)[b] : 0;
+    s.lo = (int)min(max(-start, (int64_t)0), (int64_t)n_q);
+    s.hi = (int)min(max((int64_t)s.length - start, (int64_t)s.lo), (int64_t)n_q);
+    s.start = (int)start;
+    return s;
+}
+
+// bias by distance of `heads` heads from h0 on, as bias / scale: entry d + max_distance + kPad, distances -max_distance - kPad up
+// to kPad - 1 (causal: minus infinity from 1 on) or max_distance + kPad - 1
+__host__ __device__ __forceinline__ int table_length(int max_distance, bool causal) { return (causal ? 1 : 2) * max_distance + 2 * kPad; }
+
+struct BiasArgs {
+    const void *bias;      // [n_buckets][heads]
+    const int32_t *table;  // [2 max_distance + 1]
+    int n_buckets, heads, max_distance, bf16;
+    float inv_scale;
+};
+__device__ __forceinline__ float bias_of(const BiasArgs &a, int distance, int head)
+{
+    const int M = a.max_distance, bucket = min(max(a.table[min(max(distance, -M), M) + M], 0), a.n_buckets - 1);
+    const size_t at = (size_t)bucket * a.heads + head;
+    const float x = a.bf16 ? (float)((const __bf16 *)a.bias)[at] : ((const float *)a.bias)[at];
+    // Values that stand for a mask are one (kHidden): a row that saw nothing else would have an LSE next to them, in whose fp32 the
+    // logarithm of its sum is lost, and with it the row's gradients.
+    return x <= -kHidden ? -INFINITY : fminf(x, kHidden) * a.inv_scale;
+}
+template <bool CAUSAL>
+__device__ __forceinline__ void fill_table(float *lds, const BiasArgs &a, int h0, int heads, int tid, int threads)
+{
+    const int len = table_length(a.max_distance, CAUSAL);
+    for (int g = 0; g < heads; g++)
+        for (int x = tid; x < len; x += threads) {
+            const int d = x - a.max_distance - kPad;
+            lds[g * len + x] = CAUSAL && d > 0 ? -INFINITY : bias_of(a, d, h0 + g);
+        }
+}
+
+enum class Kind { SKIP, NEAR, FAR_BEHIND, FAR_AHEAD };
+// of a block of keys [k0, k0 + 31] and positions [p0, p1] (p1 - p0 <= 31)
+template <bool CAUSAL>
+__device__ __forceinline__ Kind kind_of(int k0, int p0, int p1, int M, int length)
+{
+    if ((CAUSAL && k0 > p1) || k0 >= length) return Kind::SKIP;
+    if (k0 + 31 - p0 <= -M) return Kind::FAR_BEHIND;
+    if (!CAUSAL && k0 - p1 >= M) return Kind::FAR_AHEAD;
+    return Kind::NEAR;
+}
+
+}  // namespace hdt_rel
