@@ -155,11 +155,12 @@ hdt_status_t hdt_fail(hdt_status_t st, const char *fmt, ...);
                             #expr, hipGetErrorString(_e));                                    \
     } while (0)
 
-// neither infinite nor NaN, by the bits: the sources are compiled on the assumption that comparisons meet no NaN
+// neither infinite nor NaN, by the bits of a copy in memory: the sources are compiled on the assumption that no value is a NaN
+// (-fno-honor-nans), by which a test of the value itself is left out
 inline bool hdt_finite(double x)
 {
-    uint64_t u;
-    __builtin_memcpy(&u, &x, sizeof(u));
+    volatile double kept = x;
+    const uint64_t u = *reinterpret_cast<volatile uint64_t *>(&kept);
     return (u >> 52 & 0x7ffu) != 0x7ffu;
 }
 bool hdt_layout_ok(const hdt_layout_t *l);
