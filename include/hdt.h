@@ -391,7 +391,8 @@ hdt_status_t hdt_hpe_add(const int32_t *d_p, int32_t batch, int32_t n_pos, int32
  *   strides           in elements, rows of head_dim consecutive values, multiples of 16 bytes; all zero: dense [batch][heads][rows]
  *                     [head_dim].  A row stride is at most 2^20.  Inputs may be broadcast (stride 0 over batch or heads), the rows
  *                     of an output must not overlap.
- *   head_dim 64 or 128; n_q, n_kv up to 2^24; every size may be 0.  Tensor pointers 16-byte aligned.
+ *   head_dim 64 or 128; n_q, n_kv up to 2^24, and batch (heads + kv_heads) times the tiles of 128 rows of the longer of them below 2^20;
+ *   every size but kv_heads may be 0.  Tensor pointers 16-byte aligned.
  */
 typedef struct {
     int64_t batch, head, row;
@@ -440,7 +441,7 @@ hdt_status_t hdt_rel_attn_bwd(const hdt_rel_attn_t *h_call, const void *q, const
  * of the first word first; an element is kept iff its bits are at least t = round(65536 p), times 65536 / (65536 - t).
  * d_rng: device, int64 [2] = (seed, step), 8-byte aligned.  The kernels read it, so a captured graph that increments the step drops others
  * at every replay; a backward needs the values its forward had.  `site` tells calls with the same seed and step apart.  p = 0 drops
- * nothing and needs no d_rng.  Tensors are dense; at most 2^35 elements.
+ * nothing and needs no d_rng.  Tensors are dense; at most 2^35 elements, 2^31 - 1 rows.
  *
  * hdt_dropout_add -- out = x + y o m on n elements; x may be NULL (dropout by itself, and its gradient: the same call on the gradient);
  *   out may be x or y.

@@ -10,6 +10,8 @@
 //
 // All of it is bound by memory: a row is read once, held in registers between its statistics and its result, and written once.
 // Sums and statistics are in fp32; h is rounded once, when it is written (the norm is taken of the unrounded sum).
+#include <algorithm>
+
 #include "hdt_internal.h"
 #include "hdt_mfma.h"
 
@@ -141,21 +143,21 @@ template <typename T>
 __global__ __launch_bounds__(256) void k_dropout_add(const T *y, const T *x, T *out, unsigned long long n, Drop d)
 {
     const Key k = key_of(d);
-    const unsigned long long at = ((unsigned long long)blockIdx.x * 256 + threadIdx.x) * 8;
-    if (at >= n) return;
-    const int left = (int)min(n - at, 8ull);
-    Eight v = load8(y + at, left);
-    if (d.threshold) {
-        const Block b = philox((uint32_t)(at >> 3), d.site, k);
+    for (unsigned long long at = ((unsigned long long)blockIdx.x * 256 + threadIdx.x) * 8; at < n; at += (unsigned long long)gridDim.x * 2048) {
+        const int left = (int)min(n - at, 8ull);
+        Eight v = load8(y + at, left);
+        if (d.threshold) {
+            const Block b = philox((uint32_t)(at >> 3), d.site, k);
 #pragma unroll
-        for (int e = 0; e < 8; e++) v.x[e] *= factor(b, e, d);
-    }
-    if (x) {
-        const Eight r = load8(x + at, left);
+            for (int e = 0; e < 8; e++) v.x[e] *= factor(b, e, d);
+        }
+        if (x) {
+            const Eight r = load8(x + at, left);
 #pragma unroll
-        for (int e = 0; e < 8; e++) v.x[e] += r.x[e];
+            for (int e = 0; e < 8; e++) v.x[e] += r.x[e];
+        }
+        store8(out + at, v, left);
     }
-    store8(out + at, v, left);
 }
 
 // ------------------------------------------------------------------------------------------ sums over a row
@@ -191,61 +193,62 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_add_norm_fwd(NormArgs
 {
     constexpr int PER = (TPR < 256 ? 256 : TPR) / TPR;
     __shared__ float lds[16];
-    const int row = blockIdx.x * PER + threadIdx.x / TPR, t = threadIdx.x % TPR;
-    if (row >= a.rows) return;  // (whole waves; with several waves a row there is one row per workgroup)
+    const int sub = threadIdx.x / TPR, t = threadIdx.x % TPR;
     const Key k = key_of(a.drop);
-    const size_t at = (size_t)row * a.width;
-    Eight h[NCH];
-    float sum = 0.f;
+    for (int64_t row = (int64_t)blockIdx.x * PER + sub; row < a.rows; row += (int64_t)gridDim.x * PER) {  // (the same for whole waves, and for a workgroup that has one row)
+        const size_t at = (size_t)row * a.width;
+        Eight h[NCH];
+        float sum = 0.f;
 #pragma unroll
-    for (int u = 0; u < NCH; u++) {
-        const int c = (t + TPR * u) * 8, left = a.width - c;
-        if (left <= 0) {
+        for (int u = 0; u < NCH; u++) {
+            const int c = (t + TPR * u) * 8, left = a.width - c;
+            if (left <= 0) {
 #pragma unroll
-            for (int e = 0; e < 8; e++) h[u].x[e] = 0.f;
-            continue;
-        }
-        h[u] = load8((const T *)a.x + at + c, left);
-        if (a.y) {
-            Eight y = load8((const T *)a.y + at + c, left);
-            if (a.drop.threshold) {
-                const Block b = numbers(at + c, a.drop, k);
+                for (int e = 0; e < 8; e++) h[u].x[e] = 0.f;
+                continue;
+            }
+            h[u] = load8((const T *)a.x + at + c, left);
+            if (a.y) {
+                Eight y = load8((const T *)a.y + at + c, left);
+                if (a.drop.threshold) {
+                    const Block b = numbers(at + c, a.drop, k);
 #pragma unroll
-                for (int e = 0; e < 8; e++) y.x[e] *= factor(b, e, a.drop);
+                    for (int e = 0; e < 8; e++) y.x[e] *= factor(b, e, a.drop);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; e++) h[u].x[e] += y.x[e];
+                store8((T *)a.h_out + at + c, h[u], left);
             }
 #pragma unroll
-            for (int e = 0; e < 8; e++) h[u].x[e] += y.x[e];
-            store8((T *)a.h_out + at + c, h[u], left);
+            for (int e = 0; e < 8; e++) sum += h[u].x[e];
         }
+        const float mean = row_sum<TPR>(sum, lds) * a.inv_width;
+        float sq = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; e++) sum += h[u].x[e];
-    }
-    const float mean = row_sum<TPR>(sum, lds) * a.inv_width;
-    float sq = 0.f;
+        for (int u = 0; u < NCH; u++) {
+            const int left = a.width - (t + TPR * u) * 8;
 #pragma unroll
-    for (int u = 0; u < NCH; u++) {
-        const int left = a.width - (t + TPR * u) * 8;
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-            h[u].x[e] = e < left ? h[u].x[e] - mean : 0.f;
-            sq = fmaf(h[u].x[e], h[u].x[e], sq);
+            for (int e = 0; e < 8; e++) {
+                h[u].x[e] = e < left ? h[u].x[e] - mean : 0.f;
+                sq = fmaf(h[u].x[e], h[u].x[e], sq);
+            }
         }
-    }
-    const float rstd = 1.f / sqrtf(row_sum<TPR>(sq, lds) * a.inv_width + a.eps);
+        const float rstd = 1.f / sqrtf(row_sum<TPR>(sq, lds) * a.inv_width + a.eps);
 #pragma unroll
-    for (int u = 0; u < NCH; u++) {
-        const int c = (t + TPR * u) * 8, left = a.width - c;
-        if (left <= 0) continue;
-        const Eight w = load_weight(a.weight, a.weight_bf16, c, left);
-        Eight b = {};
-        if (a.bias) b = load_weight(a.bias, a.weight_bf16, c, left);
+        for (int u = 0; u < NCH; u++) {
+            const int c = (t + TPR * u) * 8, left = a.width - c;
+            if (left <= 0) continue;
+            const Eight w = load_weight(a.weight, a.weight_bf16, c, left);
+            Eight b = {};
+            if (a.bias) b = load_weight(a.bias, a.weight_bf16, c, left);
 #pragma unroll
-        for (int e = 0; e < 8; e++) h[u].x[e] = fmaf(h[u].x[e] * rstd, w.x[e], b.x[e]);
-        store8((T *)a.n + at + c, h[u], left);
-    }
-    if (t == 0) {
-        a.mean[row] = mean;
-        a.rstd[row] = rstd;
+            for (int e = 0; e < 8; e++) h[u].x[e] = fmaf(h[u].x[e] * rstd, w.x[e], b.x[e]);
+            store8((T *)a.n + at + c, h[u], left);
+        }
+        if (t == 0) {
+            a.mean[row] = mean;
+            a.rstd[row] = rstd;
+        }
     }
 }
 
@@ -264,7 +267,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_add_norm_bwd(NormArgs
         const int c = (t + TPR * u) * 8;
         if (c < a.width) w[u] = load_weight(a.weight, a.weight_bf16, c, a.width - c);
     }
-    for (int row = blockIdx.x * PER + sub; row < a.rows; row += gridDim.x * PER) {
+    for (int64_t row = (int64_t)blockIdx.x * PER + sub; row < a.rows; row += (int64_t)gridDim.x * PER) {
         const size_t at = (size_t)row * a.width;
         const float mean = a.mean[row], rstd = a.rstd[row];
         Eight hat[NCH], g[NCH];
@@ -374,7 +377,7 @@ RowShape row_shape(int width)
 }
 int norm_parts(int rows, int width)
 {
-    const int per = row_shape(width).tpr == 64 ? 4 : 1, groups = (rows + per - 1) / per;
+    const int per = row_shape(width).tpr == 64 ? 4 : 1, groups = (int)(((int64_t)rows + per - 1) / per);
     return groups < kMostParts ? groups : kMostParts;
 }
 
@@ -382,7 +385,7 @@ template <typename T, int TPR, int NCH>
 void launch_fwd(const NormArgs &a, hipStream_t st)
 {
     constexpr int THREADS = TPR < 256 ? 256 : TPR, PER = THREADS / TPR;
-    hipLaunchKernelGGL((k_add_norm_fwd<T, TPR, NCH>), dim3((unsigned)((a.rows + PER - 1) / PER)), dim3(THREADS), 0, st, a);
+    hipLaunchKernelGGL((k_add_norm_fwd<T, TPR, NCH>), dim3((unsigned)std::min<int64_t>(((int64_t)a.rows + PER - 1) / PER, 1 << 20)), dim3(THREADS), 0, st, a);
 }
 template <typename T, int TPR, int NCH>
 void launch_bwd(const NormArgs &a, hipStream_t st)
@@ -450,7 +453,7 @@ HDT_EXPORT hdt_status_t hdt_dropout_add(const void *y, const void *x, void *out,
     if (misaligned(y) || misaligned(x) || misaligned(out)) return hdt_fail(HDT_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", fn);
     hipStream_t st = (hipStream_t)stream;
     HdtTimer t("hdt_dropout_add", st);
-    const dim3 grid((unsigned)((n + 2047) / 2048)), block(256);
+    const dim3 grid((unsigned)(n > (1ll << 31) ? 1 << 20 : (n + 2047) / 2048)), block(256);  // (a launch has fewer than 2^32 threads)
     if (dt == HDT_BF16)
         hipLaunchKernelGGL(k_dropout_add<__bf16>, grid, block, 0, st, (const __bf16 *)y, (const __bf16 *)x, (__bf16 *)out, (unsigned long long)n, d);
     else

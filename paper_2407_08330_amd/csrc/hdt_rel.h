@@ -25,7 +25,7 @@ using namespace hdt_tile;
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 
-constexpr int kPad = 64;              // distances the table goes on beyond the last one that matters
+constexpr int kPad = 128;             // distances the table goes on beyond the last one that matters: as far as 64 x 32 pairs reach, rows that are not real among them
 constexpr float kHidden = 1e6f;       // a bias from -1e6 down hides a bucket, one from 1e6 up counts as 1e6
 
 // one row-side operand fragment (16 bytes of a row) and the contractions it takes part in
@@ -94,19 +94,54 @@ struct Rows {
         }
         return acc;
     }
-    // Starts loading R rows of a tensor from `base` on into a tile, this wave's share of NW.  Rows in front of row `low` or behind row
-    // `last` (of the R) are not read: copies of those two stand in their place.
-    template <int R, int NW>
-    static __device__ __forceinline__ void load(const void *base, uint32_t stride_bytes, int low, int last, uint32_t lds, int wave, int lane)
+};
+
+// Two tensors whose rows travel together (K and V; Q and dO): tiles of R rows of each into a stage of a ring in LDS (tile of the
+// first, tile of the second), this wave's share of NW.
+template <typename T, int D, int R, int NW>
+struct Pair {
+    typedef Rows<T, D> RowsT;
+    static constexpr int TILE = R * RowsT::ROWB, STAGE = 2 * TILE, NI = R / RowsT::RPI / NW;
+    static_assert(NI >= 1 && R % (RowsT::RPI * NW) == 0, "a wave loads whole instructions");
+    const char *a, *b;               // row 0 of the two
+    uint32_t stride_a, stride_b;     // bytes
+    uint32_t off_a[NI], off_b[NI];   // this lane's bytes of the rows it loads, from the tile's first row on
+    uint32_t lds;
+    int wave, lane;
+
+    __device__ __forceinline__ void init(const void *pa, int64_t row_a, const void *pb, int64_t row_b, const char *smem, int w, int l)
     {
-        constexpr int NI = R / RPI / NW;
-        static_assert(NI >= 1 && R % (RPI * NW) == 0, "a wave loads whole instructions");
-        const int lr = lane / CPR, c = lane % CPR;
+        a = (const char *)pa, b = (const char *)pb, stride_a = (uint32_t)row_a * sizeof(T), stride_b = (uint32_t)row_b * sizeof(T);
+        lds = lds_addr(smem), wave = w, lane = l;
+        const int c = l % RowsT::CPR;
 #pragma unroll
         for (int i = 0; i < NI; i++) {
-            const int r = (wave * NI + i) * RPI + lr;
-            dma16(base, (uint32_t)min(max(r, low), last) * stride_bytes + (uint32_t)((c ^ swz<CPR>(r & 31)) << 4),
-                  lds + (uint32_t)((wave * NI + i) * 1024));
+            const int r = (w * NI + i) * RowsT::RPI + l / RowsT::CPR;
+            off_a[i] = (uint32_t)r * stride_a + (uint32_t)((c ^ swz<RowsT::CPR>(r & 31)) << 4);
+            off_b[i] = (uint32_t)r * stride_b + (uint32_t)((c ^ swz<RowsT::CPR>(r & 31)) << 4);
+        }
+    }
+    // Starts loading rows r0 .. r0 + R - 1.  Rows in front of row `low` or behind row `last` are not read: copies of those two stand
+    // in their place.
+    __device__ __forceinline__ void request(int r0, int low, int last, int stage) const
+    {
+        const char *pa = a + (size_t)r0 * stride_a, *pb = b + (size_t)r0 * stride_b;
+        const uint32_t at = lds + (uint32_t)(stage * STAGE + wave * NI * 1024);
+        if (low <= r0 && last >= r0 + R - 1) {
+#pragma unroll
+            for (int i = 0; i < NI; i++) {
+                dma16(pa, off_a[i], at + i * 1024);
+                dma16(pb, off_b[i], at + TILE + i * 1024);
+            }
+        } else {
+            const int c = lane % RowsT::CPR;
+#pragma unroll
+            for (int i = 0; i < NI; i++) {
+                const int r = (wave * NI + i) * RowsT::RPI + lane / RowsT::CPR, from = min(max(r, low - r0), last - r0);
+                const uint32_t chunk = (uint32_t)((c ^ swz<RowsT::CPR>(r & 31)) << 4);
+                dma16(pa, (uint32_t)from * stride_a + chunk, at + i * 1024);
+                dma16(pb, (uint32_t)from * stride_b + chunk, at + TILE + i * 1024);
+            }
         }
     }
 };
@@ -137,10 +172,14 @@ struct BiasArgs {
     int n_buckets, heads, max_distance, bf16;
     float inv_scale;
 };
+__device__ __forceinline__ int bucket_of(const BiasArgs &a, int distance)
+{
+    const int M = a.max_distance;
+    return min(max(a.table[min(max(distance, -M), M) + M], 0), a.n_buckets - 1);
+}
 __device__ __forceinline__ float bias_of(const BiasArgs &a, int distance, int head)
 {
-    const int M = a.max_distance, bucket = min(max(a.table[min(max(distance, -M), M) + M], 0), a.n_buckets - 1);
-    const size_t at = (size_t)bucket * a.heads + head;
+    const size_t at = (size_t)bucket_of(a, distance) * a.heads + head;
     const float x = a.bf16 ? (float)((const __bf16 *)a.bias)[at] : ((const float *)a.bias)[at];
     // Values that stand for a mask are one (kHidden): a row that saw nothing else would have an LSE next to them, in whose fp32 the
     // logarithm of its sum is lost, and with it the row's gradients.
@@ -158,14 +197,36 @@ __device__ __forceinline__ void fill_table(float *lds, const BiasArgs &a, int h0
 }
 
 enum class Kind { SKIP, NEAR, FAR_BEHIND, FAR_AHEAD };
-// of a block of keys [k0, k0 + 31] and positions [p0, p1] (p1 - p0 <= 31)
-template <bool CAUSAL>
+// of W keys from k0 on and positions [p0, p1] (p1 - p0 <= 31, W <= 64)
+template <bool CAUSAL, int W>
 __device__ __forceinline__ Kind kind_of(int k0, int p0, int p1, int M, int length)
 {
     if ((CAUSAL && k0 > p1) || k0 >= length) return Kind::SKIP;
-    if (k0 + 31 - p0 <= -M) return Kind::FAR_BEHIND;
+    if (k0 + W - 1 - p0 <= -M) return Kind::FAR_BEHIND;
     if (!CAUSAL && k0 - p1 >= M) return Kind::FAR_AHEAD;
     return Kind::NEAR;
+}
+
+// A value of this lane and of the other lane of its column, in the other half-wave, in a fixed order: the lower half's, the upper
+// half's.  (The second operand is made opaque: of two results of one value the compiler takes one.)
+struct Halves {
+    float lower, upper;
+};
+__device__ __forceinline__ Halves halves(float x)
+{
+    const unsigned a = __builtin_bit_cast(unsigned, x), b = (unsigned)opaque((int)a);
+    const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+    return {__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1])};
+}
+__device__ __forceinline__ float max_halves(float x)
+{
+    const Halves h = halves(x);
+    return fmaxf(h.lower, h.upper);
+}
+__device__ __forceinline__ float sum_halves(float x)
+{
+    const Halves h = halves(x);
+    return h.lower + h.upper;
 }
 
 }  // namespace hdt_rel

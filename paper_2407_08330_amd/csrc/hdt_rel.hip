@@ -22,6 +22,7 @@ __global__ void k_rel_table(int32_t *table, int n_buckets, int max_distance, int
 }
 
 constexpr int kMostRows = 1 << 24, kMostDistance = 1024, kMostBuckets = 4096;
+constexpr int64_t kMostGrid = (1 << 20) - 1;  // tiles of 128 rows
 constexpr int64_t kMostRowStride = 1 << 20;  // elements: a tile's rows stay within 32-bit byte offsets
 
 struct View {
@@ -79,8 +80,9 @@ hdt_status_t check(const char *fn, const hdt_rel_attn_t *d)
         return hdt_fail(HDT_ERR_SHAPE, "%s: max_distance %d outside [1, %d]", fn, d->max_distance, kMostDistance);
     if (d->n_buckets < 1 || d->n_buckets > kMostBuckets)
         return hdt_fail(HDT_ERR_SHAPE, "%s: n_buckets %d outside [1, %d]", fn, d->n_buckets, kMostBuckets);
-    const int64_t rows = (int64_t)d->batch * d->heads * (((int64_t)d->n_q + 127) / 128), keys = (int64_t)d->batch * d->kv_heads * (((int64_t)d->n_kv + 127) / 128);
-    if (rows > 0x1ffff00 || keys > 0x1ffff00 || (int64_t)d->batch * d->heads * d->n_q > 0x7fffff00LL)
+    // a launch has fewer than 2^32 threads
+    const int64_t tiles_q = ((int64_t)d->n_q + 127) / 128, tiles_k = ((int64_t)d->n_kv + 127) / 128, both = (int64_t)d->batch * ((int64_t)d->heads + d->kv_heads);
+    if (both > kMostGrid || both * (tiles_q > tiles_k ? tiles_q : tiles_k) > kMostGrid)
         return hdt_fail(HDT_ERR_SHAPE, "%s: batch * heads * rows exceeds the grid limit", fn);
     return HDT_OK;
 }
@@ -193,5 +195,5 @@ HDT_EXPORT hdt_status_t hdt_rel_attn_bwd(const hdt_rel_attn_t *d, const void *q,
     a.batch = d->batch, a.heads = d->heads, a.kv_heads = d->kv_heads, a.group = d->heads / d->kv_heads, a.n_q = d->n_q, a.n_kv = d->n_kv;
     a.tiles_q = p.tiles_q, a.tiles_k = p.tiles_k, a.n_pad = p.n_pad;
     a.scale = d->softmax_scale, a.scale_log2 = d->softmax_scale * hdt_rel::LOG2E;
-    return hdt_launch_rel_bwd(*d, a, (hipStream_t)stream);
+    return hdt_launch_rel_bwd(*d, a, p.waves, (hipStream_t)stream);
 }

@@ -30,8 +30,8 @@ struct RelBwdArgs {
     const void *q, *k, *v, *o, *d_o;
     const float *lse;
     void *dq, *dk, *dv, *d_bias;
-    float *row_scalars;               // [batch][heads][n_pad] of -LSE log2(e), then as many of -D
-    float *bins;                      // [heads][batch * tiles_q][table length]: sums of dS by distance
+    float *row_scalars;               // four arrays of [batch][heads][n_pad], see k_rel_rows
+    float *bins;                      // [heads][batch * tiles_q][n_buckets]: sums of dS
     const int32_t *lengths, *starts;
     hdt_strides_t sq, sk, sv, so, sdo, sdq, sdk, sdv;
     hdt_rel::BiasArgs bias;
@@ -41,11 +41,11 @@ struct RelBwdArgs {
 };
 
 struct RelBwdPlan {
-    int32_t tiles_q, tiles_k, n_pad;
+    int32_t tiles_q, tiles_k, n_pad, waves;  // waves of a workgroup, 32 rows each
     size_t bins_at, bytes;
 };
 RelBwdPlan hdt_rel_bwd_plan(const hdt_rel_attn_t &d);
-hdt_status_t hdt_launch_rel_bwd(const hdt_rel_attn_t &d, const RelBwdArgs &a, hipStream_t st);
+hdt_status_t hdt_launch_rel_bwd(const hdt_rel_attn_t &d, const RelBwdArgs &a, int waves, hipStream_t st);
 
 namespace hdt_rel {
 

@@ -4,6 +4,8 @@
 // tile.  Rows are the queries of one head, or, where a head has fewer queries than a tile has rows, the queries of all heads that
 // share a key head, so that the keys are read once for them (PACK: row r is query r / gp of head r % gp).  Key tiles of BN rows
 // go through a ring of two stages in LDS.
+#include <type_traits>
+
 #include "hdt_rel.h"
 #include "hdt_rel_args.h"
 
@@ -14,23 +16,22 @@ using namespace hdt_rel;
 template <typename T, int D>
 struct FwdShape {
     static constexpr int NW = 4, BM = 32 * NW, BN = sizeof(T) == 4 && D == 128 ? 32 : 64;
-    static constexpr int TILE = BN * Rows<T, D>::ROWB, RING = 4 * TILE;
+    static constexpr int RING = 2 * Pair<T, D, BN, NW>::STAGE;
 };
 
 template <typename T, int D, bool CAUSAL>
-__global__ __launch_bounds__(256, 2) void k_rel_fwd(RelFwdArgs a)
+__global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void k_rel_fwd(RelFwdArgs a)
 {
     using S = FwdShape<T, D>;
     using RowsT = Rows<T, D>;
-    constexpr int BM = S::BM, BN = S::BN, NW = S::NW;
+    constexpr int BM = S::BM, BN = S::BN, NW = S::NW, KB = BN / 32;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     float *const tab = reinterpret_cast<float *>(smem + S::RING);
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5;
-    unsigned item = blockIdx.x;
-    const unsigned piece = item % a.pieces;
-    item /= a.pieces;
-    const int I = item % a.tiles, bh = item / a.tiles, b = bh / a.head_blocks, hb = bh - b * a.head_blocks;
+    // the longest tiles first; the head blocks side by side, so that with a multiple of 8 of them each stays on one XCD and in its L2
+    const unsigned heads = (unsigned)(a.batch * a.head_blocks), tp = blockIdx.x / heads, piece = tp % a.pieces;
+    const int bh = blockIdx.x - tp * heads, I = a.tiles - 1 - (int)(tp / a.pieces), b = bh / a.head_blocks, hb = bh - b * a.head_blocks;
     const int gp = a.gp, n_rows = a.n_q * gp, M = a.bias.max_distance;
     const Sample smp = sample_of(a.lengths, a.starts, b, a.n_q, a.n_kv);
 
@@ -46,8 +47,7 @@ __global__ __launch_bounds__(256, 2) void k_rel_fwd(RelFwdArgs a)
     }
     // rows that are not real take part as copies of one that is, and are not stored
     const int rc = min(max(row, first), max(first, last)), qi = rc / gp, g = rc - qi * gp, pos = smp.start + qi;
-    const int p0 = smp.start + min(max(r0 + wave * 32, first), max(first, last)) / gp;
-    const int p1 = smp.start + min(max(r0 + wave * 32 + 31, first), max(first, last)) / gp;
+    const int w0 = max(r0 + wave * 32, first), w1 = min(r0 + wave * 32 + 31, last), p0 = smp.start + w0 / gp, p1 = smp.start + w1 / gp;
 
     f32x16 acc[RowsT::BLOCKS];
 #pragma unroll
@@ -55,25 +55,18 @@ __global__ __launch_bounds__(256, 2) void k_rel_fwd(RelFwdArgs a)
 #pragma unroll
         for (int e = 0; e < 16; e++) acc[j][e] = 0.f;
     float m_ref = -INFINITY, l_part = 0.f;
-    const int xlane = (lane ^ 32) << 2;
 
     if (tile0 < tile1) {
         const size_t kvh = (size_t)(hb * gp / a.group);
-        const char *kb = (const char *)a.k + ((size_t)b * a.sk.batch + kvh * a.sk.head) * sizeof(T);
-        const char *vb = (const char *)a.v + ((size_t)b * a.sv.batch + kvh * a.sv.head) * sizeof(T);
-        const uint32_t krow = (uint32_t)a.sk.row * sizeof(T), vrow = (uint32_t)a.sv.row * sizeof(T);
-        const uint32_t lds = lds_addr(smem);
-        auto request = [&](int t) {
-            const uint32_t at = lds + (uint32_t)(t & 1) * 2 * S::TILE;
-            RowsT::template load<BN, NW>(kb + (size_t)t * BN * krow, krow, 0, seen - 1 - t * BN, at, wave, lane);
-            RowsT::template load<BN, NW>(vb + (size_t)t * BN * vrow, vrow, 0, seen - 1 - t * BN, at + S::TILE, wave, lane);
-        };
+        Pair<T, D, BN, NW> kv;
+        kv.init((const T *)a.k + (size_t)b * a.sk.batch + kvh * a.sk.head, a.sk.row, (const T *)a.v + (size_t)b * a.sv.batch + kvh * a.sv.head,
+                a.sv.row, smem, wave, lane);
         typename RowsT::Frag qf[RowsT::STEPS];
-        const char *qp = (const char *)a.q + ((size_t)b * a.sq.batch + (size_t)(hb * gp + g) * a.sq.head + (size_t)qi * a.sq.row) * sizeof(T);
+        const char *qp = (const char *)((const T *)a.q + (size_t)b * a.sq.batch + (size_t)(hb * gp + g) * a.sq.head + (size_t)qi * a.sq.row);
 #pragma unroll
         for (int st = 0; st < RowsT::STEPS; st++) qf[st] = *reinterpret_cast<const typename RowsT::Frag *>(qp + (2 * st + hf) * 16);
         fill_table<CAUSAL>(tab, a.bias, hb * gp, gp, tid, NW * 64);
-        request(tile0);
+        kv.request(tile0 * BN, 0, seen - 1, 0);
         const int len = table_length(M, CAUSAL);
         const float *const my_tab = tab + g * len + 4 * hf - pos + M + kPad;
         const RowLane rl = row_lane<RowsT::CPR>(lane);
@@ -81,61 +74,83 @@ __global__ __launch_bounds__(256, 2) void k_rel_fwd(RelFwdArgs a)
         __syncthreads();
         const float c_behind = tab[g * len] * a.scale_log2, c_ahead = CAUSAL ? 0.f : tab[g * len + len - 1] * a.scale_log2;
 
-        for (int t = tile0; t < tile1; t++) {
+        // one tile of keys, in stage ST of the ring (a constant: the LDS addresses of both stages are then offsets of the same registers)
+        auto tile = [&](int t, auto stage) {
+            constexpr int ST = decltype(stage)::value;
             wait_vmcnt<0>();
             wg_barrier();
-            if (t + 1 < tile1) request(t + 1);
-            const char *sK = smem + (t & 1) * 2 * S::TILE, *sV = sK + S::TILE;
+            if (t + 1 < tile1) kv.request((t + 1) * BN, 0, seen - 1, 1 - ST);
+            const char *sK = smem + ST * kv.STAGE, *sV = sK + kv.TILE;
+            const int k0 = t * BN;
+            const Kind kind = kind_of<CAUSAL, BN>(k0, p0, p1, M, smp.length);
+            if (kind == Kind::SKIP || w0 > w1) return;  // (nor has a wave without real rows anything to do)
+            f32x16 s[KB];
+            float c = 0.f;
+            if (kind == Kind::NEAR) {
 #pragma unroll
-            for (int kb32 = 0; kb32 < BN / 32; kb32++) {
-                const int k0 = t * BN + kb32 * 32;
-                const Kind kind = kind_of<CAUSAL>(k0, p0, p1, M, smp.length);
-                if (kind == Kind::SKIP) continue;
-                f32x16 s;
-                if (kind == Kind::NEAR) {
+                for (int kb = 0; kb < KB; kb++) {
 #pragma unroll
-                    for (int e = 0; e < 16; e++) s[e] = my_tab[k0 + 8 * (e >> 2) + (e & 3)];
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 16; e++) s[e] = 0.f;
+                    for (int e = 0; e < 16; e++) s[kb][e] = my_tab[k0 + 32 * kb + 8 * (e >> 2) + (e & 3)];
+                    s[kb] = Op<T>::mma(RowsT::read(sK, rl, kb * 32, 0), qf[0], s[kb]);
                 }
-                const float c = kind == Kind::FAR_BEHIND ? c_behind : kind == Kind::FAR_AHEAD ? c_ahead : 0.f;
+            } else {
+                c = kind == Kind::FAR_BEHIND ? c_behind : c_ahead;
 #pragma unroll
-                for (int st = 0; st < RowsT::STEPS; st++) s = Op<T>::mma(RowsT::read(sK, rl, kb32 * 32, st), qf[st], s);
-                if (!CAUSAL && k0 + 32 > smp.length) {
+                for (int kb = 0; kb < KB; kb++) {
 #pragma unroll
-                    for (int e = 0; e < 16; e++) s[e] = k0 + 4 * hf + 8 * (e >> 2) + (e & 3) < smp.length ? s[e] : -INFINITY;
+                    for (int e = 0; e < 16; e++) s[kb][e] = 0.f;
+                    s[kb] = Op<T>::mma(RowsT::read(sK, rl, kb * 32, 0), qf[0], s[kb]);
                 }
-                float mx = -INFINITY;
+            }
 #pragma unroll
-                for (int e = 0; e < 16; e += 2) mx = fmaxf(mx, fmaxf(s[e], s[e + 1]));
-                mx = fmaxf(mx, __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(xlane, __builtin_bit_cast(int, mx))));
-                mx = fmaf(mx, a.scale_log2, c);
-                if (__any(mx > m_ref + 8.f)) {
-                    const float m_new = fmaxf(m_ref, mx), alpha = m_new == -INFINITY ? 1.f : fast_exp2(m_ref - m_new);
-                    m_ref = m_new;
-                    l_part *= alpha;
+            for (int st = 1; st < RowsT::STEPS; st++)
 #pragma unroll
-                    for (int j = 0; j < RowsT::BLOCKS; j++)
+                for (int kb = 0; kb < KB; kb++) s[kb] = Op<T>::mma(RowsT::read(sK, rl, kb * 32, st), qf[st], s[kb]);
+            if (!CAUSAL && k0 + BN > smp.length) {
 #pragma unroll
-                        for (int e = 0; e < 16; e++) acc[j][e] *= alpha;
-                }
-                const float off = c - (m_ref == -INFINITY ? 0.f : m_ref);
+                for (int kb = 0; kb < KB; kb++)
+#pragma unroll
+                    for (int e = 0; e < 16; e++) s[kb][e] = k0 + 32 * kb + 4 * hf + 8 * (e >> 2) + (e & 3) < smp.length ? s[kb][e] : -INFINITY;
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int kb = 0; kb < KB; kb++)
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) mx = fmaxf(mx, fmaxf(s[kb][e], s[kb][e + 1]));
+            mx = fmaf(max_halves(mx), a.scale_log2, c);
+            if (__any(mx > m_ref + 8.f)) {
+                const float m_new = fmaxf(m_ref, mx), alpha = m_new == -INFINITY ? 1.f : fast_exp2(m_ref - m_new);
+                m_ref = m_new;
+                l_part *= alpha;
+#pragma unroll
+                for (int j = 0; j < RowsT::BLOCKS; j++)
+#pragma unroll
+                    for (int e = 0; e < 16; e++) acc[j][e] *= alpha;
+            }
+            const float off = c - (m_ref == -INFINITY ? 0.f : m_ref);
+#pragma unroll
+            for (int kb = 0; kb < KB; kb++) {
                 float sum = 0.f;
 #pragma unroll
                 for (int e = 0; e < 16; e++) {
-                    s[e] = fast_exp2(fmaf(s[e], a.scale_log2, off));
-                    sum += s[e];
+                    s[kb][e] = fast_exp2(fmaf(s[kb][e], a.scale_log2, off));
+                    sum += s[kb][e];
                 }
                 l_part += sum;
-                const Weights<T> w(s);
+                const Weights<T> w(s[kb]);
 #pragma unroll
-                for (int j = 0; j < RowsT::BLOCKS; j++) acc[j] = RowsT::weigh(sV, tl, lane, kb32 * 32, j, w, acc[j]);
+                for (int j = 0; j < RowsT::BLOCKS; j++) acc[j] = RowsT::weigh(sV, tl, lane, kb * 32, j, w, acc[j]);
             }
+        };
+        int t = tile0;
+        for (; t + 1 < tile1; t += 2) {
+            tile(t, std::integral_constant<int, 0>());
+            tile(t + 1, std::integral_constant<int, 1>());
         }
+        if (t < tile1) tile(t, std::integral_constant<int, 0>());
     }
 
-    const float l_tot = l_part + __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(xlane, __builtin_bit_cast(int, l_part)));
+    const float l_tot = sum_halves(l_part);
     const float inv = real && l_tot > 0.f ? 1.f / l_tot : 0.f;
     const float lse = real && l_tot > 0.f ? (m_ref + __builtin_amdgcn_logf(l_tot)) * LN2 : -INFINITY;
     if (!own) return;

@@ -40,7 +40,8 @@ def fwd(lib, c, ptrs=None, lse=4096):
     (UNSUPPORTED, dict(head_dim=0)), (UNSUPPORTED, dict(dtype=2)), (UNSUPPORTED, dict(bias_dtype=7)), (INVALID, dict(softmax_scale=0.0)),
     (INVALID, dict(softmax_scale=-1.0)), (INVALID, dict(softmax_scale=float("nan"))), (INVALID, dict(softmax_scale=float("inf"))),
     (INVALID, dict(softmax_scale=1e-39)), (INVALID, dict(softmax_scale=1e20)), (SHAPE, dict(max_distance=0)), (SHAPE, dict(max_distance=1025)), (SHAPE, dict(n_buckets=0)),
-    (SHAPE, dict(n_buckets=4097)), (SHAPE, dict(n_kv=(1 << 24) + 1)), (SHAPE, dict(batch=1 << 20, heads=1 << 10, kv_heads=1 << 10)),
+    (SHAPE, dict(n_buckets=4097)), (SHAPE, dict(n_kv=(1 << 24) + 1)), (SHAPE, dict(batch=1 << 20, heads=1 << 10, kv_heads=1 << 10)), (SHAPE, dict(n_kv=1 << 24, heads=8, kv_heads=1)),
+    (SHAPE, dict(batch=2 ** 31 - 1, heads=2 ** 30, kv_heads=2 ** 30, n_q=1 << 24)),
     (INVALID, dict(d_bias=None)), (INVALID, dict(d_table=None)),
     (INVALID, dict(q=(4096, 512, 65))), (INVALID, dict(q=(4096, 513, 64))), (INVALID, dict(k=(-4096, 512, 64))), (INVALID, dict(v=(4096, 512, 32))),
     (INVALID, dict(q=(1 << 30, 1 << 28, 1 << 21))), (INVALID, dict(o=(0, 512, 64))), (INVALID, dict(o=(2048, 0, 64))),
