@@ -52,12 +52,13 @@ __device__ __forceinline__ Block philox(uint32_t block, uint32_t site, const Key
     }
     return {{c0, c1, c2, c3}};
 }
-// the 16-bit numbers of elements at .. at + 7
+// the 16-bit numbers of elements at .. at + 7; WHOLE: of one block
+template <bool WHOLE>
 __device__ __forceinline__ Block numbers(unsigned long long at, const Drop &d, const Key &k)
 {
     const uint32_t block = (uint32_t)(at >> 3), off = (uint32_t)at & 7u;
     Block a = philox(block, d.site, k);
-    if (off == 0) return a;
+    if (WHOLE || off == 0) return a;
     const Block b = philox(block + 1, d.site, k);
     uint32_t w[8] = {a.w[0], a.w[1], a.w[2], a.w[3], b.w[0], b.w[1], b.w[2], b.w[3]};
 #pragma unroll
@@ -77,65 +78,52 @@ __device__ __forceinline__ float factor(const Block &b, int e, const Drop &d)
     return u >= d.threshold ? d.keep_scale : 0.f;
 }
 
-// 8 consecutive elements; `left` of them exist.  The address is aligned to an element only.
-typedef bf16x8 __attribute__((aligned(2))) bf16x8_any;
-typedef f32x4 __attribute__((aligned(4))) f32x4_any;
+// 8 consecutive elements as they are in memory; `left` of them exist (WHOLE: all).  The address is aligned to an element only.
+template <typename T>
+struct Vec {
+    typedef T V __attribute__((ext_vector_type(8)));
+    typedef V Any __attribute__((aligned(sizeof(T))));
+};
+template <bool WHOLE, typename T>
+__device__ __forceinline__ typename Vec<T>::V load8(const T *p, int left)
+{
+    if (WHOLE || left >= 8) return *reinterpret_cast<const typename Vec<T>::Any *>(p);
+    typename Vec<T>::V r;
+#pragma unroll
+    for (int e = 0; e < 8; e++) r[e] = e < left ? p[e] : (T)0.f;
+    return r;
+}
 struct Eight {
     float x[8];
 };
-__device__ __forceinline__ Eight load8(const __bf16 *p, int left)
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void store8(T *p, const Eight &r, int left)
+{
+    if (WHOLE || left >= 8) {
+        typename Vec<T>::V v;
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] = (T)r.x[e];
+        *reinterpret_cast<typename Vec<T>::Any *>(p) = v;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+        if (e < left) p[e] = (T)r.x[e];
+}
+template <bool WHOLE>
+__device__ __forceinline__ Eight load_weight(const void *p, int bf16, int at, int left)
 {
     Eight r;
-    if (left >= 8) {
-        const bf16x8 v = *reinterpret_cast<const bf16x8_any *>(p);
+    if (bf16) {
+        const auto v = load8<WHOLE>((const __bf16 *)p + at, left);
 #pragma unroll
         for (int e = 0; e < 8; e++) r.x[e] = (float)v[e];
     } else {
+        const auto v = load8<WHOLE>((const float *)p + at, left);
 #pragma unroll
-        for (int e = 0; e < 8; e++) r.x[e] = e < left ? (float)p[e] : 0.f;
+        for (int e = 0; e < 8; e++) r.x[e] = v[e];
     }
     return r;
-}
-__device__ __forceinline__ Eight load8(const float *p, int left)
-{
-    Eight r;
-    if (left >= 8) {
-        const f32x4 a = *reinterpret_cast<const f32x4_any *>(p), b = *reinterpret_cast<const f32x4_any *>(p + 4);
-#pragma unroll
-        for (int e = 0; e < 4; e++) r.x[e] = a[e], r.x[4 + e] = b[e];
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; e++) r.x[e] = e < left ? p[e] : 0.f;
-    }
-    return r;
-}
-__device__ __forceinline__ void store8(__bf16 *p, const Eight &r, int left)
-{
-    if (left >= 8) {
-        bf16x8 v;
-#pragma unroll
-        for (int e = 0; e < 8; e++) v[e] = (__bf16)r.x[e];
-        *reinterpret_cast<bf16x8_any *>(p) = v;
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; e++)
-            if (e < left) p[e] = (__bf16)r.x[e];
-    }
-}
-__device__ __forceinline__ void store8(float *p, const Eight &r, int left)
-{
-    if (left >= 8) {
-        *reinterpret_cast<f32x4_any *>(p) = f32x4{r.x[0], r.x[1], r.x[2], r.x[3]};
-        *reinterpret_cast<f32x4_any *>(p + 4) = f32x4{r.x[4], r.x[5], r.x[6], r.x[7]};
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; e++)
-            if (e < left) p[e] = r.x[e];
-    }
-}
-__device__ __forceinline__ Eight load_weight(const void *p, int bf16, long long at, int left)
-{
-    return bf16 ? load8((const __bf16 *)p + at, left) : load8((const float *)p + at, left);
 }
 
 // ------------------------------------------------------------------------------------------ dropout + residual
@@ -145,28 +133,53 @@ __global__ __launch_bounds__(256) void k_dropout_add(const T *y, const T *x, T *
     const Key k = key_of(d);
     for (unsigned long long at = ((unsigned long long)blockIdx.x * 256 + threadIdx.x) * 8; at < n; at += (unsigned long long)gridDim.x * 2048) {
         const int left = (int)min(n - at, 8ull);
-        Eight v = load8(y + at, left);
-        if (d.threshold) {
-            const Block b = philox((uint32_t)(at >> 3), d.site, k);
+        const typename Vec<T>::V yv = load8<false>(y + at, left);
+        typename Vec<T>::V xv = {};
+        if (x) xv = load8<false>(x + at, left);
+        Block b = {};
+        if (d.threshold) b = philox((uint32_t)(at >> 3), d.site, k);
+        Eight v;
 #pragma unroll
-            for (int e = 0; e < 8; e++) v.x[e] *= factor(b, e, d);
+        for (int e = 0; e < 8; e++) {
+            v.x[e] = (float)yv[e];
+            if (d.threshold) v.x[e] *= factor(b, e, d);
+            if (x) v.x[e] += (float)xv[e];
         }
-        if (x) {
-            const Eight r = load8(x + at, left);
-#pragma unroll
-            for (int e = 0; e < 8; e++) v.x[e] += r.x[e];
-        }
-        store8(out + at, v, left);
+        store8<false>(out + at, v, left);
     }
 }
 
 // ------------------------------------------------------------------------------------------ sums over a row
+// The sum over a wave, in every lane: pairs, quads, eights and rows of 16 by shifted operands, rows and halves by exchanges (the
+// second operand of an exchange is made opaque: of two results of one value the compiler takes one).
+template <int CTRL>
+__device__ __forceinline__ float plus_dpp(float x)
+{
+    return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ unsigned hidden(unsigned x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+__device__ __forceinline__ float wave_sum(float x)
+{
+    x = plus_dpp<0xb1>(x);   // lane ^ 1
+    x = plus_dpp<0x4e>(x);   // lane ^ 2
+    x = plus_dpp<0x141>(x);  // the other quad of eight
+    x = plus_dpp<0x140>(x);  // the other eight of a row of 16
+    unsigned v = __builtin_bit_cast(unsigned, x);
+    const auto rows = __builtin_amdgcn_permlane16_swap(v, hidden(v), false, false);
+    x = __builtin_bit_cast(float, (unsigned)rows[0]) + __builtin_bit_cast(float, (unsigned)rows[1]);
+    v = __builtin_bit_cast(unsigned, x);
+    const auto half = __builtin_amdgcn_permlane32_swap(v, hidden(v), false, false);
+    return __builtin_bit_cast(float, (unsigned)half[0]) + __builtin_bit_cast(float, (unsigned)half[1]);
+}
 // the sum over the threads of a row: a wave, or (TPR > 64) the whole workgroup
 template <int TPR>
 __device__ __forceinline__ float row_sum(float x, float *lds)
 {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
+    x = wave_sum(x);
     if (TPR > 64) {
         __syncthreads();
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
@@ -187,40 +200,46 @@ struct NormArgs {
     Drop drop;
 };
 
-// a row's threads hold its 16-byte chunks c = thread + TPR u, u < NCH
-template <typename T, int TPR, int NCH>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_add_norm_fwd(NormArgs a)
+// A row's TPR threads hold its chunks of eight columns c = thread + TPR u, u < NCH.  WHOLE: the width is a multiple of eight, so that
+// chunks are whole, and a chunk's random numbers those of one block.
+template <int TPR, int NCH>
+struct Shape {
+    static constexpr int FWD = TPR < 256 ? 256 : TPR, BWD = TPR > 64 ? TPR : NCH < 4 ? 512 : 256;  // threads of a workgroup
+};
+
+template <typename T, int TPR, int NCH, bool WHOLE, bool DROP>
+__global__ __launch_bounds__((Shape<TPR, NCH>::FWD)) void k_add_norm_fwd(NormArgs a)
 {
-    constexpr int PER = (TPR < 256 ? 256 : TPR) / TPR;
+    constexpr int PER = Shape<TPR, NCH>::FWD / TPR;
+    typedef typename Vec<T>::V V;
     __shared__ float lds[16];
     const int sub = threadIdx.x / TPR, t = threadIdx.x % TPR;
-    const Key k = key_of(a.drop);
+    const Key k = DROP ? key_of(a.drop) : Key{};
     for (int64_t row = (int64_t)blockIdx.x * PER + sub; row < a.rows; row += (int64_t)gridDim.x * PER) {  // (the same for whole waves, and for a workgroup that has one row)
         const size_t at = (size_t)row * a.width;
+        V x[NCH], y[NCH];
+#pragma unroll
+        for (int u = 0; u < NCH; u++) {
+            const int c = (t + TPR * u) * 8, left = a.width - c;
+            x[u] = V{}, y[u] = V{};
+            if (left > 0) {
+                x[u] = load8<WHOLE>((const T *)a.x + at + c, left);
+                if (a.y) y[u] = load8<WHOLE>((const T *)a.y + at + c, left);
+            }
+        }
         Eight h[NCH];
         float sum = 0.f;
 #pragma unroll
         for (int u = 0; u < NCH; u++) {
             const int c = (t + TPR * u) * 8, left = a.width - c;
-            if (left <= 0) {
+            Block b = {};
+            if (DROP && left > 0) b = numbers<WHOLE>(at + c, a.drop, k);
 #pragma unroll
-                for (int e = 0; e < 8; e++) h[u].x[e] = 0.f;
-                continue;
+            for (int e = 0; e < 8; e++) {
+                h[u].x[e] = (float)x[u][e] + (DROP ? (float)y[u][e] * factor(b, e, a.drop) : (float)y[u][e]);
+                sum += h[u].x[e];
             }
-            h[u] = load8((const T *)a.x + at + c, left);
-            if (a.y) {
-                Eight y = load8((const T *)a.y + at + c, left);
-                if (a.drop.threshold) {
-                    const Block b = numbers(at + c, a.drop, k);
-#pragma unroll
-                    for (int e = 0; e < 8; e++) y.x[e] *= factor(b, e, a.drop);
-                }
-#pragma unroll
-                for (int e = 0; e < 8; e++) h[u].x[e] += y.x[e];
-                store8((T *)a.h_out + at + c, h[u], left);
-            }
-#pragma unroll
-            for (int e = 0; e < 8; e++) sum += h[u].x[e];
+            if (a.y && left > 0) store8<WHOLE>((T *)a.h_out + at + c, h[u], left);
         }
         const float mean = row_sum<TPR>(sum, lds) * a.inv_width;
         float sq = 0.f;
@@ -229,7 +248,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_add_norm_fwd(NormArgs
             const int left = a.width - (t + TPR * u) * 8;
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                h[u].x[e] = e < left ? h[u].x[e] - mean : 0.f;
+                h[u].x[e] = (WHOLE ? 0 : e) < left ? h[u].x[e] - mean : 0.f;
                 sq = fmaf(h[u].x[e], h[u].x[e], sq);
             }
         }
@@ -238,12 +257,12 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_add_norm_fwd(NormArgs
         for (int u = 0; u < NCH; u++) {
             const int c = (t + TPR * u) * 8, left = a.width - c;
             if (left <= 0) continue;
-            const Eight w = load_weight(a.weight, a.weight_bf16, c, left);
+            const Eight w = load_weight<WHOLE>(a.weight, a.weight_bf16, c, left);
             Eight b = {};
-            if (a.bias) b = load_weight(a.bias, a.weight_bf16, c, left);
+            if (a.bias) b = load_weight<WHOLE>(a.bias, a.weight_bf16, c, left);
 #pragma unroll
             for (int e = 0; e < 8; e++) h[u].x[e] = fmaf(h[u].x[e] * rstd, w.x[e], b.x[e]);
-            store8((T *)a.n + at + c, h[u], left);
+            store8<WHOLE>((T *)a.n + at + c, h[u], left);
         }
         if (t == 0) {
             a.mean[row] = mean;
@@ -254,36 +273,47 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_add_norm_fwd(NormArgs
 
 // Rows blockIdx, blockIdx + gridDim, ... of a workgroup's wave (or of the workgroup), the columns' sums of dn xhat and dn in
 // registers throughout; at the end a row of the workgroup's sums: parts[workgroup][2][width]
-template <typename T, int TPR, int NCH>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_add_norm_bwd(NormArgs a)
+template <typename T, int TPR, int NCH, bool WHOLE, bool DROP>
+__global__ __launch_bounds__((Shape<TPR, NCH>::BWD)) void k_add_norm_bwd(NormArgs a)
 {
-    constexpr int PER = (TPR < 256 ? 256 : TPR) / TPR;
+    constexpr int PER = Shape<TPR, NCH>::BWD / TPR;
+    typedef typename Vec<T>::V V;
     extern __shared__ __attribute__((aligned(16))) float lds[];  // 32, then (PER > 1) PER rows of `width` up to whole chunks
     const int sub = threadIdx.x / TPR, t = threadIdx.x % TPR;
-    const Key k = key_of(a.drop);
+    const Key k = DROP ? key_of(a.drop) : Key{};
     Eight w[NCH], sw[NCH] = {}, sb[NCH] = {};
 #pragma unroll
     for (int u = 0; u < NCH; u++) {
         const int c = (t + TPR * u) * 8;
-        if (c < a.width) w[u] = load_weight(a.weight, a.weight_bf16, c, a.width - c);
+        if (c < a.width) w[u] = load_weight<WHOLE>(a.weight, a.weight_bf16, c, a.width - c);
     }
     for (int64_t row = (int64_t)blockIdx.x * PER + sub; row < a.rows; row += (int64_t)gridDim.x * PER) {
         const size_t at = (size_t)row * a.width;
         const float mean = a.mean[row], rstd = a.rstd[row];
+        V hv[NCH], gv[NCH], dv[NCH];
+#pragma unroll
+        for (int u = 0; u < NCH; u++) {
+            const int c = (t + TPR * u) * 8, left = a.width - c;
+            hv[u] = V{}, gv[u] = V{}, dv[u] = V{};
+            if (left > 0) {
+                hv[u] = load8<WHOLE>((const T *)a.h + at + c, left);
+                gv[u] = load8<WHOLE>((const T *)a.dn + at + c, left);
+                if (a.dh) dv[u] = load8<WHOLE>((const T *)a.dh + at + c, left);
+            }
+        }
         Eight hat[NCH], g[NCH];
         float s0 = 0.f, s1 = 0.f;
 #pragma unroll
         for (int u = 0; u < NCH; u++) {
-            const int c = (t + TPR * u) * 8, left = a.width - c;
+            const int left = a.width - (t + TPR * u) * 8;
             if (left <= 0) continue;
-            hat[u] = load8((const T *)a.h + at + c, left);
-            g[u] = load8((const T *)a.dn + at + c, left);
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                hat[u].x[e] = e < left ? (hat[u].x[e] - mean) * rstd : 0.f;
-                sw[u].x[e] = fmaf(g[u].x[e], hat[u].x[e], sw[u].x[e]);
-                sb[u].x[e] += g[u].x[e];
-                g[u].x[e] *= w[u].x[e];
+                const float dn = (float)gv[u][e];
+                hat[u].x[e] = WHOLE || e < left ? ((float)hv[u][e] - mean) * rstd : 0.f;
+                sw[u].x[e] = fmaf(dn, hat[u].x[e], sw[u].x[e]);
+                sb[u].x[e] += dn;
+                g[u].x[e] = dn * w[u].x[e];
                 s0 += g[u].x[e];
                 s1 = fmaf(g[u].x[e], hat[u].x[e], s1);
             }
@@ -294,16 +324,15 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_add_norm_bwd(NormArgs
         for (int u = 0; u < NCH; u++) {
             const int c = (t + TPR * u) * 8, left = a.width - c;
             if (left <= 0) continue;
-            Eight d = {};
-            if (a.dh) d = load8((const T *)a.dh + at + c, left);
+            Eight d;
 #pragma unroll
-            for (int e = 0; e < 8; e++) d.x[e] = fmaf(rstd, g[u].x[e] - s0 - hat[u].x[e] * s1, d.x[e]);
-            store8((T *)a.dx + at + c, d, left);
-            if (a.drop.threshold) {
-                const Block b = numbers(at + c, a.drop, k);
+            for (int e = 0; e < 8; e++) d.x[e] = fmaf(rstd, g[u].x[e] - s0 - hat[u].x[e] * s1, (float)dv[u][e]);
+            store8<WHOLE>((T *)a.dx + at + c, d, left);
+            if (DROP) {
+                const Block b = numbers<WHOLE>(at + c, a.drop, k);
 #pragma unroll
                 for (int e = 0; e < 8; e++) d.x[e] *= factor(b, e, a.drop);
-                store8((T *)a.dy + at + c, d, left);
+                store8<WHOLE>((T *)a.dy + at + c, d, left);
             }
         }
     }
@@ -313,8 +342,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_add_norm_bwd(NormArgs
         for (int u = 0; u < NCH; u++) {
             const int c = (t + TPR * u) * 8;
             if (c >= a.width) continue;
-            store8(out + c, sw[u], a.width - c);
-            store8(out + a.width + c, sb[u], a.width - c);
+            store8<WHOLE>(out + c, sw[u], a.width - c);
+            store8<WHOLE>(out + a.width + c, sb[u], a.width - c);
         }
         return;
     }
@@ -325,7 +354,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_add_norm_bwd(NormArgs
 #pragma unroll
         for (int u = 0; u < NCH; u++) {
             const int c = (t + TPR * u) * 8;
-            if (c < a.width) store8(lds + 32 + (size_t)sub * whole + c, which ? sb[u] : sw[u], 8);
+            if (c < a.width) store8<true>(lds + 32 + (size_t)sub * whole + c, which ? sb[u] : sw[u], 8);
         }
         __syncthreads();
         for (int c = threadIdx.x; c < a.width; c += TPR * PER) {
@@ -337,20 +366,24 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_add_norm_bwd(NormArgs
     }
 }
 
-// the workgroups' sums added up in a fixed order: 64 columns a workgroup, 16 runs of parts
-__global__ __launch_bounds__(1024) void k_norm_parts(NormArgs a, int parts)
+// The workgroups' sums added up in a fixed order: 16 columns a workgroup, 64 runs of parts.  (64 columns and 16 runs left most of the
+// chip idle: 1536 sums of 1024 parts 20.4 us.)
+constexpr int kPartColumns = 16, kPartRuns = 64;
+__global__ __launch_bounds__(kPartColumns * kPartRuns) void k_norm_parts(NormArgs a, int parts)
 {
-    __shared__ float lds[16][64];
-    const int lane = threadIdx.x & 63, run = threadIdx.x >> 6, x = blockIdx.x * 64 + lane;
+    __shared__ float lds[kPartRuns][kPartColumns];
+    const int lane = threadIdx.x % kPartColumns, run = threadIdx.x / kPartColumns, x = blockIdx.x * kPartColumns + lane;
     float sum = 0.f;
-    if (x < 2 * a.width)
-        for (int p = run; p < parts; p += 16) sum += a.parts[(size_t)p * 2 * a.width + x];
+    if (x < 2 * a.width) {
+#pragma unroll 8
+        for (int p = run; p < parts; p += kPartRuns) sum += a.parts[(size_t)p * 2 * a.width + x];
+    }
     lds[run][lane] = sum;
     __syncthreads();
     if (run != 0 || x >= 2 * a.width) return;
     sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; i++) sum += lds[i][lane];
+    for (int i = 0; i < kPartRuns; i++) sum += lds[i][lane];
     void *out = x < a.width ? a.d_weight : a.d_bias;
     const int c = x < a.width ? x : x - a.width;
     if (!out) return;
@@ -360,7 +393,7 @@ __global__ __launch_bounds__(1024) void k_norm_parts(NormArgs a, int parts)
         ((float *)out)[c] = sum;
 }
 
-constexpr int kMostWidth = 32768, kMostParts = 1024;
+constexpr int kMostWidth = 32768, kMostParts = 512;
 constexpr long long kMostElements = 1ll << 35;  // 2^32 blocks of eight
 
 // threads a row and chunks a thread: a wave up to 2048 columns, then a workgroup of 256 or 1024
@@ -375,40 +408,45 @@ RowShape row_shape(int width)
     if (chunks <= 256) return {64, 4};
     return chunks <= 1024 ? RowShape{256, 4} : RowShape{1024, 4};
 }
+// workgroups of the backward: two or more per compute unit, and no more sums to add up behind it than that takes
 int norm_parts(int rows, int width)
 {
-    const int per = row_shape(width).tpr == 64 ? 4 : 1, groups = (int)(((int64_t)rows + per - 1) / per);
-    return groups < kMostParts ? groups : kMostParts;
+    const RowShape s = row_shape(width);
+    const int per = s.tpr == 64 ? (s.nch < 4 ? Shape<64, 1>::BWD : Shape<64, 4>::BWD) / 64 : 1;
+    return (int)std::min<int64_t>(((int64_t)rows + per - 1) / per, kMostParts);
 }
 
-template <typename T, int TPR, int NCH>
-void launch_fwd(const NormArgs &a, hipStream_t st)
+template <typename T, int TPR, int NCH, bool WHOLE, bool DROP>
+void launch_one(const NormArgs &a, bool bwd, hipStream_t st)
 {
-    constexpr int THREADS = TPR < 256 ? 256 : TPR, PER = THREADS / TPR;
-    hipLaunchKernelGGL((k_add_norm_fwd<T, TPR, NCH>), dim3((unsigned)std::min<int64_t>(((int64_t)a.rows + PER - 1) / PER, 1 << 20)), dim3(THREADS), 0, st, a);
+    using S = Shape<TPR, NCH>;
+    if (!bwd) {
+        const int64_t grid = std::min<int64_t>(((int64_t)a.rows + S::FWD / TPR - 1) / (S::FWD / TPR), 1 << 20);
+        hipLaunchKernelGGL((k_add_norm_fwd<T, TPR, NCH, WHOLE, DROP>), dim3((unsigned)grid), dim3(S::FWD), 0, st, a);
+    } else {
+        constexpr int PER = S::BWD / TPR;
+        const size_t lds = (32 + (PER > 1 ? (size_t)PER * ((a.width + 7) & ~7) : 0)) * sizeof(float);
+        hipLaunchKernelGGL((k_add_norm_bwd<T, TPR, NCH, WHOLE, DROP>), dim3((unsigned)norm_parts(a.rows, a.width)), dim3(S::BWD), lds, st, a);
+    }
 }
 template <typename T, int TPR, int NCH>
-void launch_bwd(const NormArgs &a, hipStream_t st)
+void launch_shape(const NormArgs &a, bool bwd, hipStream_t st)
 {
-    constexpr int THREADS = TPR < 256 ? 256 : TPR, PER = THREADS / TPR;
-    const size_t lds = (32 + (PER > 1 ? (size_t)PER * ((a.width + 7) & ~7) : 0)) * sizeof(float);
-    hipLaunchKernelGGL((k_add_norm_bwd<T, TPR, NCH>), dim3((unsigned)norm_parts(a.rows, a.width)), dim3(THREADS), lds, st, a);
+    const bool whole = a.width % 8 == 0, drop = a.drop.threshold != 0;
+    if (whole)
+        drop ? launch_one<T, TPR, NCH, true, true>(a, bwd, st) : launch_one<T, TPR, NCH, true, false>(a, bwd, st);
+    else
+        drop ? launch_one<T, TPR, NCH, false, true>(a, bwd, st) : launch_one<T, TPR, NCH, false, false>(a, bwd, st);
 }
 template <typename T>
 void launch(const NormArgs &a, bool bwd, hipStream_t st)
 {
     const RowShape s = row_shape(a.width);
-#define HDT_ROWS(TPR, NCH)                                                                     \
-    if (s.tpr == TPR && s.nch == NCH) {                                                        \
-        bwd ? launch_bwd<T, TPR, NCH>(a, st) : launch_fwd<T, TPR, NCH>(a, st);                 \
-        return;                                                                                \
-    }
-    HDT_ROWS(64, 1)
-    HDT_ROWS(64, 2)
-    HDT_ROWS(64, 4)
-    HDT_ROWS(256, 4)
-    HDT_ROWS(1024, 4)
-#undef HDT_ROWS
+    if (s.tpr == 64 && s.nch == 1) return launch_shape<T, 64, 1>(a, bwd, st);
+    if (s.tpr == 64 && s.nch == 2) return launch_shape<T, 64, 2>(a, bwd, st);
+    if (s.tpr == 64) return launch_shape<T, 64, 4>(a, bwd, st);
+    if (s.tpr == 256) return launch_shape<T, 256, 4>(a, bwd, st);
+    launch_shape<T, 1024, 4>(a, bwd, st);
 }
 
 bool misaligned(const void *p) { return ((uintptr_t)p & 15u) != 0; }
@@ -527,7 +565,7 @@ HDT_EXPORT hdt_status_t hdt_add_norm_bwd(const void *dn, const void *dh, const v
         HDT_HIP_TRY(hipGetLastError());
     }
     HdtTimer t("hdt_norm_parts", st);
-    hipLaunchKernelGGL(k_norm_parts, dim3((unsigned)((2 * width + 63) / 64)), dim3(1024), 0, st, a, rows > 0 ? norm_parts((int)rows, width) : 0);
+    hipLaunchKernelGGL(k_norm_parts, dim3((unsigned)((2 * width + kPartColumns - 1) / kPartColumns)), dim3(kPartColumns * kPartRuns), 0, st, a, rows > 0 ? norm_parts((int)rows, width) : 0);
     HDT_HIP_TRY(hipGetLastError());
     return HDT_OK;
 }
