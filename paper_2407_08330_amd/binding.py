@@ -1,6 +1,6 @@
 """Binding of libhdt.so: argument marshalling only.  Every step of the method runs in the
 HIP kernels behind the C ABI declared in ``include/hdt.h``; there is no fallback path, and a
-missing library is an error.  The calls every layer makes (build, forward, backward) go through native code
+missing library is an error.  The calls every layer makes (build, forward, backward; relative-bias attention, dropout, norm) go through native code
 (``csrc/hdt_pycall.cpp``) where their arguments are plain tensors and numbers, and through ctypes otherwise; that module is
 compiled for one Python and one torch, and under others, or without it, ctypes takes all calls."""
 from __future__ import annotations
@@ -70,7 +70,7 @@ def library_path() -> str:
 
 class _NoCalls:
     """In the place of csrc/hdt_pycall.cpp: takes no call."""
-    build_layout = attn_fwd = attn_bwd = staticmethod(lambda *a: None)
+    build_layout = attn_fwd = attn_bwd = rel_attn_fwd = rel_attn_bwd = dropout_add = add_norm_fwd = add_norm_bwd = staticmethod(lambda *a: None)
 
 
 def _native_calls(lib, torch_version: str):
@@ -86,6 +86,9 @@ def _native_calls(lib, torch_version: str):
         return _NoCalls
     calls.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.hdt_build_layout, lib.hdt_attn_fwd, lib.hdt_attn_fwd_ws,
                                                                  lib.hdt_attn_bwd, lib.hdt_attn_bwd_workspace_bytes)))
+    calls.bind_operators(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        lib.hdt_rel_attn_fwd_workspace_bytes, lib.hdt_rel_attn_fwd, lib.hdt_rel_attn_bwd_workspace_bytes, lib.hdt_rel_attn_bwd, lib.hdt_dropout_add,
+        lib.hdt_add_norm_fwd, lib.hdt_add_norm_bwd_workspace_bytes, lib.hdt_add_norm_bwd)))
     return calls
 
 
@@ -576,8 +579,15 @@ def hdt_rel_attn_fwd(q, k, v, bias, table, softmax_scale: float, causal: bool = 
     """Self-attention with a relative position bias (hdt_rel_attn_fwd in include/hdt.h).  q [batch][heads][n_q][head_dim], k, v
     [batch][kv_heads][n_kv][head_dim], of any strides with consecutive row values; bias [n_buckets][heads]; table: of
     hdt_rel_table; lengths, q_start: int32 device tensors [batch] or None.  Returns (o, lse)."""
+    if _lib is None:
+        load_library()
+    r = _calls.rel_attn_fwd(q, k, v, bias, table, softmax_scale, causal, lengths, q_start, o, lse, workspace, None if stream is None else stream.cuda_stream)
+    if r.__class__ is tuple:
+        return r
+    if r is not None:
+        _check(r)
     import torch
-    lib = load_library()
+    lib = _lib
     if o is None:
         o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     if lse is None:
@@ -597,8 +607,15 @@ def hdt_rel_attn_fwd(q, k, v, bias, table, softmax_scale: float, causal: bool = 
 def hdt_rel_attn_bwd(q, k, v, bias, table, o, lse, d_o, softmax_scale: float, causal: bool = True, lengths=None, q_start=None, dq=None,
                      dk=None, dv=None, dbias=None, workspace=None, stream=None):
     """The gradients of hdt_rel_attn_fwd: (dq, dk, dv, dbias), dbias like bias."""
+    if _lib is None:
+        load_library()
+    r = _calls.rel_attn_bwd(q, k, v, bias, table, softmax_scale, causal, lengths, q_start, o, lse, d_o, dq, dk, dv, dbias, workspace, None if stream is None else stream.cuda_stream)
+    if r.__class__ is tuple:
+        return r
+    if r is not None:
+        _check(r)
     import torch
-    lib = load_library()
+    lib = _lib
     dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
     dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dk is None else dk
     dv = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dv is None else dv
@@ -634,6 +651,13 @@ def _check_like(t, ts):
 def hdt_dropout_add(y, p: float, rng=None, site: int = 0, x=None, out=None, stream=None):
     """x + dropout(y) (x = None: dropout alone; on a gradient: its backward).  ``rng``: int64 device tensor (seed, step); ``site``: which
     of the calls with that seed and step.  ``out`` may be x or y.  Returns out."""
+    if _lib is None:
+        load_library()
+    r = _calls.dropout_add(y, p, rng, site, x, out, None if stream is None else stream.cuda_stream)
+    if r is not None:
+        if r.__class__ is not int:
+            return r
+        _check(r)
     import torch
     out = torch.empty_like(y) if out is None else out
     _check_like(y, (y, x, out))
@@ -658,6 +682,13 @@ def _check_norm(x, weight, vectors, statistics):
 def hdt_add_norm_fwd(x, weight, bias=None, eps: float = 1e-5, y=None, p: float = 0.0, rng=None, site: int = 0, h=None, n=None, mean=None,
                      rstd=None, stream=None):
     """h = x + dropout(y), n = layer norm of h over the last dimension.  Returns (n, h, mean, rstd); h is x where y is None."""
+    if _lib is None:
+        load_library()
+    r = _calls.add_norm_fwd(x, weight, bias, eps, y, p, rng, site, h, n, mean, rstd, None if stream is None else stream.cuda_stream)
+    if r.__class__ is tuple:
+        return r
+    if r is not None:
+        _check(r)
     import torch
     if x.dim() < 1:
         raise ValueError("x must have a last dimension")
@@ -684,8 +715,15 @@ def hdt_add_norm_bwd(dn, h, weight, mean, rstd, dh=None, p: float = 0.0, rng=Non
                      dweight=None, dbias=None, workspace=None, stream=None):
     """Gradients of hdt_add_norm_fwd from dn (that of n) and dh (that of h from elsewhere, or None).  Returns (dx, dy, dweight, dbias):
     dy is dx itself where nothing is dropped, dbias None with ``bias=False``."""
+    if _lib is None:
+        load_library()
+    r = _calls.add_norm_bwd(dn, h, weight, mean, rstd, dh, p, rng, site, bias, dx, dy, dweight, dbias, workspace, None if stream is None else stream.cuda_stream)
+    if r.__class__ is tuple:
+        return r
+    if r is not None:
+        _check(r)
     import torch
-    lib = load_library()
+    lib = _lib
     dx = torch.empty_like(h) if dx is None else dx
     dropped = int(float(p) * 65536 + 0.5) > 0
     if not dropped:

@@ -147,7 +147,7 @@ HDT_EXPORT hdt_status_t hdt_rel_attn_fwd(const hdt_rel_attn_t *d, const void *q,
     a.batch = d->batch, a.heads = d->heads, a.group = d->heads / d->kv_heads, a.n_q = d->n_q, a.n_kv = d->n_kv;
     a.gp = p.gp, a.head_blocks = p.head_blocks, a.tiles = p.tiles, a.pieces = p.pieces;
     a.scale_log2 = d->softmax_scale * hdt_rel::LOG2E;
-    return hdt_launch_rel_fwd(*d, a, (hipStream_t)stream);
+    return hdt_launch_rel_fwd(*d, a, p.waves, (hipStream_t)stream);
 }
 
 HDT_EXPORT size_t hdt_rel_attn_bwd_workspace_bytes(const hdt_rel_attn_t *d)

@@ -20,11 +20,12 @@ struct RelFwdArgs {
 
 struct RelFwdPlan {
     int32_t gp, head_blocks, tiles;
+    int32_t waves;         // of a workgroup, 32 rows each; 0: few rows, the waves divide the keys
     uint32_t pieces;
     size_t lse_at, bytes;  // of the workspace
 };
 RelFwdPlan hdt_rel_fwd_plan(const hdt_rel_attn_t &d);
-hdt_status_t hdt_launch_rel_fwd(const hdt_rel_attn_t &d, const RelFwdArgs &a, hipStream_t st);
+hdt_status_t hdt_launch_rel_fwd(const hdt_rel_attn_t &d, const RelFwdArgs &a, int waves, hipStream_t st);
 
 struct RelBwdArgs {
     const void *q, *k, *v, *o, *d_o;

@@ -4,6 +4,7 @@
 // tile.  Rows are the queries of one head, or, where a head has fewer queries than a tile has rows, the queries of all heads that
 // share a key head, so that the keys are read once for them (PACK: row r is query r / gp of head r % gp).  Key tiles of BN rows
 // go through a ring of two stages in LDS.
+#include <algorithm>
 #include <type_traits>
 
 #include "hdt_rel.h"
@@ -13,16 +14,16 @@ namespace {
 
 using namespace hdt_rel;
 
-template <typename T, int D>
+template <typename T, int D, int NW_>
 struct FwdShape {
-    static constexpr int NW = 4, BM = 32 * NW, BN = sizeof(T) == 4 && D == 128 ? 32 : 64;
+    static constexpr int NW = NW_, BM = 32 * NW, BN = sizeof(T) == 4 && D == 128 ? 32 : 64;
     static constexpr int RING = 2 * Pair<T, D, BN, NW>::STAGE;
 };
 
-template <typename T, int D, bool CAUSAL>
-__global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void k_rel_fwd(RelFwdArgs a)
+template <typename T, int D, int NW_, bool CAUSAL>
+__global__ __launch_bounds__(NW_ * 64, sizeof(T) == 4 && D == 128 ? 1 : 2) void k_rel_fwd(RelFwdArgs a)
 {
-    using S = FwdShape<T, D>;
+    using S = FwdShape<T, D, NW_>;
     using RowsT = Rows<T, D>;
     constexpr int BM = S::BM, BN = S::BN, NW = S::NW, KB = BN / 32;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -179,27 +180,220 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void k_rel
     if (hf == 0) a.lse[((size_t)b * a.heads + head) * a.n_q + oi] = lse;
 }
 
-// O = sum_p exp(LSE_p - LSE) O_p, LSE = log sum_p exp(LSE_p) over the pieces of a row's keys, in their order
+// Few rows (at most 32 in a head block: new tokens): the waves of a workgroup divide the keys instead of the rows.  Each walks blocks of
+// 32 keys through a ring of its own (no barriers; two blocks in flight a wave, 64 KB a workgroup, which the stream from memory
+// wants) and they join what they have in LDS, so that up to a few thousand keys need no second kernel.
+template <typename T, int D>
+struct FewShape {
+    static constexpr int ROWB = Rows<T, D>::ROWB, NW = 1024 / ROWB, NI = 32 * ROWB / 1024;
+    static constexpr int TILE = 32 * ROWB, STAGE = 2 * TILE, RING = NW * 2 * STAGE;  // 128 KB
+    static constexpr int OROW = D + 4;                                               // floats of a row of partial O in LDS
+    static_assert(NW * 32 * (OROW + 2) * 4 <= RING, "the partial results fit the rings");
+};
+
+template <typename T, int D, bool CAUSAL>
+__global__ __launch_bounds__((FewShape<T, D>::NW * 64)) void k_rel_few(RelFwdArgs a)
+{
+    using S = FewShape<T, D>;
+    using RowsT = Rows<T, D>;
+    constexpr int NW = S::NW, NI = S::NI;
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    float *const tab = reinterpret_cast<float *>(smem + S::RING);
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5;
+    const unsigned heads = (unsigned)(a.batch * a.head_blocks), piece = blockIdx.x / heads;
+    const int bh = blockIdx.x - piece * heads, b = bh / a.head_blocks, hb = bh - b * a.head_blocks;
+    const int gp = a.gp, n_rows = a.n_q * gp, M = a.bias.max_distance;
+    const Sample smp = sample_of(a.lengths, a.starts, b, a.n_q, a.n_kv);
+    const int first = smp.lo * gp, last = smp.hi * gp - 1;
+    int block0 = 0, block1 = 0, seen = 0;  // this piece's blocks of 32 keys
+    if (first <= last) {
+        seen = CAUSAL ? smp.start + last / gp + 1 : smp.length;
+        const int all = (seen + 31) / 32, per = (all + (int)a.pieces - 1) / (int)a.pieces;
+        block0 = min((int)piece * per, all);
+        block1 = min(block0 + per, all);
+    }
+    const int row = lane & 31, rc = min(max(row, first), max(first, last)), qi = rc / gp, g = rc - qi * gp, pos = smp.start + qi;
+    const int p0 = smp.start + smp.lo, p1 = smp.start + smp.hi - 1;
+
+    f32x16 acc[RowsT::BLOCKS];
+#pragma unroll
+    for (int j = 0; j < RowsT::BLOCKS; j++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) acc[j][e] = 0.f;
+    float m_ref = -INFINITY, l_part = 0.f;
+
+    if (block0 < block1) {
+        const size_t kvh = (size_t)(hb * gp / a.group);
+        const char *kb = (const char *)((const T *)a.k + (size_t)b * a.sk.batch + kvh * a.sk.head);
+        const char *vb = (const char *)((const T *)a.v + (size_t)b * a.sv.batch + kvh * a.sv.head);
+        const uint32_t krow = (uint32_t)a.sk.row * sizeof(T), vrow = (uint32_t)a.sv.row * sizeof(T);
+        const char *const mine = smem + wave * 2 * S::STAGE;
+        const uint32_t lds = lds_addr(mine);
+        auto request = [&](int blk, int stage) {
+            const char *pk = kb + (size_t)blk * 32 * krow, *pv = vb + (size_t)blk * 32 * vrow;
+            const int left = seen - 1 - blk * 32, c = lane % RowsT::CPR;
+            const uint32_t at = lds + (uint32_t)(stage * S::STAGE);
+#pragma unroll
+            for (int i = 0; i < NI; i++) {
+                const int r = i * RowsT::RPI + lane / RowsT::CPR;
+                const uint32_t from = (uint32_t)min(r, left), chunk = (uint32_t)((c ^ swz<RowsT::CPR>(r)) << 4);
+                dma16(pk, from * krow + chunk, at + i * 1024);
+                dma16(pv, from * vrow + chunk, at + S::TILE + i * 1024);
+            }
+        };
+        if (block0 + wave < block1) request(block0 + wave, 0);
+        typename RowsT::Frag qf[RowsT::STEPS];
+        const char *qp = (const char *)((const T *)a.q + (size_t)b * a.sq.batch + (size_t)(hb * gp + g) * a.sq.head + (size_t)qi * a.sq.row);
+#pragma unroll
+        for (int st = 0; st < RowsT::STEPS; st++) qf[st] = *reinterpret_cast<const typename RowsT::Frag *>(qp + (2 * st + hf) * 16);
+        fill_table<CAUSAL>(tab, a.bias, hb * gp, gp, tid, NW * 64);
+        const int len = table_length(M, CAUSAL);
+        const float *const my_tab = tab + g * len + 4 * hf - pos + M + kPad;
+        const RowLane rl = row_lane<RowsT::CPR>(lane);
+        const TrLane tl = tr_lane<RowsT::CPR>(lane);
+        __syncthreads();
+        const float c_behind = tab[g * len] * a.scale_log2, c_ahead = CAUSAL ? 0.f : tab[g * len + len - 1] * a.scale_log2;
+
+        int stage = 0;
+        for (int blk = block0 + wave; blk < block1; blk += NW, stage ^= 1) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the block before last has been read)
+            if (blk + NW < block1) {
+                request(blk + NW, stage ^ 1);
+                wait_vmcnt<2 * NI>();
+            } else {
+                wait_vmcnt<0>();
+            }
+            const char *sK = mine + stage * S::STAGE, *sV = sK + S::TILE;
+            const int k0 = blk * 32;
+            const Kind kind = kind_of<CAUSAL, 32>(k0, p0, p1, M, smp.length);
+            if (kind == Kind::SKIP) continue;
+            f32x16 s;
+            float c = 0.f;
+            if (kind == Kind::NEAR) {
+#pragma unroll
+                for (int e = 0; e < 16; e++) s[e] = my_tab[k0 + 8 * (e >> 2) + (e & 3)];
+            } else {
+                c = kind == Kind::FAR_BEHIND ? c_behind : c_ahead;
+#pragma unroll
+                for (int e = 0; e < 16; e++) s[e] = 0.f;
+            }
+#pragma unroll
+            for (int st = 0; st < RowsT::STEPS; st++) s = Op<T>::mma(RowsT::read(sK, rl, 0, st), qf[st], s);
+            if (!CAUSAL && k0 + 32 > smp.length) {
+#pragma unroll
+                for (int e = 0; e < 16; e++) s[e] = k0 + 4 * hf + 8 * (e >> 2) + (e & 3) < smp.length ? s[e] : -INFINITY;
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) mx = fmaxf(mx, fmaxf(s[e], s[e + 1]));
+            mx = fmaf(max_halves(mx), a.scale_log2, c);
+            if (__any(mx > m_ref + 8.f)) {
+                const float m_new = fmaxf(m_ref, mx), alpha = m_new == -INFINITY ? 1.f : fast_exp2(m_ref - m_new);
+                m_ref = m_new;
+                l_part *= alpha;
+#pragma unroll
+                for (int j = 0; j < RowsT::BLOCKS; j++)
+#pragma unroll
+                    for (int e = 0; e < 16; e++) acc[j][e] *= alpha;
+            }
+            const float off = c - (m_ref == -INFINITY ? 0.f : m_ref);
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 16; e++) {
+                s[e] = fast_exp2(fmaf(s[e], a.scale_log2, off));
+                sum += s[e];
+            }
+            l_part += sum;
+            const Weights<T> w(s);
+#pragma unroll
+            for (int j = 0; j < RowsT::BLOCKS; j++) acc[j] = RowsT::weigh(sV, tl, lane, 0, j, w, acc[j]);
+        }
+    }
+
+    // the waves' results: references and sums [wave][32], O [wave][row][OROW], in their order
+    float *const ms = reinterpret_cast<float *>(smem), *const ls = ms + NW * 32, *const os = ls + NW * 32;
+    const float l_tot = sum_halves(l_part);
+    __syncthreads();
+    if (hf == 0) ms[wave * 32 + row] = m_ref, ls[wave * 32 + row] = l_tot;
+    if (row < n_rows) {
+        float *const o = os + (wave * 32 + row) * S::OROW + 4 * hf;
+#pragma unroll
+        for (int j = 0; j < RowsT::BLOCKS; j++)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; q4++)
+                *reinterpret_cast<f32x4 *>(o + 32 * j + 8 * q4) = f32x4{acc[j][4 * q4], acc[j][4 * q4 + 1], acc[j][4 * q4 + 2], acc[j][4 * q4 + 3]};
+    }
+    __syncthreads();
+    for (int x = tid; x < n_rows * (D / 4); x += NW * 64) {
+        const int r = x / (D / 4), c = x - r * (D / 4);
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < NW; w++) top = fmaxf(top, ms[w * 32 + r]);
+        float sum = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NW; w++) {
+            const float m = ms[w * 32 + r], weight = m == -INFINITY ? 0.f : fast_exp2(m - top);
+            const f32x4 y = *reinterpret_cast<const f32x4 *>(os + (w * 32 + r) * S::OROW + 4 * c);
+            sum = fmaf(weight, ls[w * 32 + r], sum);
+#pragma unroll
+            for (int e = 0; e < 4; e++) o[e] = fmaf(weight, y[e], o[e]);
+        }
+        const bool any = r >= first && r <= last && sum > 0.f;
+        const float inv = any ? 1.f / sum : 0.f, lse = any ? (top + __builtin_amdgcn_logf(sum)) * LN2 : -INFINITY;
+        const int i = r / gp, head = hb * gp + r - i * gp;
+        if (a.pieces > 1) {
+            const size_t at = ((size_t)bh * n_rows + r) * a.pieces + piece;
+            *reinterpret_cast<f32x4 *>(a.part_o + at * D + 4 * c) = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+            if (c == 0) a.part_lse[at] = lse;
+        } else {
+            store4((T *)a.o + (size_t)b * a.so.batch + (size_t)head * a.so.head + (size_t)i * a.so.row + 4 * c, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+            if (c == 0) a.lse[((size_t)b * a.heads + head) * a.n_q + i] = lse;
+        }
+    }
+}
+
+// O = sum_p exp(LSE_p - LSE) O_p, LSE = log sum_p exp(LSE_p) over the pieces of a row's keys, in their order, eight pieces requested at
+// a time
 template <typename T, int D>
 __global__ __launch_bounds__(256) void k_rel_join(RelFwdArgs a, long long rows)
 {
-    constexpr int LANES = D / 4, PER = 256 / LANES;
+    constexpr int LANES = D / 4, PER = 256 / LANES, U = 8;
     const long long r = (long long)blockIdx.x * PER + threadIdx.x / LANES;
     if (r >= rows) return;
-    const int c = threadIdx.x % LANES, n_rows = a.n_q * a.gp;
-    const float *pl = a.part_lse + r * a.pieces;
-    float top = -INFINITY;
-    for (unsigned p = 0; p < a.pieces; p++) top = fmaxf(top, pl[p]);
-    float sum = 0.f;
+    const int c = threadIdx.x % LANES, n_rows = a.n_q * a.gp, pieces = (int)a.pieces;
+    const float *pl = a.part_lse + r * pieces;
+    const f32x4 *po = reinterpret_cast<const f32x4 *>(a.part_o + (size_t)r * pieces * D) + c;
+    float top = -INFINITY, sum = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (unsigned p = 0; p < a.pieces; p++) {
-        const float l = pl[p];
-        if (l == -INFINITY) continue;
-        const float w = fast_exp2((l - top) * LOG2E);
-        const f32x4 x = *reinterpret_cast<const f32x4 *>(a.part_o + ((size_t)r * a.pieces + p) * D + 4 * c);
-        sum += w;
+    for (int p0 = 0; p0 < pieces; p0 += U) {
+        f32x4 x[U];
+        float l[U], most = top;
 #pragma unroll
-        for (int e = 0; e < 4; e++) acc[e] = fmaf(w, x[e], acc[e]);
+        for (int u = 0; u < U; u++) {
+            const int p = min(p0 + u, pieces - 1);
+            x[u] = po[p * LANES];
+            l[u] = pl[p];
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            if (p0 + u >= pieces) l[u] = -INFINITY;
+            most = fmaxf(most, l[u]);
+        }
+        if (most == -INFINITY) continue;
+        const float old = fast_exp2((top - most) * LOG2E);  // (nothing so far: 0)
+        sum *= old;
+#pragma unroll
+        for (int e = 0; e < 4; e++) acc[e] *= old;
+        top = most;
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const float w = fast_exp2((l[u] - top) * LOG2E);  // (a piece without keys: 0, its O is 0)
+            sum += w;
+#pragma unroll
+            for (int e = 0; e < 4; e++) acc[e] = fmaf(w, x[u][e], acc[e]);
+        }
     }
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
     const int bh = (int)(r / n_rows), row = (int)(r - (long long)bh * n_rows), b = bh / a.head_blocks, hb = bh - b * a.head_blocks;
@@ -209,30 +403,36 @@ __global__ __launch_bounds__(256) void k_rel_join(RelFwdArgs a, long long rows)
     if (c == 0) a.lse[((size_t)b * a.heads + head) * a.n_q + i] = sum > 0.f ? top + __builtin_amdgcn_logf(sum) * LN2 : -INFINITY;
 }
 
-template <typename T, int D>
-hdt_status_t launch(const RelFwdArgs &a, bool causal, hipStream_t st)
+template <typename K>
+hdt_status_t launch_kernel(K kernel, const char *name, dim3 grid, int threads, size_t lds, const RelFwdArgs &a, hipStream_t st)
 {
-    using S = FwdShape<T, D>;
-    const size_t lds = S::RING + (size_t)a.gp * table_length(a.bias.max_distance, causal) * sizeof(float);
+    HdtTimer t(name, st);
+    if (lds > 65536) HDT_HIP_TRY(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, st, a);
+    HDT_HIP_TRY(hipGetLastError());
+    return HDT_OK;
+}
+
+template <typename T, int D>
+hdt_status_t launch(const RelFwdArgs &a, int waves, bool causal, hipStream_t st)
+{
+    const size_t table = (size_t)a.gp * table_length(a.bias.max_distance, causal) * sizeof(float);
     const long long bh = (long long)a.batch * a.head_blocks;
-    const dim3 grid((unsigned)(bh * a.tiles * a.pieces)), block(S::NW * 64);
-    {
-        HdtTimer t("hdt_rel_fwd", st);
-        const void *f = causal ? (const void *)k_rel_fwd<T, D, true> : (const void *)k_rel_fwd<T, D, false>;
-        if (lds > 65536) HDT_HIP_TRY(hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-        if (causal)
-            hipLaunchKernelGGL((k_rel_fwd<T, D, true>), grid, block, lds, st, a);
-        else
-            hipLaunchKernelGGL((k_rel_fwd<T, D, false>), grid, block, lds, st, a);
-        HDT_HIP_TRY(hipGetLastError());
-    }
-    if (a.pieces > 1) {
-        HdtTimer t("hdt_rel_join", st);
-        const long long rows = bh * a.n_q * a.gp;
-        constexpr int PER = 256 / (D / 4);
-        hipLaunchKernelGGL((k_rel_join<T, D>), dim3((unsigned)((rows + PER - 1) / PER)), dim3(256), 0, st, a, rows);
-        HDT_HIP_TRY(hipGetLastError());
-    }
+    const dim3 grid((unsigned)(bh * a.tiles * a.pieces));
+    hdt_status_t r;
+    if (waves == 0)
+        r = launch_kernel(causal ? k_rel_few<T, D, true> : k_rel_few<T, D, false>, "hdt_rel_few", grid, FewShape<T, D>::NW * 64,
+                          FewShape<T, D>::RING + table, a, st);
+    else if (waves == 2)
+        r = launch_kernel(causal ? k_rel_fwd<T, D, 2, true> : k_rel_fwd<T, D, 2, false>, "hdt_rel_fwd", grid, 128, FwdShape<T, D, 2>::RING + table, a, st);
+    else
+        r = launch_kernel(causal ? k_rel_fwd<T, D, 4, true> : k_rel_fwd<T, D, 4, false>, "hdt_rel_fwd", grid, 256, FwdShape<T, D, 4>::RING + table, a, st);
+    if (r != HDT_OK || a.pieces == 1) return r;
+    HdtTimer t("hdt_rel_join", st);
+    const long long rows = bh * a.n_q * a.gp;
+    constexpr int PER = 256 / (D / 4);
+    hipLaunchKernelGGL((k_rel_join<T, D>), dim3((unsigned)((rows + PER - 1) / PER)), dim3(256), 0, st, a, rows);
+    HDT_HIP_TRY(hipGetLastError());
     return HDT_OK;
 }
 
@@ -241,25 +441,33 @@ hdt_status_t launch(const RelFwdArgs &a, bool causal, hipStream_t st)
 RelFwdPlan hdt_rel_fwd_plan(const hdt_rel_attn_t &d)
 {
     RelFwdPlan p;
-    constexpr int BM = 128, BN = 64;
     const int group = d.heads / d.kv_heads;
+    const size_t table = table_length(d.max_distance, d.causal != 0) * sizeof(float);
     // queries of the heads that share a key head together, where one head's do not fill a tile of rows (and the heads' tables fit)
-    p.gp = d.n_q < BM && (size_t)group * table_length(d.max_distance, d.causal != 0) * sizeof(float) <= 32768 ? group : 1;
+    p.gp = d.n_q < 128 && group * table <= 24576 ? group : 1;
     p.head_blocks = d.heads / p.gp;
-    p.tiles = (d.n_q * p.gp + BM - 1) / BM;
-    const long long items = (long long)d.batch * p.head_blocks * p.tiles, key_tiles = (d.n_kv + BN - 1) / BN;
-    long long pieces = items >= 512 ? 1 : (512 + items - 1) / items;
-    if (pieces > (key_tiles + 1) / 2) pieces = (key_tiles + 1) / 2;
+    const long long rows = (long long)d.n_q * p.gp, heads = (long long)d.batch * p.head_blocks;
+    long long pieces;
+    if (rows <= 32) {
+        p.waves = 0, p.tiles = 1;
+        // a workgroup takes about 1 us for 256 keys, a second kernel 4
+        pieces = d.n_kv <= 2048 ? 1 : std::min<long long>(1024 / heads, (d.n_kv + 1023) / 1024);
+    } else {
+        const long long tiles = heads * ((rows + 127) / 128);
+        p.waves = tiles < 512 ? 2 : 4;  // tiles of 64 rows where 128 would leave compute units without work
+        p.tiles = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
+        pieces = std::min<long long>(1024 / (heads * p.tiles), d.n_kv / 1024);
+    }
     p.pieces = pieces < 1 ? 1 : (unsigned)pieces;
-    const size_t rows = (size_t)d.batch * d.heads * d.n_q;
-    p.lse_at = rows * p.pieces * d.head_dim * sizeof(float);
-    p.bytes = p.pieces > 1 ? p.lse_at + rows * p.pieces * sizeof(float) : 0;
+    const size_t all = (size_t)d.batch * d.heads * d.n_q;
+    p.lse_at = all * p.pieces * d.head_dim * sizeof(float);
+    p.bytes = p.pieces > 1 ? p.lse_at + all * p.pieces * sizeof(float) : 0;
     return p;
 }
 
-hdt_status_t hdt_launch_rel_fwd(const hdt_rel_attn_t &d, const RelFwdArgs &a, hipStream_t st)
+hdt_status_t hdt_launch_rel_fwd(const hdt_rel_attn_t &d, const RelFwdArgs &a, int waves, hipStream_t st)
 {
     const bool causal = d.causal != 0;
-    if (d.dtype == HDT_BF16) return d.head_dim == 64 ? launch<__bf16, 64>(a, causal, st) : launch<__bf16, 128>(a, causal, st);
-    return d.head_dim == 64 ? launch<float, 64>(a, causal, st) : launch<float, 128>(a, causal, st);
+    if (d.dtype == HDT_BF16) return d.head_dim == 64 ? launch<__bf16, 64>(a, waves, causal, st) : launch<__bf16, 128>(a, waves, causal, st);
+    return d.head_dim == 64 ? launch<float, 64>(a, waves, causal, st) : launch<float, 128>(a, waves, causal, st);
 }
