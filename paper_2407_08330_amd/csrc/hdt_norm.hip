@@ -13,6 +13,7 @@
 #include <algorithm>
 
 #include "hdt_internal.h"
+#include "hdt_lanes.h"
 #include "hdt_mfma.h"
 
 namespace {
@@ -150,36 +151,11 @@ __global__ __launch_bounds__(256) void k_dropout_add(const T *y, const T *x, T *
 }
 
 // ------------------------------------------------------------------------------------------ sums over a row
-// The sum over a wave, in every lane: pairs, quads, eights and rows of 16 by shifted operands, rows and halves by exchanges (the
-// second operand of an exchange is made opaque: of two results of one value the compiler takes one).
-template <int CTRL>
-__device__ __forceinline__ float plus_dpp(float x)
-{
-    return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
-}
-__device__ __forceinline__ unsigned hidden(unsigned x)
-{
-    asm volatile("" : "+v"(x));
-    return x;
-}
-__device__ __forceinline__ float wave_sum(float x)
-{
-    x = plus_dpp<0xb1>(x);   // lane ^ 1
-    x = plus_dpp<0x4e>(x);   // lane ^ 2
-    x = plus_dpp<0x141>(x);  // the other quad of eight
-    x = plus_dpp<0x140>(x);  // the other eight of a row of 16
-    unsigned v = __builtin_bit_cast(unsigned, x);
-    const auto rows = __builtin_amdgcn_permlane16_swap(v, hidden(v), false, false);
-    x = __builtin_bit_cast(float, (unsigned)rows[0]) + __builtin_bit_cast(float, (unsigned)rows[1]);
-    v = __builtin_bit_cast(unsigned, x);
-    const auto half = __builtin_amdgcn_permlane32_swap(v, hidden(v), false, false);
-    return __builtin_bit_cast(float, (unsigned)half[0]) + __builtin_bit_cast(float, (unsigned)half[1]);
-}
 // the sum over the threads of a row: a wave, or (TPR > 64) the whole workgroup
 template <int TPR>
 __device__ __forceinline__ float row_sum(float x, float *lds)
 {
-    x = wave_sum(x);
+    x = hdt_lanes::wave_sum(x);
     if (TPR > 64) {
         __syncthreads();
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;

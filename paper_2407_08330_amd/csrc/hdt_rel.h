@@ -15,17 +15,22 @@
 // 16 bytes of a row are 8 contraction values of one instruction in bf16 and one value of each of four in fp32 (Op<T>).
 #pragma once
 
+#include <type_traits>
+
 #include "hdt_internal.h"
+#include "hdt_lanes.h"
 #include "hdt_mfma.h"
 #include "hdt_tile.h"
 
 namespace hdt_rel {
 
 using namespace hdt_tile;
+using namespace hdt_lanes;
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 
 constexpr int kPad = 128;             // distances the table goes on beyond the last one that matters: as far as 64 x 32 pairs reach, rows that are not real among them
+constexpr int kMostDistance = 1024;   // max_distance at most
 constexpr float kHidden = 1e6f;       // a bias from -1e6 down hides a bucket, one from 1e6 up counts as 1e6
 
 // one row-side operand fragment (16 bytes of a row) and the contractions it takes part in
@@ -57,11 +62,13 @@ struct Weights;
 template <>
 struct Weights<__bf16> {  // rounded to bf16: the operand type of the fast contraction; its sum is taken before
     bf16x8 lo, hi;
+    __device__ __forceinline__ Weights() = default;
     __device__ __forceinline__ explicit Weights(const f32x16 &p) : lo(pack_bf16x8(p, 0)), hi(pack_bf16x8(p, 8)) {}
 };
 template <>
 struct Weights<float> {
     f32x16 p;
+    __device__ __forceinline__ Weights() = default;
     __device__ __forceinline__ explicit Weights(const f32x16 &x) : p(x) {}
 };
 
@@ -77,22 +84,26 @@ struct Rows {
     {
         return *reinterpret_cast<const Frag *>(tile + (r0 + r.row) * ROWB + ((((st << 1) ^ r.x)) << 4));
     }
-    // acc += (rows r0 .. r0 + 31 of the tile, columns 32 j ..)^T times the weights of those rows
-    static __device__ __forceinline__ f32x16 weigh(const char *tile, const TrLane &t, int lane, int r0, int j, const Weights<T> &w, f32x16 acc)
+    // acc += (rows r0 .. r0 + 31 of the tile, columns 32 j ..)^T times the weights of those rows, in WSTEPS contractions: the operand of
+    // step s, and the contraction
+    static constexpr int WSTEPS = sizeof(T) == 2 ? 2 : 16;
+    typedef typename std::conditional<sizeof(T) == 2, bf16x8, float>::type WFrag;
+    static __device__ __forceinline__ WFrag wread(const char *tile, const TrLane &t, int lane, int r0, int j, int s)
     {
         if constexpr (sizeof(T) == 2) {
-            acc = mfma_32x32x16(read_tr<ROWB>(tile, t, r0, j), w.lo, acc);
-            acc = mfma_32x32x16(read_tr<ROWB>(tile, t, r0 + 16, j), w.hi, acc);
+            return read_tr<ROWB>(tile, t, r0 + 16 * s, j);
         } else {
-            const int c = 8 * j + ((lane & 31) >> 2), hf = lane >> 5;
-#pragma unroll
-            for (int v = 0; v < 16; v++) {
-                const int r = r0 + 8 * (v >> 2) + (v & 3) + 4 * hf;
-                const float a = *reinterpret_cast<const float *>(tile + r * ROWB + ((c ^ swz<CPR>(r & 31)) << 4) + (lane & 3) * 4);
-                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w.p[v], acc, 0, 0, 0);
-            }
+            const int c = 8 * j + ((lane & 31) >> 2), r = r0 + 8 * (s >> 2) + (s & 3) + 4 * (lane >> 5);
+            return *reinterpret_cast<const float *>(tile + r * ROWB + ((c ^ swz<CPR>(r & 31)) << 4) + (lane & 3) * 4);
         }
-        return acc;
+    }
+    static __device__ __forceinline__ f32x16 wmma(WFrag a, const Weights<T> &w, int s, f32x16 acc)
+    {
+        if constexpr (sizeof(T) == 2) {
+            return mfma_32x32x16(a, s ? w.hi : w.lo, acc);
+        } else {
+            return __builtin_amdgcn_mfma_f32_32x32x2f32(a, w.p[s], acc, 0, 0, 0);
+        }
     }
 };
 
@@ -105,7 +116,7 @@ struct Pair {
     static_assert(NI >= 1 && R % (RowsT::RPI * NW) == 0, "a wave loads whole instructions");
     const char *a, *b;               // row 0 of the two
     uint32_t stride_a, stride_b;     // bytes
-    uint32_t off_a[NI], off_b[NI];   // this lane's bytes of the rows it loads, from the tile's first row on
+    uint32_t off_a[NI], off_b[NI];  // this lane's bytes of the rows it loads, from the tile's first row on
     uint32_t lds;
     int wave, lane;
 
@@ -146,6 +157,91 @@ struct Pair {
     }
 };
 
+// Values the compiler loads itself are waited for here, in front of a loop whose own loads it does not count: where it first used them,
+// inside the loop, its wait would be repeated in every round, and would wait for the next tile.
+template <typename F>
+__device__ __forceinline__ void settle(const F &f)
+{
+    asm volatile("" ::"v"(f));
+}
+
+// N contractions whose operands come from LDS, AHEAD of them requested before the first is waited for and one more behind each
+// contraction.  Left to itself the compiler asks for an operand where it needs it and waits for it on the spot (to keep registers few),
+// which leaves a wave waiting for most of its time.  What may move across the fixed order is arithmetic (mask 0x406: vector, scalar and
+// transcendental instructions).
+template <int N, int AHEAD, typename Frag, typename Read>
+struct Ahead {
+    Frag buf[AHEAD];
+    const Read &read;
+    __device__ __forceinline__ explicit Ahead(const Read &r) : read(r)
+    {
+#pragma unroll
+        for (int i = 0; i < AHEAD && i < N; i++) buf[i] = read(i);
+        __builtin_amdgcn_sched_barrier(0x406);
+    }
+    template <typename Mma>
+    __device__ __forceinline__ void run(const Mma &mma)
+    {
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            mma(i, buf[i % AHEAD]);
+            if (i + AHEAD < N) buf[i % AHEAD] = read(i + AHEAD);
+            __builtin_amdgcn_sched_barrier(0x406);
+        }
+    }
+};
+template <int N, int AHEAD, typename Frag, typename Read>
+__device__ __forceinline__ Ahead<N, AHEAD, Frag, Read> ahead(const Read &read)
+{
+    return Ahead<N, AHEAD, Frag, Read>(read);
+}
+
+// The rounds of a walk along tiles that go through a ring of two stages: `tile(round, stage)`.  CONST: the stage is a constant for the
+// compiler, and the LDS addresses of both stages are then offsets of the same registers, for twice the code.
+template <bool CONST, typename Tile>
+__device__ __forceinline__ void walk(int rounds, const Tile &tile)
+{
+    int i = 0;
+    if constexpr (CONST) {
+        for (; i + 1 < rounds; i += 2) {
+            tile(i, std::integral_constant<int, 0>());
+            tile(i + 1, std::integral_constant<int, 1>());
+        }
+        if (i < rounds) tile(i, std::integral_constant<int, 0>());
+    } else {
+        for (; i < rounds; i++) tile(i, i & 1);
+    }
+}
+
+// A wave's 32 x D accumulators, held transposed (lane (row l % 32, hf), columns 32 j + 8 q + 4 hf ..), times the lane's `mult`, or zeros where it is
+// not `real`, to rows of a tensor: through 32 rows of LDS of the wave's own, so that whole rows leave, 16 bytes a lane.  (From the registers, 8 bytes to each of 32
+// rows an instruction, the stores took 40 of the 660 us of a backward of 4096 x 32 heads of 128.)  Row r keeps chunk c at c ^ (r & 7).
+template <typename T, int D>
+__device__ __forceinline__ void store_rows(char *wave_lds, int lane, const f32x16 (&acc)[D / 32], bool real, float mult, T *dst, int64_t stride, int rows_valid)
+{
+    typedef Rows<T, D> R;
+    const int r = lane & 31, hf = lane >> 5;
+    const uint32_t at = lds_addr(wave_lds) + (uint32_t)(r * R::ROWB);
+#pragma unroll
+    for (int j = 0; j < D / 32; j++)
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            const int c = sizeof(T) == 2 ? 4 * j + q : 8 * j + 2 * q + hf;
+            typedef T V __attribute__((ext_vector_type(4)));
+            V v;
+#pragma unroll
+            for (int e = 0; e < 4; e++) v[e] = (T)(real ? acc[j][4 * q + e] * mult : 0.f);
+            *(HDT_LDS V *)(uintptr_t)(at + (uint32_t)((c ^ (r & 7)) << 4) + (sizeof(T) == 2 ? hf * 8 : 0)) = v;
+        }
+    const int lr = lane / R::CPR, c = lane % R::CPR;
+#pragma unroll
+    for (int i = 0; i < 32 / R::RPI; i++) {
+        const int row = i * R::RPI + lr;
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(wave_lds + row * R::ROWB + ((c ^ (row & 7)) << 4));
+        if (row < rows_valid) *reinterpret_cast<u32x4 *>((char *)(dst + (int64_t)row * stride) + c * 16) = v;
+    }
+}
+
 // The rows of a sample that stand for positions, and its keys
 struct Sample {
     int start, length;  // position of query 0; keys
@@ -177,23 +273,33 @@ __device__ __forceinline__ int bucket_of(const BiasArgs &a, int distance)
     const int M = a.max_distance;
     return min(max(a.table[min(max(distance, -M), M) + M], 0), a.n_buckets - 1);
 }
-__device__ __forceinline__ float bias_of(const BiasArgs &a, int distance, int head)
+__device__ __forceinline__ float bias_at(const BiasArgs &a, int bucket, int head)
 {
-    const size_t at = (size_t)bucket_of(a, distance) * a.heads + head;
+    const size_t at = (size_t)bucket * a.heads + head;
     const float x = a.bf16 ? (float)((const __bf16 *)a.bias)[at] : ((const float *)a.bias)[at];
     // Values that stand for a mask are one (kHidden): a row that saw nothing else would have an LSE next to them, in whose fp32 the
     // logarithm of its sum is lost, and with it the row's gradients.
     return x <= -kHidden ? -INFINITY : fminf(x, kHidden) * a.inv_scale;
 }
-template <bool CAUSAL>
-__device__ __forceinline__ void fill_table(float *lds, const BiasArgs &a, int h0, int heads, int tid, int threads)
+__device__ __forceinline__ float bias_of(const BiasArgs &a, int distance, int head) { return bias_at(a, bucket_of(a, distance), head); }
+__device__ __forceinline__ void fill_table(float *to, const BiasArgs &a, int h0, int heads, bool causal, int tid, int threads)
 {
-    const int len = table_length(a.max_distance, CAUSAL);
-    for (int g = 0; g < heads; g++)
-        for (int x = tid; x < len; x += threads) {
-            const int d = x - a.max_distance - kPad;
-            lds[g * len + x] = CAUSAL && d > 0 ? -INFINITY : bias_of(a, d, h0 + g);
+    constexpr int U = 4;  // entries a thread has in flight: two loads each, the second at the first's word
+    const int len = table_length(a.max_distance, causal), M = a.max_distance, all = heads * len;
+    for (int x0 = tid; x0 < all; x0 += U * threads) {
+        int bucket[U];
+        float bias[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int x = x0 + u * threads, d = x % len - M - kPad;
+            bucket[u] = x < all && !(causal && d > 0) ? bucket_of(a, d) : -1;
         }
+#pragma unroll
+        for (int u = 0; u < U; u++) bias[u] = bucket[u] >= 0 ? bias_at(a, bucket[u], h0 + (x0 + u * threads) / len) : -INFINITY;
+#pragma unroll
+        for (int u = 0; u < U; u++)
+            if (x0 + u * threads < all) to[x0 + u * threads] = bias[u];
+    }
 }
 
 enum class Kind { SKIP, NEAR, FAR_BEHIND, FAR_AHEAD };
@@ -205,28 +311,6 @@ __device__ __forceinline__ Kind kind_of(int k0, int p0, int p1, int M, int lengt
     if (k0 + W - 1 - p0 <= -M) return Kind::FAR_BEHIND;
     if (!CAUSAL && k0 - p1 >= M) return Kind::FAR_AHEAD;
     return Kind::NEAR;
-}
-
-// A value of this lane and of the other lane of its column, in the other half-wave, in a fixed order: the lower half's, the upper
-// half's.  (The second operand is made opaque: of two results of one value the compiler takes one.)
-struct Halves {
-    float lower, upper;
-};
-__device__ __forceinline__ Halves halves(float x)
-{
-    const unsigned a = __builtin_bit_cast(unsigned, x), b = (unsigned)opaque((int)a);
-    const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
-    return {__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1])};
-}
-__device__ __forceinline__ float max_halves(float x)
-{
-    const Halves h = halves(x);
-    return fmaxf(h.lower, h.upper);
-}
-__device__ __forceinline__ float sum_halves(float x)
-{
-    const Halves h = halves(x);
-    return h.lower + h.upper;
 }
 
 }  // namespace hdt_rel

@@ -21,7 +21,7 @@ __global__ void k_rel_table(int32_t *table, int n_buckets, int max_distance, int
     table[x] = bucket + (both && d > 0 ? half : 0);
 }
 
-constexpr int kMostRows = 1 << 24, kMostDistance = 1024, kMostBuckets = 4096;
+constexpr int kMostRows = 1 << 24, kMostBuckets = 4096;
 constexpr int64_t kMostGrid = (1 << 20) - 1;  // tiles of 128 rows
 constexpr int64_t kMostRowStride = 1 << 20;  // elements: a tile's rows stay within 32-bit byte offsets
 
@@ -76,8 +76,8 @@ hdt_status_t check(const char *fn, const hdt_rel_attn_t *d)
     if (!hdt_finite(d->softmax_scale) || d->softmax_scale <= 1e-20f || d->softmax_scale >= 1e20f)
         return hdt_fail(HDT_ERR_INVALID_ARG, "%s: softmax_scale must be between 1e-20 and 1e20", fn);
     if (d->n_q > kMostRows || d->n_kv > kMostRows) return hdt_fail(HDT_ERR_SHAPE, "%s: more than %d rows", fn, kMostRows);
-    if (d->max_distance < 1 || d->max_distance > kMostDistance)
-        return hdt_fail(HDT_ERR_SHAPE, "%s: max_distance %d outside [1, %d]", fn, d->max_distance, kMostDistance);
+    if (d->max_distance < 1 || d->max_distance > hdt_rel::kMostDistance)
+        return hdt_fail(HDT_ERR_SHAPE, "%s: max_distance %d outside [1, %d]", fn, d->max_distance, hdt_rel::kMostDistance);
     if (d->n_buckets < 1 || d->n_buckets > kMostBuckets)
         return hdt_fail(HDT_ERR_SHAPE, "%s: n_buckets %d outside [1, %d]", fn, d->n_buckets, kMostBuckets);
     // a launch has fewer than 2^32 threads
@@ -104,8 +104,8 @@ HDT_EXPORT hdt_status_t hdt_rel_table(int32_t n_buckets, int32_t max_distance, i
     if (n_buckets < 0 || max_distance < 0) return hdt_fail(HDT_ERR_INVALID_ARG, "hdt_rel_table: negative size");
     if (n_buckets > kMostBuckets || half < 2 || (both_ways && n_buckets % 2))
         return hdt_fail(HDT_ERR_SHAPE, "hdt_rel_table: %d buckets (2 to %d; both ways an even number from 4 on)", n_buckets, kMostBuckets);
-    if (max_distance > kMostDistance || max_distance <= half / 2)
-        return hdt_fail(HDT_ERR_SHAPE, "hdt_rel_table: max_distance %d outside (%d, %d]", max_distance, half / 2, kMostDistance);
+    if (max_distance > hdt_rel::kMostDistance || max_distance <= half / 2)
+        return hdt_fail(HDT_ERR_SHAPE, "hdt_rel_table: max_distance %d outside (%d, %d]", max_distance, half / 2, hdt_rel::kMostDistance);
     if (!d_table) return hdt_fail(HDT_ERR_INVALID_ARG, "hdt_rel_table: NULL pointer");
     hipStream_t st = (hipStream_t)stream;
     HdtTimer t("hdt_rel_table", st);
@@ -189,6 +189,7 @@ HDT_EXPORT hdt_status_t hdt_rel_attn_bwd(const hdt_rel_attn_t *d, const void *q,
         return hdt_fail(HDT_ERR_INVALID_ARG, "%s: a 16-byte aligned workspace of %zu bytes needed, %zu given", fn, p.bytes, workspace ? workspace_bytes : (size_t)0);
     a.q = q, a.k = k, a.v = v, a.o = o, a.d_o = d_o, a.lse = lse, a.dq = dq, a.dk = dk, a.dv = dv, a.d_bias = d_bias_grad;
     a.row_scalars = (float *)workspace;
+    a.tables = (float *)((char *)workspace + p.tables_at);
     a.bins = (float *)((char *)workspace + p.bins_at);
     a.lengths = d->d_lengths, a.starts = d->d_q_start;
     a.bias = bias_args(*d);

@@ -27,12 +27,26 @@ struct RelFwdPlan {
 RelFwdPlan hdt_rel_fwd_plan(const hdt_rel_attn_t &d);
 hdt_status_t hdt_launch_rel_fwd(const hdt_rel_attn_t &d, const RelFwdArgs &a, int waves, hipStream_t st);
 
+// Waves of 32 rows a workgroup's tile has: 4, or 2 or 1 whose workgroups divide the walk along the other side among groups of waves, where
+// more rows would leave compute units without work.  A unit holds two workgroups of 4 or 2 waves of 64 columns, and one otherwise: 4 from
+// 1.5 (of 128 columns: one) a unit on, 1 where they fit at once; in fp32, whose walk is bound by the matrix instructions, up to twice that.
+// (us, 4 | 2 | 1 waves.  Backward bf16, heads x rows of 64: 128 x 512 47.6 | 58.8 | 136, 64 x 512 35.8 | 36.1 | 71, 32 x 512 27.5 | 26.5 | 39.9,
+// 16 x 512 27.1 | 22.2 | 25.9, 8 x 512 26.7 | 22.4 | 19.3; of 128: 32 x 512 36.0 | 41.9, 16 x 512 34.5 | 29.2.  fp32 of 64: 64 x 512
+// 112 | 116 | 152, 32 x 512 88 | 64 | 82, 16 x 512 87 | 54 | 47.  Forward bf16 of 64: 128 x 512 13.8 | 18.1 | 51, 64 x 512 12.2 | 10.9 | 26,
+// 16 x 512 11.6 | 9.6 | 8.8.)
+inline int hdt_rel_row_waves(long long tiles128, long long tiles32, const hdt_rel_attn_t &d)
+{
+    if (tiles128 >= (d.head_dim == 64 ? 384 : 256)) return 4;
+    return tiles32 > (d.dtype == HDT_BF16 ? 256 : 512) || d.head_dim == 128 ? 2 : 1;
+}
+
 struct RelBwdArgs {
     const void *q, *k, *v, *o, *d_o;
     const float *lse;
     void *dq, *dk, *dv, *d_bias;
     float *row_scalars;               // four arrays of [batch][heads][n_pad], see k_rel_rows
-    float *bins;                      // [heads][batch * tiles_q][n_buckets]: sums of dS
+    float *tables;                    // [heads][row]: bias by distance over the scale, row = table_row()
+    float *bins;                      // [heads][batch * tiles_q][row]: sums of dS by distance
     const int32_t *lengths, *starts;
     hdt_strides_t sq, sk, sv, so, sdo, sdq, sdk, sdv;
     hdt_rel::BiasArgs bias;
@@ -43,7 +57,7 @@ struct RelBwdArgs {
 
 struct RelBwdPlan {
     int32_t tiles_q, tiles_k, n_pad, waves;  // waves of a workgroup, 32 rows each
-    size_t bins_at, bytes;
+    size_t tables_at, bins_at, bytes;
 };
 RelBwdPlan hdt_rel_bwd_plan(const hdt_rel_attn_t &d);
 hdt_status_t hdt_launch_rel_bwd(const hdt_rel_attn_t &d, const RelBwdArgs &a, int waves, hipStream_t st);

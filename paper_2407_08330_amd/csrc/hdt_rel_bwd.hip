@@ -12,13 +12,20 @@ namespace {
 
 using namespace hdt_rel;
 
-// Four numbers of every row, four arrays of [batch][heads][n_pad]: n = -LSE log2(e), minus infinity for a row without keys (its pairs then
-// weigh exp2(-inf) = 0); -D; and n with the bias of far keys behind and ahead, what the exponent of a far block starts from.  Every
-// head's rows are filled up to whole tiles with rows without keys.
+// Four numbers of every row, four arrays of [batch][heads][n_pad]: n = -LSE / scale, minus infinity for a row without keys (its pairs then
+// weigh exp2(-inf) = 0); -D; and n with the bias of far keys behind and ahead, over the scale too: what the contractions of a far block
+// start from.  Every head's rows are filled up to whole tiles with rows without keys.
+// The last workgroups write every head's bias by distance, which the tiles' workgroups then read at one load's latency instead of two.
 constexpr int kRowsU = 2;  // rows a thread has in flight
+__host__ __device__ __forceinline__ int table_row(int max_distance, bool causal) { return (table_length(max_distance, causal) + 3) & ~3; }
 template <typename T, int D>
-__global__ __launch_bounds__(256) void k_rel_rows(RelBwdArgs a, long long rows)
+__global__ __launch_bounds__(256) void k_rel_rows(RelBwdArgs a, long long rows, unsigned row_groups, bool causal)
 {
+    if (blockIdx.x >= row_groups) {
+        const int h = blockIdx.x - row_groups;
+        fill_table(a.tables + (size_t)h * table_row(a.bias.max_distance, causal), a.bias, h, 1, causal, threadIdx.x, 256);
+        return;
+    }
     constexpr int LANES = D * (int)sizeof(T) / 16, PER = 256 / LANES, V = 16 / (int)sizeof(T);
     typedef typename Op<T>::Frag Frag;
     const int c = threadIdx.x % LANES;
@@ -47,11 +54,11 @@ __global__ __launch_bounds__(256) void k_rel_rows(RelBwdArgs a, long long rows)
         const int b = bh[u] / a.heads, h = bh[u] - b * a.heads;
         const Sample smp = sample_of(a.lengths, a.starts, b, a.n_q, a.n_kv);
         const bool dead = ri[u] < smp.lo || ri[u] >= smp.hi || lse[u] == -INFINITY;
-        const float n = dead ? -INFINITY : -lse[u] * LOG2E;
+        const float n = dead ? -INFINITY : -lse[u] * a.bias.inv_scale;
         a.row_scalars[r] = n;
         a.row_scalars[rows + r] = dead ? 0.f : -d;
-        a.row_scalars[2 * rows + r] = n + bias_of(a.bias, -a.bias.max_distance, h) * a.scale_log2;
-        a.row_scalars[3 * rows + r] = n + bias_of(a.bias, a.bias.max_distance, h) * a.scale_log2;
+        a.row_scalars[2 * rows + r] = n + bias_of(a.bias, -a.bias.max_distance, h);
+        a.row_scalars[3 * rows + r] = n + bias_of(a.bias, a.bias.max_distance, h);
     }
 }
 
@@ -77,29 +84,72 @@ __device__ __forceinline__ void add_diagonals(const f32x16 &x, float (&d)[3])
     }
 }
 
-template <typename T, int D, int NW_>
+constexpr int kAheadRows = 3, kAheadCols = 2;  // operands on their way from LDS
+
+// KS groups of NW waves take every KS-th tile of the walk, each through a ring of its own, and their sums are added up at the end
+template <typename T, int D, int NW_, int KS_>
 struct BwdShape {
-    static constexpr int NW = NW_, BM = 32 * NW, BN = sizeof(T) == 4 && D == 128 ? 32 : 64;
+    static constexpr int NW = NW_, KS = KS_, THREADS = NW * KS * 64, BM = 32 * NW, BN = sizeof(T) == 4 ? 32 : 64;
     static constexpr int RING = 2 * Pair<T, D, BN, NW>::STAGE, SCALARS = 2 * 4 * 256;  // two stages of four arrays of 64 floats
-    static constexpr int KB = BN / 32, J = sizeof(T) == 2 && D == 64 ? KB : 1;          // blocks of a tile, and how many at a time
+    static constexpr bool CONST = sizeof(T) == 2 && (D == 128 || KS == 1);
+    static constexpr int KB = BN / 32, J = CONST ? KB : 1;  // blocks of a tile, and how many at a time
 };
 
-// dQ of a tile of query rows, and the sums of its dS by bucket
-template <typename T, int D, int NW_, bool CAUSAL>
+// bytes of LDS that the joining of the groups leaves in use
+template <int NW, int KS, int BLOCKS>
+constexpr int kJoined = (KS - 1) * NW * BLOCKS * 16 * 256;
+
+// A wave's accumulators plus those of the same rows' waves in the other groups, in their order; false for those other waves
+template <int NW, int KS, int BLOCKS>
+__device__ __forceinline__ bool join_groups(char *smem, f32x16 (&acc)[BLOCKS], int grp, int wave, int lane)
+{
+    if constexpr (KS > 1) {
+        float *const at = reinterpret_cast<float *>(smem) + lane;
+        __syncthreads();
+        if (grp > 0) {
+            float *const to = at + ((grp - 1) * NW + wave) * BLOCKS * 16 * 64;
+#pragma unroll
+            for (int j = 0; j < BLOCKS; j++)
+#pragma unroll
+                for (int e = 0; e < 16; e++) to[(16 * j + e) * 64] = acc[j][e];
+        }
+        __syncthreads();
+        if (grp > 0) return false;
+#pragma unroll
+        for (int k = 1; k < KS; k++) {
+            const float *const from = at + ((k - 1) * NW + wave) * BLOCKS * 16 * 64;
+#pragma unroll
+            for (int j = 0; j < BLOCKS; j++)
+#pragma unroll
+                for (int e = 0; e < 16; e++) acc[j][e] += from[(16 * j + e) * 64];
+        }
+    }
+    return true;
+}
+
+// a head's bias by distance into LDS
+__device__ __forceinline__ void copy_table(float *lds, const RelBwdArgs &a, int h, int row, int tid, int threads)
+{
+    for (int x = 4 * tid; x < row; x += 4 * threads) *reinterpret_cast<f32x4 *>(lds + x) = *reinterpret_cast<const f32x4 *>(a.tables + (size_t)h * row + x);
+}
+
+// dQ of a tile of query rows, and the sums of its dS by distance
+template <typename T, int D, int NW_, int KS_, bool CAUSAL>
 __device__ __forceinline__ void dq_role(const RelBwdArgs &a, char *smem, int bh, int I)
 {
-    using S = BwdShape<T, D, NW_>;
+    using S = BwdShape<T, D, NW_, KS_>;
     using RowsT = Rows<T, D>;
-    constexpr int BM = S::BM, BN = S::BN, NW = S::NW, KB = S::KB, J = S::J;
-    const int M = a.bias.max_distance, len = table_length(M, CAUSAL);
-    float *const tab = reinterpret_cast<float *>(smem + S::RING), *const bins = tab + len;
+    constexpr int BM = S::BM, BN = S::BN, NW = S::NW, KS = S::KS, KB = S::KB, J = S::J;
+    const int M = a.bias.max_distance, len = table_length(M, CAUSAL), line = table_row(M, CAUSAL);
+    float *const tab = reinterpret_cast<float *>(smem + KS * S::RING), *const bins = tab + line;
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5;
+    const int wave_all = __builtin_amdgcn_readfirstlane(tid >> 6), grp = KS > 1 ? wave_all / NW : 0, wave = wave_all - grp * NW;
     const int b = bh / a.heads, h = bh - b * a.heads;
     const Sample smp = sample_of(a.lengths, a.starts, b, a.n_q, a.n_kv);
     const int r0 = I * BM, first = max(r0, smp.lo), last = min(r0 + BM, smp.hi) - 1;
     const int row = r0 + wave * 32 + (lane & 31);
-    const bool own = row < a.n_q, real = row >= first && row <= last;
+    const bool real = row >= first && row <= last;
     const int seen = first <= last ? (CAUSAL ? smp.start + last + 1 : smp.length) : 0, tiles = (seen + BN - 1) / BN;
 
     f32x16 acc[RowsT::BLOCKS];
@@ -107,9 +157,9 @@ __device__ __forceinline__ void dq_role(const RelBwdArgs &a, char *smem, int bh,
     for (int j = 0; j < RowsT::BLOCKS; j++)
 #pragma unroll
         for (int e = 0; e < 16; e++) acc[j][e] = 0.f;
-    float behind = 0.f, ahead = 0.f;                       // this lane's sums of dS in the far tiles
-    float *const my_bins = bins + (wave * 2 + hf) * len;   // one copy for each half-wave: no two lanes of an instruction meet
-    for (int x = tid; x < len * NW * 2; x += NW * 64) bins[x] = 0.f;
+    float behind = 0.f, beyond = 0.f;                       // this lane's sums of dS in the far tiles
+    float *const my_bins = bins + (wave_all * 2 + hf) * line;   // one copy for each half-wave: no two lanes of an instruction meet
+    for (int x = 4 * tid; x < line * NW * KS * 2; x += 4 * S::THREADS) *reinterpret_cast<f32x4 *>(bins + x) = f32x4{0.f, 0.f, 0.f, 0.f};
 
     if (tiles > 0) {
         const int rc = min(max(row, first), last), pos = smp.start + rc;
@@ -117,7 +167,7 @@ __device__ __forceinline__ void dq_role(const RelBwdArgs &a, char *smem, int bh,
         const size_t kvh = (size_t)(h / a.group);
         Pair<T, D, BN, NW> kv;
         kv.init((const T *)a.k + (size_t)b * a.sk.batch + kvh * a.sk.head, a.sk.row, (const T *)a.v + (size_t)b * a.sv.batch + kvh * a.sv.head,
-                a.sv.row, smem, wave, lane);
+                a.sv.row, smem + grp * S::RING, wave, lane);
         typename RowsT::Frag qf[RowsT::STEPS], dof[RowsT::STEPS];
         const char *qp = (const char *)((const T *)a.q + (size_t)b * a.sq.batch + (size_t)h * a.sq.head + (size_t)rc * a.sq.row);
         const char *dp = (const char *)((const T *)a.d_o + (size_t)b * a.sdo.batch + (size_t)h * a.sdo.head + (size_t)rc * a.sdo.row);
@@ -127,56 +177,60 @@ __device__ __forceinline__ void dq_role(const RelBwdArgs &a, char *smem, int bh,
             dof[st] = *reinterpret_cast<const typename RowsT::Frag *>(dp + (2 * st + hf) * 16);
         }
         const size_t at_row = (size_t)bh * a.n_pad + rc, rows = (size_t)a.batch * a.heads * a.n_pad;
-        const float nl = real ? a.row_scalars[at_row] : -INFINITY, nd = a.row_scalars[rows + at_row];
-        fill_table<CAUSAL>(tab, a.bias, h, 1, tid, NW * 64);
-        kv.request(0, 0, seen - 1, 0);
+        const float nl = real ? a.row_scalars[at_row] * a.scale_log2 : -INFINITY, nd = a.row_scalars[rows + at_row];
+        if (grp < tiles) kv.request(grp * BN, 0, seen - 1, 0);
+        copy_table(tab, a, h, line, tid, S::THREADS);
         const float *const my_tab = tab + 4 * hf - pos + M + kPad;
         float *const diagonal = my_bins + 4 * hf - (lane & 31) - (smp.start + r0 + wave * 32) + M + kPad;  // of key 0 and j = 0
         const RowLane rl = row_lane<RowsT::CPR>(lane);
         const TrLane tl = tr_lane<RowsT::CPR>(lane);
         __syncthreads();
+#pragma unroll
+        for (int st = 0; st < RowsT::STEPS; st++) {
+            settle(qf[st]);
+            settle(dof[st]);
+        }
+        settle(nl);
+        settle(nd);
         const float c_behind = tab[0] * a.scale_log2, c_ahead = tab[len - 1] * a.scale_log2;
+        f32x16 nd16;  // what dP starts from
+#pragma unroll
+        for (int e = 0; e < 16; e++) nd16[e] = nd;
 
-        auto tile = [&](int t, auto stage) {
-            constexpr int ST = decltype(stage)::value;
+        auto tile = [&](int round, auto stage) {
+            const int ST = stage, t = round * KS + grp;
             wait_vmcnt<0>();
             wg_barrier();
-            if (t + 1 < tiles) kv.request((t + 1) * BN, 0, seen - 1, 1 - ST);
-            const char *sK = smem + ST * kv.STAGE, *sV = sK + kv.TILE;
+            if (t + KS < tiles) kv.request((t + KS) * BN, 0, seen - 1, 1 - ST);
+            const char *sK = smem + grp * S::RING + ST * kv.STAGE, *sV = sK + kv.TILE;
             const Kind kind = kind_of<CAUSAL, BN>(t * BN, p0, p1, M, smp.length);
-            if (kind == Kind::SKIP || w0 > w1) return;  // (nor has a wave without real rows anything to do)
+            if (kind == Kind::SKIP || w0 > w1 || (KS > 1 && t >= tiles)) return;  // (nor has a wave without real rows anything to do)
             const float off = nl + (kind == Kind::FAR_BEHIND ? c_behind : kind == Kind::FAR_AHEAD ? c_ahead : 0.f);
 #pragma unroll
             for (int k2 = 0; k2 < KB; k2 += J) {
                 const int k0 = t * BN + 32 * k2;
                 f32x16 s[J], dp16[J];
+                // S^T = K Q^T, then dP^T - D = V dO^T - D
+                constexpr int N = J * RowsT::STEPS;
+                auto read = [&](int i) { return RowsT::read(i < N ? sK : sV, rl, (k2 + i % J) * 32, i % N / J); };
+                auto rows_ahead = ahead<2 * N, kAheadRows, typename RowsT::Frag>(read);
                 if (kind == Kind::NEAR) {
 #pragma unroll
-                    for (int u = 0; u < J; u++) {
+                    for (int u = 0; u < J; u++)
 #pragma unroll
                         for (int e = 0; e < 16; e++) s[u][e] = my_tab[k0 + 32 * u + 8 * (e >> 2) + (e & 3)];
-                        s[u] = Op<T>::mma(RowsT::read(sK, rl, (k2 + u) * 32, 0), qf[0], s[u]);
-                    }
                 } else {
 #pragma unroll
-                    for (int u = 0; u < J; u++) {
+                    for (int u = 0; u < J; u++)
 #pragma unroll
                         for (int e = 0; e < 16; e++) s[u][e] = 0.f;
-                        s[u] = Op<T>::mma(RowsT::read(sK, rl, (k2 + u) * 32, 0), qf[0], s[u]);
-                    }
                 }
-#pragma unroll
-                for (int u = 0; u < J; u++)
-#pragma unroll
-                    for (int e = 0; e < 16; e++) dp16[u][e] = nd;
-#pragma unroll
-                for (int st = 1; st < RowsT::STEPS; st++)
-#pragma unroll
-                    for (int u = 0; u < J; u++) s[u] = Op<T>::mma(RowsT::read(sK, rl, (k2 + u) * 32, st), qf[st], s[u]);
-#pragma unroll
-                for (int st = 0; st < RowsT::STEPS; st++)
-#pragma unroll
-                    for (int u = 0; u < J; u++) dp16[u] = Op<T>::mma(RowsT::read(sV, rl, (k2 + u) * 32, st), dof[st], dp16[u]);
+                rows_ahead.run([&](int i, typename RowsT::Frag f) {
+                    if (i < N) s[i % J] = Op<T>::mma(f, qf[i / J], s[i % J]);
+                    else dp16[i % J] = Op<T>::mma(f, dof[(i - N) / J], i < N + J ? nd16 : dp16[i % J]);
+                });
+                auto read_t = [&](int i) { return RowsT::wread(sK, tl, lane, (k2 + i / (RowsT::WSTEPS * RowsT::BLOCKS)) * 32, i % RowsT::BLOCKS, i / RowsT::BLOCKS % RowsT::WSTEPS); };
+                auto k_ahead = ahead<J * RowsT::WSTEPS * RowsT::BLOCKS, kAheadCols, typename RowsT::WFrag>(read_t);
                 if (!CAUSAL && k0 + 32 * J > smp.length) {
 #pragma unroll
                     for (int u = 0; u < J; u++)
@@ -204,76 +258,57 @@ __device__ __forceinline__ void dq_role(const RelBwdArgs &a, char *smem, int bh,
 #pragma unroll
                         for (int e = 0; e < 16; e++) sum += s[u][e];
                     if (CAUSAL || kind == Kind::FAR_BEHIND) behind += sum;
-                    else ahead += sum;
+                    else beyond += sum;
                 }
+                Weights<T> w[J];
 #pragma unroll
-                for (int u = 0; u < J; u++) {
-                    const Weights<T> w(s[u]);
-#pragma unroll
-                    for (int j = 0; j < RowsT::BLOCKS; j++) acc[j] = RowsT::weigh(sK, tl, lane, (k2 + u) * 32, j, w, acc[j]);
-                }
+                for (int u = 0; u < J; u++) w[u] = Weights<T>(s[u]);
+                k_ahead.run([&](int i, typename RowsT::WFrag f) {
+                    acc[i % RowsT::BLOCKS] = RowsT::wmma(f, w[i / (RowsT::WSTEPS * RowsT::BLOCKS)], i / RowsT::BLOCKS % RowsT::WSTEPS, acc[i % RowsT::BLOCKS]);
+                });
             }
         };
-        int t = 0;
-        for (; t + 1 < tiles; t += 2) {
-            tile(t, std::integral_constant<int, 0>());
-            tile(t + 1, std::integral_constant<int, 1>());
-        }
-        if (t < tiles) tile(t, std::integral_constant<int, 0>());
+        walk<S::CONST>((tiles + KS - 1) / KS, tile);  // (barriers are the whole workgroup's: every group takes the same number of rounds)
     }
     // the far tiles' sums join the bins at the two ends of the table
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        behind += __shfl_xor(behind, m);
-        if (!CAUSAL) ahead += __shfl_xor(ahead, m);
-    }
+    behind = wave_sum(behind);
+    if (!CAUSAL) beyond = wave_sum(beyond);
     __syncthreads();
     if (lane == 0) {
-        bins[wave * 2 * len] += behind;
-        if (!CAUSAL) bins[wave * 2 * len + len - 1] += ahead;
+        bins[wave_all * 2 * line] += behind;
+        if (!CAUSAL) bins[wave_all * 2 * line + len - 1] += beyond;
     }
-    __syncthreads();
-    // sums over the copies, by distance; their buckets beside them (the ring is free)
-    int *const bucket = reinterpret_cast<int *>(smem);
-    for (int x = tid; x < len; x += NW * 64) {
-        float sum = 0.f;
+    __syncthreads();  // (and the ring is free)
+    float *const out = a.bins + ((size_t)(h * a.batch + b) * a.tiles_q + I) * line;
+    for (int x = 4 * tid; x < line; x += 4 * S::THREADS) {
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int u = 0; u < NW * 2; u++) sum += bins[u * len + x];
-        const int d = x - M - kPad;
-        bins[x] = sum;
-        bucket[x] = CAUSAL && d > 0 ? -1 : bucket_of(a.bias, d);
+        for (int u = 0; u < NW * KS * 2; u++) {
+            const f32x4 y = *reinterpret_cast<const f32x4 *>(bins + u * line + x);
+#pragma unroll
+            for (int e = 0; e < 4; e++) sum[e] += y[e];
+        }
+        *reinterpret_cast<f32x4 *>(out + x) = sum;
     }
-    __syncthreads();
-    float *const out = a.bins + ((size_t)h * a.batch * a.tiles_q + (size_t)b * a.tiles_q + I) * a.bias.n_buckets;
-    for (int u = wave; u < a.bias.n_buckets; u += NW) {
-        float sum = 0.f;
-        for (int x = lane; x < len; x += 64) sum += bucket[x] == u ? bins[x] : 0.f;
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m);
-        if (lane == 0) out[u] = sum;
-    }
-    if (!own) return;
-    T *dq = (T *)a.dq + (size_t)b * a.sdq.batch + (size_t)h * a.sdq.head + (size_t)row * a.sdq.row;
-    const float mult = real ? a.scale : 0.f;
-#pragma unroll
-    for (int j = 0; j < RowsT::BLOCKS; j++)
-#pragma unroll
-        for (int q4 = 0; q4 < 4; q4++)
-            store4(dq + 32 * j + 8 * q4 + 4 * hf, acc[j][q4 * 4] * mult, acc[j][q4 * 4 + 1] * mult, acc[j][q4 * 4 + 2] * mult, acc[j][q4 * 4 + 3] * mult);
+    if (!join_groups<NW, KS>(smem, acc, grp, wave, lane)) return;
+    const int w0 = r0 + wave * 32;
+    store_rows<T, D>(smem + kJoined<NW, KS, RowsT::BLOCKS> + wave * 32 * RowsT::ROWB, opaque(lane), acc, real, a.scale,
+                     (T *)a.dq + (size_t)b * a.sdq.batch + (size_t)h * a.sdq.head + (size_t)w0 * a.sdq.row, a.sdq.row, a.n_q - w0);
 }
 
 // dK and dV of a tile of keys of one key head: over the query rows of every head that shares it
-template <typename T, int D, int NW_, bool CAUSAL>
+template <typename T, int D, int NW_, int KS_, bool CAUSAL>
 __device__ __forceinline__ void dkv_role(const RelBwdArgs &a, char *smem, int bk, int J0)
 {
-    using S = BwdShape<T, D, NW_>;
+    using S = BwdShape<T, D, NW_, KS_>;
     using RowsT = Rows<T, D>;
-    constexpr int BM = S::BM, BN = S::BN, NW = S::NW, KB = S::KB, J = S::J;
-    constexpr bool LEAN = D == 128;  // what can be computed anew from the lane number is: registers are short
-    const int M = a.bias.max_distance, len = table_length(M, CAUSAL);
-    float *const scal = reinterpret_cast<float *>(smem + S::RING), *const tab = scal + S::SCALARS / 4;
+    constexpr int BM = S::BM, BN = S::BN, NW = S::NW, KS = S::KS, KB = S::KB, J = S::J;
+    const int M = a.bias.max_distance, line = table_row(M, CAUSAL);
+    float *const scal_all = reinterpret_cast<float *>(smem + KS * S::RING), *const tab = scal_all + KS * S::SCALARS / 4;
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5;
+    const int wave_all = __builtin_amdgcn_readfirstlane(tid >> 6), grp = KS > 1 ? wave_all / NW : 0, wave = wave_all - grp * NW;
+    float *const scal = scal_all + grp * (S::SCALARS / 4);
     const int b = bk / a.kv_heads, kvh = bk - b * a.kv_heads;
     const Sample smp = sample_of(a.lengths, a.starts, b, a.n_q, a.n_kv);
     const int key0 = J0 * BM, kw0 = key0 + wave * 32, key = kw0 + (lane & 31), kc = min(key, smp.length - 1);
@@ -296,58 +331,65 @@ __device__ __forceinline__ void dkv_role(const RelBwdArgs &a, char *smem, int bk
             kf[st] = *reinterpret_cast<const typename RowsT::Frag *>(kp + (2 * st + hf) * 16);
             vf[st] = *reinterpret_cast<const typename RowsT::Frag *>(vp + (2 * st + hf) * 16);
         }
+#pragma unroll
+        for (int st = 0; st < RowsT::STEPS; st++) {
+            settle(kf[st]);
+            settle(vf[st]);
+        }
+        const RowLane rl = row_lane<RowsT::CPR>(lane);
+        const TrLane tl = tr_lane<RowsT::CPR>(lane);
         const size_t rows = (size_t)a.batch * a.heads * a.n_pad;
         for (int h = kvh * a.group; h < (kvh + 1) * a.group; h++) {
             Pair<T, D, BN, NW> qd;
             qd.init((const T *)a.q + (size_t)b * a.sq.batch + (size_t)h * a.sq.head, a.sq.row,
-                    (const T *)a.d_o + (size_t)b * a.sdo.batch + (size_t)h * a.sdo.head, a.sdo.row, smem, wave, lane);
+                    (const T *)a.d_o + (size_t)b * a.sdo.batch + (size_t)h * a.sdo.head, a.sdo.row, smem + grp * S::RING, wave, lane);
             const float *rs = a.row_scalars + ((size_t)b * a.heads + h) * a.n_pad;
             auto request = [&](int t, int stage) {
                 // (rows that are not real: copies, weighed zero)
                 qd.request(t * BN, smp.lo, smp.hi - 1, stage);
                 for (int w = wave; w < 4; w += NW)
-                    dma4(rs + w * rows + t * BN, (uint32_t)(lane & (BN - 1)) * 4u, qd.lds + S::RING + (stage * 4 + w) * 256);
+                    dma4(rs + w * rows + t * BN, (uint32_t)(lane & (BN - 1)) * 4u, __builtin_amdgcn_readfirstlane(lds_addr(scal) + (stage * 4 + w) * 256));
             };
             __syncthreads();  // the head before is done with the table and the ring
-            fill_table<CAUSAL>(tab, a.bias, h, 1, tid, NW * 64);
-            request(tile0, 0);
+            if (tile0 + grp < tile1) request(tile0 + grp, 0);
+            copy_table(tab, a, h, line, tid, S::THREADS);
             __syncthreads();
-            auto tile = [&](int t, auto stage) {
-                constexpr int ST = decltype(stage)::value;
+            auto tile = [&](int round, auto stage) {
+                const int ST = stage, t = tile0 + round * KS + grp;
                 wait_vmcnt<0>();
                 wg_barrier();
-                if (t + 1 < tile1) request(t + 1, 1 - ST);
-                const char *sQ = smem + ST * qd.STAGE, *sDO = sQ + qd.TILE;
+                if (t + KS < tile1) request(t + KS, 1 - ST);
+                const char *sQ = smem + grp * S::RING + ST * qd.STAGE, *sDO = sQ + qd.TILE;
                 const int q0 = smp.start + t * BN;  // position of the tile's first row
                 // seen from the wave's 32 keys: the kinds of keys kw0 .. kw0 + 31 against positions q0 .. q0 + BN - 1
                 const Kind kind = (CAUSAL && kw0 > q0 + BN - 1) || kw0 >= smp.length ? Kind::SKIP
                                   : kw0 + 31 - q0 <= -M                              ? Kind::FAR_BEHIND
                                   : !CAUSAL && kw0 - (q0 + BN - 1) >= M              ? Kind::FAR_AHEAD
                                                                                      : Kind::NEAR;
-                if (kind == Kind::SKIP) return;
+                if (kind == Kind::SKIP || (KS > 1 && t >= tile1)) return;
                 const float *const st4 = scal + ST * 256, *const nd = st4 + 64;
                 const float *const nl = kind == Kind::FAR_BEHIND ? st4 + 128 : kind == Kind::FAR_AHEAD ? st4 + 192 : st4;
-                const int ol = LEAN ? opaque(lane) : lane;
-                const RowLane rl = row_lane<RowsT::CPR>(ol);
-                const TrLane tl = tr_lane<RowsT::CPR>(ol);
 #pragma unroll
                 for (int q2 = 0; q2 < KB; q2 += J) {
                     f32x16 s[J], dp16[J];
+                    // S = Q K^T, then dP - D = dO V^T - D
+                    constexpr int N = J * RowsT::STEPS;
+                    auto read = [&](int i) { return RowsT::read(i < N ? sQ : sDO, rl, (q2 + i % J) * 32, i % N / J); };
+                    auto rows_ahead = ahead<2 * N, kAheadRows, typename RowsT::Frag>(read);
+#pragma unroll
+                    for (int u = 0; u < J; u++)
+#pragma unroll
+                        for (int q4 = 0; q4 < 4; q4++) {
+                            const f32x4 x = *reinterpret_cast<const f32x4 *>(nl + (q2 + u) * 32 + 4 * hf + 8 * q4);
+#pragma unroll
+                            for (int e = 0; e < 4; e++) s[u][4 * q4 + e] = x[e];
+                        }
                     if (kind == Kind::NEAR) {
-                        const float *my = tab + key - (q0 + 32 * q2) - 4 * hf + M + kPad;
+                        const float *my = tab + key - (q0 + 32 * q2) - 4 * hf + M + kPad - 64;  // (from 64 back: offsets count up)
 #pragma unroll
-                        for (int u = 0; u < J; u++) {
+                        for (int u = 0; u < J; u++)
 #pragma unroll
-                            for (int e = 0; e < 16; e++) s[u][e] = my[-(32 * u + 8 * (e >> 2) + (e & 3))];
-                            s[u] = Op<T>::mma(RowsT::read(sQ, rl, (q2 + u) * 32, 0), kf[0], s[u]);
-                        }
-                    } else {
-#pragma unroll
-                        for (int u = 0; u < J; u++) {
-#pragma unroll
-                            for (int e = 0; e < 16; e++) s[u][e] = 0.f;
-                            s[u] = Op<T>::mma(RowsT::read(sQ, rl, (q2 + u) * 32, 0), kf[0], s[u]);
-                        }
+                            for (int e = 0; e < 16; e++) s[u][e] += my[64 - (32 * u + 8 * (e >> 2) + (e & 3))];
                     }
 #pragma unroll
                     for (int u = 0; u < J; u++)
@@ -357,122 +399,140 @@ __device__ __forceinline__ void dkv_role(const RelBwdArgs &a, char *smem, int bk
 #pragma unroll
                             for (int e = 0; e < 4; e++) dp16[u][4 * q4 + e] = x[e];
                         }
-#pragma unroll
-                    for (int st = 1; st < RowsT::STEPS; st++)
-#pragma unroll
-                        for (int u = 0; u < J; u++) s[u] = Op<T>::mma(RowsT::read(sQ, rl, (q2 + u) * 32, st), kf[st], s[u]);
-#pragma unroll
-                    for (int st = 0; st < RowsT::STEPS; st++)
-#pragma unroll
-                        for (int u = 0; u < J; u++) dp16[u] = Op<T>::mma(RowsT::read(sDO, rl, (q2 + u) * 32, st), vf[st], dp16[u]);
+                    rows_ahead.run([&](int i, typename RowsT::Frag f) {
+                        if (i < N) s[i % J] = Op<T>::mma(f, kf[i / J], s[i % J]);
+                        else dp16[i % J] = Op<T>::mma(f, vf[(i - N) / J], dp16[i % J]);
+                    });
+                    constexpr int WN = J * RowsT::WSTEPS * RowsT::BLOCKS;
+                    auto column = [&](const char *from, int i) { return RowsT::wread(from, tl, lane, (q2 + i / (RowsT::WSTEPS * RowsT::BLOCKS)) * 32, i % RowsT::BLOCKS, i / RowsT::BLOCKS % RowsT::WSTEPS); };
+                    auto read_do = [&](int i) { return column(sDO, i); };
+                    auto read_q = [&](int i) { return column(sQ, i); };
+                    auto do_ahead = ahead<WN, kAheadCols, typename RowsT::WFrag>(read_do);
+                    Weights<T> w[J];
 #pragma unroll
                     for (int u = 0; u < J; u++) {
 #pragma unroll
-                        for (int q4 = 0; q4 < 4; q4++) {
-                            const f32x4 x = *reinterpret_cast<const f32x4 *>(nl + (q2 + u) * 32 + 4 * hf + 8 * q4);
-#pragma unroll
-                            for (int e = 0; e < 4; e++) s[u][4 * q4 + e] = fast_exp2(fmaf(s[u][4 * q4 + e], a.scale_log2, x[e]));
-                        }
-                        const Weights<T> w(s[u]);
-#pragma unroll
-                        for (int j = 0; j < RowsT::BLOCKS; j++) dv[j] = RowsT::weigh(sDO, tl, lane, (q2 + u) * 32, j, w, dv[j]);
+                        for (int e = 0; e < 16; e++) s[u][e] = fast_exp2(s[u][e] * a.scale_log2);
+                        w[u] = Weights<T>(s[u]);
                     }
+                    do_ahead.run([&](int i, typename RowsT::WFrag f) {
+                        dv[i % RowsT::BLOCKS] = RowsT::wmma(f, w[i / (RowsT::WSTEPS * RowsT::BLOCKS)], i / RowsT::BLOCKS % RowsT::WSTEPS, dv[i % RowsT::BLOCKS]);
+                    });
+                    auto q_ahead = ahead<WN, kAheadCols, typename RowsT::WFrag>(read_q);
 #pragma unroll
                     for (int u = 0; u < J; u++) {
 #pragma unroll
                         for (int e = 0; e < 16; e++) s[u][e] *= dp16[u][e];
-                        const Weights<T> w(s[u]);
-#pragma unroll
-                        for (int j = 0; j < RowsT::BLOCKS; j++) dk[j] = RowsT::weigh(sQ, tl, lane, (q2 + u) * 32, j, w, dk[j]);
+                        w[u] = Weights<T>(s[u]);
                     }
+                    q_ahead.run([&](int i, typename RowsT::WFrag f) {
+                        dk[i % RowsT::BLOCKS] = RowsT::wmma(f, w[i / (RowsT::WSTEPS * RowsT::BLOCKS)], i / RowsT::BLOCKS % RowsT::WSTEPS, dk[i % RowsT::BLOCKS]);
+                    });
                 }
             };
-            int t = tile0;
-            for (; t + 1 < tile1; t += 2) {
-                tile(t, std::integral_constant<int, 0>());
-                tile(t + 1, std::integral_constant<int, 1>());
-            }
-            if (t < tile1) tile(t, std::integral_constant<int, 0>());
+            walk<S::CONST>((tile1 - tile0 + KS - 1) / KS, tile);
         }
     }
-    if (key >= a.n_kv) return;
+    if (KS == 1) __syncthreads();  // (the ring is free)
+    join_groups<NW, KS>(smem, dk, grp, wave, lane);
+    if (!join_groups<NW, KS>(smem, dv, grp, wave, lane)) return;
+    static_assert(kJoined<NW, KS, RowsT::BLOCKS> + NW * 32 * RowsT::ROWB <= KS * S::RING, "they fit the rings");
     const bool real = key < smp.length;
-    T *ok = (T *)a.dk + (size_t)b * a.sdk.batch + (size_t)kvh * a.sdk.head + (size_t)key * a.sdk.row;
-    T *ov = (T *)a.dv + (size_t)b * a.sdv.batch + (size_t)kvh * a.sdv.head + (size_t)key * a.sdv.row;
-    const float mk = real ? a.scale : 0.f, mv = real ? 1.f : 0.f;
-#pragma unroll
-    for (int j = 0; j < RowsT::BLOCKS; j++)
-#pragma unroll
-        for (int q4 = 0; q4 < 4; q4++) {
-            store4(ok + 32 * j + 8 * q4 + 4 * hf, dk[j][q4 * 4] * mk, dk[j][q4 * 4 + 1] * mk, dk[j][q4 * 4 + 2] * mk, dk[j][q4 * 4 + 3] * mk);
-            store4(ov + 32 * j + 8 * q4 + 4 * hf, dv[j][q4 * 4] * mv, dv[j][q4 * 4 + 1] * mv, dv[j][q4 * 4 + 2] * mv, dv[j][q4 * 4 + 3] * mv);
-        }
+    char *const rows_lds = smem + kJoined<NW, KS, RowsT::BLOCKS> + wave * 32 * RowsT::ROWB;
+    const int le = opaque(lane);
+    store_rows<T, D>(rows_lds, le, dk, real, a.scale, (T *)a.dk + (size_t)b * a.sdk.batch + (size_t)kvh * a.sdk.head + (size_t)kw0 * a.sdk.row,
+                     a.sdk.row, a.n_kv - kw0);
+    store_rows<T, D>(rows_lds, le, dv, real, 1.f, (T *)a.dv + (size_t)b * a.sdv.batch + (size_t)kvh * a.sdv.head + (size_t)kw0 * a.sdv.row,
+                     a.sdv.row, a.n_kv - kw0);
 }
 
 // Both roles in one launch, the longest tiles first: level l holds key tile l of every key head and query tile tiles_q - 1 - l of
 // every head, which in the causal form have the same number of tiles to walk.
-template <typename T, int D, int NW, bool CAUSAL>
-__global__ __launch_bounds__(NW * 64, sizeof(T) == 4 ? 1 : 2) void k_rel_bwd(RelBwdArgs a)
+template <typename T, int D, int NW, int KS, bool CAUSAL>
+__global__ __launch_bounds__(NW * KS * 64, sizeof(T) == 4 || D == 128 ? 1 : 2) void k_rel_bwd(RelBwdArgs a)
 {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int nk = a.batch * a.kv_heads, nq = a.batch * a.heads, level = blockIdx.x / (nk + nq), x = blockIdx.x - level * (nk + nq);
     if (x < nk) {
-        if (level < a.tiles_k) dkv_role<T, D, NW, CAUSAL>(a, smem, x, level);
+        if (level < a.tiles_k) dkv_role<T, D, NW, KS, CAUSAL>(a, smem, x, level);
     } else if (level < a.tiles_q) {
-        dq_role<T, D, NW, CAUSAL>(a, smem, x - nk, a.tiles_q - 1 - level);
+        dq_role<T, D, NW, KS, CAUSAL>(a, smem, x - nk, a.tiles_q - 1 - level);
     }
 }
 
-// dbias of one head: the workgroups' sums by bucket added up in their order, 16 runs of them
-__global__ __launch_bounds__(1024) void k_rel_dbias(RelBwdArgs a, int parts)
+// dbias of one head: the workgroups' sums by distance added up in their order, several runs of them side by side; then by bucket
+__global__ __launch_bounds__(1024) void k_rel_dbias(RelBwdArgs a, int parts, bool causal)
 {
-    __shared__ float lds[16][64];
-    const int lane = threadIdx.x & 63, run = threadIdx.x >> 6, u = blockIdx.y * 64 + lane, h = blockIdx.x, nb = a.bias.n_buckets;
-    float sum = 0.f;
-    if (u < nb) {
-        const float *p = a.bins + (size_t)h * parts * nb + u;
-        for (int i = run; i < parts; i += 16) sum += p[(size_t)i * nb];
+    __shared__ f32x4 runs[1024];
+    __shared__ int bucket[4096];
+    const int tid = threadIdx.x, lane = tid & 63, h = blockIdx.x, nb = a.bias.n_buckets, M = a.bias.max_distance;
+    const int len = table_length(M, causal), line = table_row(M, causal), cols = line / 4, n = min(1024 / cols, 16), run = tid / cols;
+    for (int x = tid; x < len; x += 1024) {
+        const int d = x - M - kPad;
+        bucket[x] = causal && d > 0 ? -1 : bucket_of(a.bias, d);
     }
-    lds[run][lane] = sum;
-    __syncthreads();
-    if (run != 0 || u >= nb) return;
-    sum = 0.f;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    if (run < n) {
+        const float *p = a.bins + (size_t)h * parts * line + 4 * (tid - run * cols);
+#pragma unroll 4
+        for (int i = run; i < parts; i += n) {
+            const f32x4 y = *reinterpret_cast<const f32x4 *>(p + (size_t)i * line);
 #pragma unroll
-    for (int i = 0; i < 16; i++) sum += lds[i][lane];
-    if (a.bias.bf16)
-        ((__bf16 *)a.d_bias)[(size_t)u * a.heads + h] = (__bf16)sum;
-    else
-        ((float *)a.d_bias)[(size_t)u * a.heads + h] = sum;
+            for (int e = 0; e < 4; e++) sum[e] += y[e];
+        }
+    }
+    runs[tid] = sum;
+    __syncthreads();
+    if (run == 0) {
+        for (int i = 1; i < n; i++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) sum[e] += runs[i * cols + tid][e];
+        runs[tid] = sum;
+    }
+    __syncthreads();
+    const float *const by_distance = reinterpret_cast<const float *>(runs);
+    for (int u = tid >> 6; u < nb; u += 16) {
+        float s = 0.f;
+        for (int x = lane; x < len; x += 64) s += bucket[x] == u ? by_distance[x] : 0.f;
+        s = wave_sum(s);
+        if (lane != 0) continue;
+        if (a.bias.bf16)
+            ((__bf16 *)a.d_bias)[(size_t)u * a.heads + h] = (__bf16)s;
+        else
+            ((float *)a.d_bias)[(size_t)u * a.heads + h] = s;
+    }
 }
 
-template <typename T, int D, int NW>
+template <typename T, int D, int NW, int KS>
 hdt_status_t launch(const RelBwdArgs &a, bool causal, hipStream_t st)
 {
-    using S = BwdShape<T, D, NW>;
-    const int len = table_length(a.bias.max_distance, causal);
+    using S = BwdShape<T, D, NW, KS>;
+    const int line = table_row(a.bias.max_distance, causal);
     const long long rows = (long long)a.batch * a.heads * a.n_pad;
     if (rows > 0) {
         HdtTimer t("hdt_rel_rows", st);
         constexpr int PER = kRowsU * 256 / (D * (int)sizeof(T) / 16);
-        hipLaunchKernelGGL((k_rel_rows<T, D>), dim3((unsigned)((rows + PER - 1) / PER)), dim3(256), 0, st, a, rows);
+        const unsigned groups = (unsigned)((rows + PER - 1) / PER);
+        hipLaunchKernelGGL((k_rel_rows<T, D>), dim3(groups + (unsigned)a.heads), dim3(256), 0, st, a, rows, groups, causal);
         HDT_HIP_TRY(hipGetLastError());
     }
     const long long levels = std::max(a.heads ? a.tiles_q : 0, a.tiles_k), grid = levels * a.batch * (a.heads + a.kv_heads);
     if (grid > 0) {
         HdtTimer t("hdt_rel_bwd", st);
-        const size_t lds_q = S::RING + (size_t)len * (1 + 2 * NW) * sizeof(float), lds_k = S::RING + S::SCALARS + (size_t)len * sizeof(float);
+        const size_t lds_q = KS * S::RING + (size_t)line * (1 + 2 * NW * KS) * sizeof(float), lds_k = KS * (S::RING + S::SCALARS) + (size_t)line * sizeof(float);
         const size_t lds = lds_q > lds_k ? lds_q : lds_k;
-        const void *f = causal ? (const void *)k_rel_bwd<T, D, NW, true> : (const void *)k_rel_bwd<T, D, NW, false>;
+        const void *f = causal ? (const void *)k_rel_bwd<T, D, NW, KS, true> : (const void *)k_rel_bwd<T, D, NW, KS, false>;
         if (lds > 65536) HDT_HIP_TRY(hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
         if (causal)
-            hipLaunchKernelGGL((k_rel_bwd<T, D, NW, true>), dim3((unsigned)grid), dim3(NW * 64), lds, st, a);
+            hipLaunchKernelGGL((k_rel_bwd<T, D, NW, KS, true>), dim3((unsigned)grid), dim3(S::THREADS), lds, st, a);
         else
-            hipLaunchKernelGGL((k_rel_bwd<T, D, NW, false>), dim3((unsigned)grid), dim3(NW * 64), lds, st, a);
+            hipLaunchKernelGGL((k_rel_bwd<T, D, NW, KS, false>), dim3((unsigned)grid), dim3(S::THREADS), lds, st, a);
         HDT_HIP_TRY(hipGetLastError());
     }
     if (a.heads == 0) return HDT_OK;
     HdtTimer t("hdt_rel_dbias", st);
-    hipLaunchKernelGGL(k_rel_dbias, dim3((unsigned)a.heads, (unsigned)(a.bias.n_buckets + 63) / 64), dim3(1024), 0, st, a, a.batch * a.tiles_q);
+    static_assert(2 * kMostDistance + 2 * kPad <= 4096, "a head's distances fit k_rel_dbias");
+    hipLaunchKernelGGL(k_rel_dbias, dim3((unsigned)a.heads), dim3(1024), 0, st, a, a.batch * a.tiles_q, causal);
     HDT_HIP_TRY(hipGetLastError());
     return HDT_OK;
 }
@@ -480,7 +540,9 @@ hdt_status_t launch(const RelBwdArgs &a, bool causal, hipStream_t st)
 template <typename T, int D>
 hdt_status_t launch_shape(const RelBwdArgs &a, int nw, bool causal, hipStream_t st)
 {
-    return nw == 4 ? launch<T, D, 4>(a, causal, st) : launch<T, D, 2>(a, causal, st);
+    if (nw == 4) return launch<T, D, 4, 1>(a, causal, st);
+    if (nw == 2) return launch<T, D, 2, 2>(a, causal, st);
+    return launch<T, D, D == 64 ? 1 : 2, D == 64 ? 4 : 2>(a, causal, st);
 }
 
 }  // namespace
@@ -488,16 +550,19 @@ hdt_status_t launch_shape(const RelBwdArgs &a, int nw, bool causal, hipStream_t 
 RelBwdPlan hdt_rel_bwd_plan(const hdt_rel_attn_t &d)
 {
     RelBwdPlan p;
-    // tiles of 64 rows where 128 would leave compute units without work
-    const long long tiles = (long long)d.batch * d.heads * ((d.n_q + 127) / 128) + (long long)d.batch * d.kv_heads * ((d.n_kv + 127) / 128);
-    p.waves = tiles < 768 ? 2 : 4;
+    auto tiles = [&](long long bm) { return d.batch * (d.heads * ((d.n_q + bm - 1) / bm) + d.kv_heads * ((d.n_kv + bm - 1) / bm)); };
+    p.waves = hdt_rel_row_waves(tiles(128), tiles(32), d);
+    // (a ring for each group, the table, and a row of sums by distance for each half-wave have to fit a compute unit's LDS)
+    const size_t ring = (size_t)4 * (d.dtype == HDT_BF16 ? 64 * 2 : 32 * 4) * d.head_dim, line = table_row(d.max_distance, d.causal != 0) * sizeof(float);
+    while (p.waves < 4 && 4 / p.waves * ring + 9 * line > 160 * 1024) p.waves *= 2;
     const int bm = 32 * p.waves;
     p.tiles_q = (d.n_q + bm - 1) / bm;
     p.tiles_k = (d.n_kv + bm - 1) / bm;
     p.n_pad = (d.n_q + 127) & ~127;
     const size_t rows = (size_t)d.batch * d.heads * p.n_pad;
-    p.bins_at = (4 * rows * sizeof(float) + 255) & ~(size_t)255;
-    p.bytes = p.bins_at + (size_t)d.heads * d.batch * p.tiles_q * d.n_buckets * sizeof(float);
+    p.tables_at = (4 * rows * sizeof(float) + 255) & ~(size_t)255;
+    p.bins_at = p.tables_at + d.heads * line;
+    p.bytes = p.bins_at + (size_t)d.heads * d.batch * p.tiles_q * line;
     return p;
 }
 

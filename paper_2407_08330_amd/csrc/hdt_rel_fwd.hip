@@ -14,22 +14,27 @@ namespace {
 
 using namespace hdt_rel;
 
-template <typename T, int D, int NW_>
+constexpr int kAheadK = 4, kAheadV = 4;  // operands on their way from LDS
+
+// KS: groups of NW waves that take every KS-th key tile, each through a ring of its own, and join at the end.  Where there are few row
+// tiles a wave's walk along the keys is what takes the time, and this shortens it.
+template <typename T, int D, int NW_, int KS_>
 struct FwdShape {
-    static constexpr int NW = NW_, BM = 32 * NW, BN = sizeof(T) == 4 && D == 128 ? 32 : 64;
+    static constexpr int NW = NW_, KS = KS_, THREADS = NW * KS * 64, BM = 32 * NW, BN = sizeof(T) == 4 ? 32 : 64;
     static constexpr int RING = 2 * Pair<T, D, BN, NW>::STAGE;
 };
 
-template <typename T, int D, int NW_, bool CAUSAL>
-__global__ __launch_bounds__(NW_ * 64, sizeof(T) == 4 && D == 128 ? 1 : 2) void k_rel_fwd(RelFwdArgs a)
+template <typename T, int D, int NW_, int KS_, bool CAUSAL>
+__global__ __launch_bounds__(NW_ * KS_ * 64, sizeof(T) == 4 && D == 128 ? 1 : 2) void k_rel_fwd(RelFwdArgs a)
 {
-    using S = FwdShape<T, D, NW_>;
+    using S = FwdShape<T, D, NW_, KS_>;
     using RowsT = Rows<T, D>;
-    constexpr int BM = S::BM, BN = S::BN, NW = S::NW, KB = BN / 32;
+    constexpr int BM = S::BM, BN = S::BN, NW = S::NW, KS = S::KS, KB = BN / 32;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    float *const tab = reinterpret_cast<float *>(smem + S::RING);
+    float *const tab = reinterpret_cast<float *>(smem + KS * S::RING);
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5;
+    const int wave_all = __builtin_amdgcn_readfirstlane(tid >> 6), grp = KS > 1 ? wave_all / NW : 0, wave = wave_all - grp * NW;
     // the longest tiles first; the head blocks side by side, so that with a multiple of 8 of them each stays on one XCD and in its L2
     const unsigned heads = (unsigned)(a.batch * a.head_blocks), tp = blockIdx.x / heads, piece = tp % a.pieces;
     const int bh = blockIdx.x - tp * heads, I = a.tiles - 1 - (int)(tp / a.pieces), b = bh / a.head_blocks, hb = bh - b * a.head_blocks;
@@ -61,52 +66,48 @@ __global__ __launch_bounds__(NW_ * 64, sizeof(T) == 4 && D == 128 ? 1 : 2) void 
         const size_t kvh = (size_t)(hb * gp / a.group);
         Pair<T, D, BN, NW> kv;
         kv.init((const T *)a.k + (size_t)b * a.sk.batch + kvh * a.sk.head, a.sk.row, (const T *)a.v + (size_t)b * a.sv.batch + kvh * a.sv.head,
-                a.sv.row, smem, wave, lane);
+                a.sv.row, smem + grp * S::RING, wave, lane);
         typename RowsT::Frag qf[RowsT::STEPS];
         const char *qp = (const char *)((const T *)a.q + (size_t)b * a.sq.batch + (size_t)(hb * gp + g) * a.sq.head + (size_t)qi * a.sq.row);
 #pragma unroll
         for (int st = 0; st < RowsT::STEPS; st++) qf[st] = *reinterpret_cast<const typename RowsT::Frag *>(qp + (2 * st + hf) * 16);
-        fill_table<CAUSAL>(tab, a.bias, hb * gp, gp, tid, NW * 64);
-        kv.request(tile0 * BN, 0, seen - 1, 0);
+        if (tile0 + grp < tile1) kv.request((tile0 + grp) * BN, 0, seen - 1, 0);
+        fill_table(tab, a.bias, hb * gp, gp, CAUSAL, tid, S::THREADS);
         const int len = table_length(M, CAUSAL);
         const float *const my_tab = tab + g * len + 4 * hf - pos + M + kPad;
         const RowLane rl = row_lane<RowsT::CPR>(lane);
         const TrLane tl = tr_lane<RowsT::CPR>(lane);
         __syncthreads();
+#pragma unroll
+        for (int st = 0; st < RowsT::STEPS; st++) settle(qf[st]);
         const float c_behind = tab[g * len] * a.scale_log2, c_ahead = CAUSAL ? 0.f : tab[g * len + len - 1] * a.scale_log2;
 
-        // one tile of keys, in stage ST of the ring (a constant: the LDS addresses of both stages are then offsets of the same registers)
-        auto tile = [&](int t, auto stage) {
-            constexpr int ST = decltype(stage)::value;
+        auto tile = [&](int round, auto stage) {  // one tile of keys
+            const int ST = stage, t = tile0 + round * KS + grp;
             wait_vmcnt<0>();
             wg_barrier();
-            if (t + 1 < tile1) kv.request((t + 1) * BN, 0, seen - 1, 1 - ST);
-            const char *sK = smem + ST * kv.STAGE, *sV = sK + kv.TILE;
+            if (t + KS < tile1) kv.request((t + KS) * BN, 0, seen - 1, 1 - ST);
+            const char *sK = smem + grp * S::RING + ST * kv.STAGE, *sV = sK + kv.TILE;
             const int k0 = t * BN;
             const Kind kind = kind_of<CAUSAL, BN>(k0, p0, p1, M, smp.length);
-            if (kind == Kind::SKIP || w0 > w1) return;  // (nor has a wave without real rows anything to do)
+            if (kind == Kind::SKIP || w0 > w1 || (KS > 1 && t >= tile1)) return;  // (nor has a wave without real rows anything to do)
             f32x16 s[KB];
             float c = 0.f;
+            auto read_k = [&](int i) { return RowsT::read(sK, rl, i % KB * 32, i / KB); };
+            auto k_ahead = ahead<KB * RowsT::STEPS, kAheadK, typename RowsT::Frag>(read_k);
             if (kind == Kind::NEAR) {
 #pragma unroll
-                for (int kb = 0; kb < KB; kb++) {
+                for (int kb = 0; kb < KB; kb++)
 #pragma unroll
                     for (int e = 0; e < 16; e++) s[kb][e] = my_tab[k0 + 32 * kb + 8 * (e >> 2) + (e & 3)];
-                    s[kb] = Op<T>::mma(RowsT::read(sK, rl, kb * 32, 0), qf[0], s[kb]);
-                }
+                k_ahead.run([&](int i, typename RowsT::Frag f) { s[i % KB] = Op<T>::mma(f, qf[i / KB], s[i % KB]); });
             } else {
                 c = kind == Kind::FAR_BEHIND ? c_behind : c_ahead;
-#pragma unroll
-                for (int kb = 0; kb < KB; kb++) {
-#pragma unroll
-                    for (int e = 0; e < 16; e++) s[kb][e] = 0.f;
-                    s[kb] = Op<T>::mma(RowsT::read(sK, rl, kb * 32, 0), qf[0], s[kb]);
-                }
+                const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                k_ahead.run([&](int i, typename RowsT::Frag f) { s[i % KB] = Op<T>::mma(f, qf[i / KB], i < KB ? zero : s[i % KB]); });
             }
-#pragma unroll
-            for (int st = 1; st < RowsT::STEPS; st++)
-#pragma unroll
-                for (int kb = 0; kb < KB; kb++) s[kb] = Op<T>::mma(RowsT::read(sK, rl, kb * 32, st), qf[st], s[kb]);
+            auto read_v = [&](int i) { return RowsT::wread(sV, tl, lane, i / (RowsT::WSTEPS * RowsT::BLOCKS) * 32, i % RowsT::BLOCKS, i / RowsT::BLOCKS % RowsT::WSTEPS); };
+            auto v_ahead = ahead<KB * RowsT::WSTEPS * RowsT::BLOCKS, kAheadV, typename RowsT::WFrag>(read_v);
             if (!CAUSAL && k0 + BN > smp.length) {
 #pragma unroll
                 for (int kb = 0; kb < KB; kb++)
@@ -129,6 +130,7 @@ __global__ __launch_bounds__(NW_ * 64, sizeof(T) == 4 && D == 128 ? 1 : 2) void 
                     for (int e = 0; e < 16; e++) acc[j][e] *= alpha;
             }
             const float off = c - (m_ref == -INFINITY ? 0.f : m_ref);
+            Weights<T> w[KB];
 #pragma unroll
             for (int kb = 0; kb < KB; kb++) {
                 float sum = 0.f;
@@ -138,51 +140,75 @@ __global__ __launch_bounds__(NW_ * 64, sizeof(T) == 4 && D == 128 ? 1 : 2) void 
                     sum += s[kb][e];
                 }
                 l_part += sum;
-                const Weights<T> w(s[kb]);
-#pragma unroll
-                for (int j = 0; j < RowsT::BLOCKS; j++) acc[j] = RowsT::weigh(sV, tl, lane, kb * 32, j, w, acc[j]);
+                w[kb] = Weights<T>(s[kb]);
             }
+            v_ahead.run([&](int i, typename RowsT::WFrag f) {
+                acc[i % RowsT::BLOCKS] = RowsT::wmma(f, w[i / (RowsT::WSTEPS * RowsT::BLOCKS)], i / RowsT::BLOCKS % RowsT::WSTEPS, acc[i % RowsT::BLOCKS]);
+            });
         };
-        int t = tile0;
-        for (; t + 1 < tile1; t += 2) {
-            tile(t, std::integral_constant<int, 0>());
-            tile(t + 1, std::integral_constant<int, 1>());
-        }
-        if (t < tile1) tile(t, std::integral_constant<int, 0>());
+        walk<true>((tile1 - tile0 + KS - 1) / KS, tile);  // (barriers are the whole workgroup's: every group takes the same number of rounds)
     }
 
+    if constexpr (KS > 1) {  // the groups' results, in their order, a wave's beside those of the same rows
+        constexpr int REGS = 16 * RowsT::BLOCKS + 2;
+        static_assert((KS - 1) * NW * REGS * 256 <= KS * S::RING, "they fit the rings");
+        float *const at = reinterpret_cast<float *>(smem) + lane;
+        __syncthreads();
+        if (grp > 0) {
+            float *const to = at + ((grp - 1) * NW + wave) * REGS * 64;
+            to[0] = m_ref, to[64] = l_part;
+#pragma unroll
+            for (int j = 0; j < RowsT::BLOCKS; j++)
+#pragma unroll
+                for (int e = 0; e < 16; e++) to[(2 + 16 * j + e) * 64] = acc[j][e];
+        }
+        __syncthreads();
+        if (grp > 0) return;
+#pragma unroll
+        for (int k = 1; k < KS; k++) {
+            const float *const from = at + ((k - 1) * NW + wave) * REGS * 64;
+            const float m = from[0], top = fmaxf(m, m_ref), w = m == -INFINITY ? 0.f : fast_exp2(m - top), own_w = m_ref == -INFINITY ? 0.f : fast_exp2(m_ref - top);
+            m_ref = top;
+            l_part = l_part * own_w + from[64] * w;
+#pragma unroll
+            for (int j = 0; j < RowsT::BLOCKS; j++)
+#pragma unroll
+                for (int e = 0; e < 16; e++) acc[j][e] = acc[j][e] * own_w + from[(2 + 16 * j + e) * 64] * w;
+        }
+    }
+    // rows on their way out: behind what the joining used
+    char *const out_lds = smem + (KS - 1) * NW * (16 * RowsT::BLOCKS + 2) * 256 + wave * 32 * D * 4;
+    static_assert((KS - 1) * NW * (16 * RowsT::BLOCKS + 2) * 256 + NW * 32 * D * 4 <= KS * S::RING, "they fit the rings");
     const float l_tot = sum_halves(l_part);
     const float inv = real && l_tot > 0.f ? 1.f / l_tot : 0.f;
     const float lse = real && l_tot > 0.f ? (m_ref + __builtin_amdgcn_logf(l_tot)) * LN2 : -INFINITY;
-    if (!own) return;
     const int oi = row / gp, og = row - oi * gp, head = hb * gp + og;
     if (a.pieces > 1) {
-        const size_t at = ((size_t)bh * n_rows + row) * a.pieces + piece;
-        float *o = a.part_o + at * D;
-#pragma unroll
-        for (int j = 0; j < RowsT::BLOCKS; j++)
-#pragma unroll
-            for (int q4 = 0; q4 < 4; q4++) {
-                f32x4 x;
-#pragma unroll
-                for (int e = 0; e < 4; e++) x[e] = acc[j][q4 * 4 + e] * inv;
-                *reinterpret_cast<f32x4 *>(o + 32 * j + 8 * q4 + 4 * hf) = x;
-            }
-        if (hf == 0) a.part_lse[at] = lse;
+        if (KS == 1) __syncthreads();  // (the ring is free)
+        const size_t at = (size_t)bh * n_rows + r0 + wave * 32;
+        store_rows<float, D>(out_lds, lane, acc, real, inv, a.part_o + (at * a.pieces + piece) * D, (int64_t)a.pieces * D, n_rows - r0 - wave * 32);
+        if (own && hf == 0) a.part_lse[(at + (lane & 31)) * a.pieces + piece] = lse;
         return;
     }
-    T *o = (T *)a.o + (size_t)b * a.so.batch + (size_t)head * a.so.head + (size_t)oi * a.so.row;
+    if (own && hf == 0) a.lse[((size_t)b * a.heads + head) * a.n_q + oi] = lse;
+    T *const o = (T *)a.o + (size_t)b * a.so.batch;
+    if (gp == 1) {
+        if (KS == 1) __syncthreads();
+        store_rows<T, D>(out_lds, lane, acc, real, inv, o + (size_t)hb * a.so.head + (size_t)(r0 + wave * 32) * a.so.row, a.so.row, n_rows - r0 - wave * 32);
+        return;
+    }
+    if (!own) return;
+    T *const to = o + (size_t)head * a.so.head + (size_t)oi * a.so.row;  // (rows of several heads)
 #pragma unroll
     for (int j = 0; j < RowsT::BLOCKS; j++)
 #pragma unroll
         for (int q4 = 0; q4 < 4; q4++)
-            store4(o + 32 * j + 8 * q4 + 4 * hf, acc[j][q4 * 4] * inv, acc[j][q4 * 4 + 1] * inv, acc[j][q4 * 4 + 2] * inv, acc[j][q4 * 4 + 3] * inv);
-    if (hf == 0) a.lse[((size_t)b * a.heads + head) * a.n_q + oi] = lse;
+            store4(to + 32 * j + 8 * q4 + 4 * hf, acc[j][q4 * 4] * inv, acc[j][q4 * 4 + 1] * inv, acc[j][q4 * 4 + 2] * inv, acc[j][q4 * 4 + 3] * inv);
 }
 
 // Few rows (at most 32 in a head block: new tokens): the waves of a workgroup divide the keys instead of the rows.  Each walks blocks of
 // 32 keys through a ring of its own (no barriers; two blocks in flight a wave, 64 KB a workgroup, which the stream from memory
-// wants) and they join what they have in LDS, so that up to a few thousand keys need no second kernel.
+// wants) and they join what they have in LDS.
 template <typename T, int D>
 struct FewShape {
     static constexpr int ROWB = Rows<T, D>::ROWB, NW = 1024 / ROWB, NI = 32 * ROWB / 1024;
@@ -247,12 +273,14 @@ __global__ __launch_bounds__((FewShape<T, D>::NW * 64)) void k_rel_few(RelFwdArg
         const char *qp = (const char *)((const T *)a.q + (size_t)b * a.sq.batch + (size_t)(hb * gp + g) * a.sq.head + (size_t)qi * a.sq.row);
 #pragma unroll
         for (int st = 0; st < RowsT::STEPS; st++) qf[st] = *reinterpret_cast<const typename RowsT::Frag *>(qp + (2 * st + hf) * 16);
-        fill_table<CAUSAL>(tab, a.bias, hb * gp, gp, tid, NW * 64);
+        fill_table(tab, a.bias, hb * gp, gp, CAUSAL, tid, NW * 64);
         const int len = table_length(M, CAUSAL);
         const float *const my_tab = tab + g * len + 4 * hf - pos + M + kPad;
         const RowLane rl = row_lane<RowsT::CPR>(lane);
         const TrLane tl = tr_lane<RowsT::CPR>(lane);
         __syncthreads();
+#pragma unroll
+        for (int st = 0; st < RowsT::STEPS; st++) settle(qf[st]);
         const float c_behind = tab[g * len] * a.scale_log2, c_ahead = CAUSAL ? 0.f : tab[g * len + len - 1] * a.scale_log2;
 
         int stage = 0;
@@ -307,7 +335,9 @@ __global__ __launch_bounds__((FewShape<T, D>::NW * 64)) void k_rel_few(RelFwdArg
             l_part += sum;
             const Weights<T> w(s);
 #pragma unroll
-            for (int j = 0; j < RowsT::BLOCKS; j++) acc[j] = RowsT::weigh(sV, tl, lane, 0, j, w, acc[j]);
+            for (int x = 0; x < RowsT::WSTEPS; x++)
+#pragma unroll
+                for (int j = 0; j < RowsT::BLOCKS; j++) acc[j] = RowsT::wmma(RowsT::wread(sV, tl, lane, 0, j, x), w, x, acc[j]);
         }
     }
 
@@ -413,6 +443,13 @@ hdt_status_t launch_kernel(K kernel, const char *name, dim3 grid, int threads, s
     return HDT_OK;
 }
 
+template <typename T, int D, int NW, int KS>
+hdt_status_t launch_rows(const RelFwdArgs &a, bool causal, dim3 grid, size_t table, hipStream_t st)
+{
+    using S = FwdShape<T, D, NW, KS>;
+    return launch_kernel(causal ? k_rel_fwd<T, D, NW, KS, true> : k_rel_fwd<T, D, NW, KS, false>, "hdt_rel_fwd", grid, S::THREADS, KS * S::RING + table, a, st);
+}
+
 template <typename T, int D>
 hdt_status_t launch(const RelFwdArgs &a, int waves, bool causal, hipStream_t st)
 {
@@ -423,10 +460,12 @@ hdt_status_t launch(const RelFwdArgs &a, int waves, bool causal, hipStream_t st)
     if (waves == 0)
         r = launch_kernel(causal ? k_rel_few<T, D, true> : k_rel_few<T, D, false>, "hdt_rel_few", grid, FewShape<T, D>::NW * 64,
                           FewShape<T, D>::RING + table, a, st);
+    else if (waves == 4)
+        r = launch_rows<T, D, 4, 1>(a, causal, grid, table, st);
     else if (waves == 2)
-        r = launch_kernel(causal ? k_rel_fwd<T, D, 2, true> : k_rel_fwd<T, D, 2, false>, "hdt_rel_fwd", grid, 128, FwdShape<T, D, 2>::RING + table, a, st);
+        r = launch_rows<T, D, 2, 2>(a, causal, grid, table, st);
     else
-        r = launch_kernel(causal ? k_rel_fwd<T, D, 4, true> : k_rel_fwd<T, D, 4, false>, "hdt_rel_fwd", grid, 256, FwdShape<T, D, 4>::RING + table, a, st);
+        r = launch_rows<T, D, D == 64 ? 1 : 2, D == 64 ? 4 : 2>(a, causal, grid, table, st);
     if (r != HDT_OK || a.pieces == 1) return r;
     HdtTimer t("hdt_rel_join", st);
     const long long rows = bh * a.n_q * a.gp;
@@ -450,13 +489,19 @@ RelFwdPlan hdt_rel_fwd_plan(const hdt_rel_attn_t &d)
     long long pieces;
     if (rows <= 32) {
         p.waves = 0, p.tiles = 1;
-        // a workgroup takes about 1 us for 256 keys, a second kernel 4
-        pieces = d.n_kv <= 2048 ? 1 : std::min<long long>(1024 / heads, (d.n_kv + 1023) / 1024);
+        // Pieces of the keys in workgroups of their own, one a compute unit (its rings fill the LDS), and a second kernel that joins them:
+        // for keys whose walk takes longer than that, and where one workgroup a head leaves most units without work.  (us, heads of 64 x
+        // keys: one piece | these: 8 x 1000 8.7 | 9.8, 8 x 2000 11.8 | 10.1, 8 x 8192 30.2 | 10.9, 32 x 8192 30.8 | 17.7, 96 x 8192 34 | 37,
+        // 96 x 32768 205 | 142; 4 workgroups a unit instead of one: 256 x 8192 92 | 100.)
+        const bool few = heads <= 64 || d.n_kv > 16384;
+        pieces = (long long)d.n_kv * d.head_dim < 96 * 1024 || !few ? 1 : std::min<long long>(256 / heads, (d.n_kv + 511) / 512);
     } else {
-        const long long tiles = heads * ((rows + 127) / 128);
-        p.waves = tiles < 512 ? 2 : 4;  // tiles of 64 rows where 128 would leave compute units without work
+        p.waves = hdt_rel_row_waves(heads * ((rows + 127) / 128), heads * ((rows + 31) / 32), d);
         p.tiles = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
-        pieces = std::min<long long>(1024 / (heads * p.tiles), d.n_kv / 1024);
+        // a second kernel pays where workgroups are few: up to one a compute unit.  (us, bf16, heads x rows x keys of 64, 256 | 1024
+        // workgroups: 32 x 200 x 4096 25 | 45, 16 x 512 x 8192 43 | 63; pieces from 512 | 1024 keys: 1 x 64 x 1024 12.2 | 10.5,
+        // 1 x 200 x 4096 12.8 | 14.4, of 128 16.2 | 21.3)
+        pieces = d.n_kv < 2048 ? 1 : std::min<long long>(256 / (heads * p.tiles), d.n_kv / 512);
     }
     p.pieces = pieces < 1 ? 1 : (unsigned)pieces;
     const size_t all = (size_t)d.batch * d.heads * d.n_q;
