@@ -27,17 +27,17 @@ struct RelFwdPlan {
 RelFwdPlan hdt_rel_fwd_plan(const hdt_rel_attn_t &d);
 hdt_status_t hdt_launch_rel_fwd(const hdt_rel_attn_t &d, const RelFwdArgs &a, int waves, hipStream_t st);
 
-// Waves of 32 rows a workgroup's tile has: 4, or 2 or 1 whose workgroups divide the walk along the other side among groups of waves, where
-// more rows would leave compute units without work.  A unit holds two workgroups of 4 or 2 waves of 64 columns, and one otherwise: 4 from
-// 1.5 (of 128 columns: one) a unit on, 1 where they fit at once; in fp32, whose walk is bound by the matrix instructions, up to twice that.
+// Waves of 32 rows a workgroup's tile has: 4, or 2 or 1 whose workgroups divide the walk along the other side among groups of waves, which
+// is quicker for a tile, where all of them fit the card at once.  A compute unit holds two workgroups of 2 waves of 64 columns and one of
+// the others; in fp32, whose walk is bound by the matrix instructions, a second round of small tiles still pays.
 // (us, 4 | 2 | 1 waves.  Backward bf16, heads x rows of 64: 128 x 512 47.6 | 58.8 | 136, 64 x 512 35.8 | 36.1 | 71, 32 x 512 27.5 | 26.5 | 39.9,
 // 16 x 512 27.1 | 22.2 | 25.9, 8 x 512 26.7 | 22.4 | 19.3; of 128: 32 x 512 36.0 | 41.9, 16 x 512 34.5 | 29.2.  fp32 of 64: 64 x 512
 // 112 | 116 | 152, 32 x 512 88 | 64 | 82, 16 x 512 87 | 54 | 47.  Forward bf16 of 64: 128 x 512 13.8 | 18.1 | 51, 64 x 512 12.2 | 10.9 | 26,
 // 16 x 512 11.6 | 9.6 | 8.8.)
-inline int hdt_rel_row_waves(long long tiles128, long long tiles32, const hdt_rel_attn_t &d)
+inline int hdt_rel_row_waves(long long tiles64, long long tiles32, const hdt_rel_attn_t &d)
 {
-    if (tiles128 >= (d.head_dim == 64 ? 384 : 256)) return 4;
-    return tiles32 > (d.dtype == HDT_BF16 ? 256 : 512) || d.head_dim == 128 ? 2 : 1;
+    if (d.head_dim == 64 && tiles32 <= (d.dtype == HDT_BF16 ? 256 : 512)) return 1;
+    return tiles64 <= (d.head_dim == 64 ? 512 : 256) ? 2 : 4;
 }
 
 struct RelBwdArgs {

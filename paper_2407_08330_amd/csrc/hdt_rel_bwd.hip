@@ -551,7 +551,7 @@ RelBwdPlan hdt_rel_bwd_plan(const hdt_rel_attn_t &d)
 {
     RelBwdPlan p;
     auto tiles = [&](long long bm) { return d.batch * (d.heads * ((d.n_q + bm - 1) / bm) + d.kv_heads * ((d.n_kv + bm - 1) / bm)); };
-    p.waves = hdt_rel_row_waves(tiles(128), tiles(32), d);
+    p.waves = hdt_rel_row_waves(tiles(64), tiles(32), d);
     // (a ring for each group, the table, and a row of sums by distance for each half-wave have to fit a compute unit's LDS)
     const size_t ring = (size_t)4 * (d.dtype == HDT_BF16 ? 64 * 2 : 32 * 4) * d.head_dim, line = table_row(d.max_distance, d.causal != 0) * sizeof(float);
     while (p.waves < 4 && 4 / p.waves * ring + 9 * line > 160 * 1024) p.waves *= 2;
@@ -561,7 +561,7 @@ RelBwdPlan hdt_rel_bwd_plan(const hdt_rel_attn_t &d)
     p.n_pad = (d.n_q + 127) & ~127;
     const size_t rows = (size_t)d.batch * d.heads * p.n_pad;
     p.tables_at = (4 * rows * sizeof(float) + 255) & ~(size_t)255;
-    p.bins_at = p.tables_at + d.heads * line;
+    p.bins_at = p.tables_at + (rows ? d.heads * line : 0);
     p.bytes = p.bins_at + (size_t)d.heads * d.batch * p.tiles_q * line;
     return p;
 }

@@ -490,18 +490,19 @@ RelFwdPlan hdt_rel_fwd_plan(const hdt_rel_attn_t &d)
     if (rows <= 32) {
         p.waves = 0, p.tiles = 1;
         // Pieces of the keys in workgroups of their own, one a compute unit (its rings fill the LDS), and a second kernel that joins them:
-        // for keys whose walk takes longer than that, and where one workgroup a head leaves most units without work.  (us, heads of 64 x
-        // keys: one piece | these: 8 x 1000 8.7 | 9.8, 8 x 2000 11.8 | 10.1, 8 x 8192 30.2 | 10.9, 32 x 8192 30.8 | 17.7, 96 x 8192 34 | 37,
-        // 96 x 32768 205 | 142; 4 workgroups a unit instead of one: 256 x 8192 92 | 100.)
-        const bool few = heads <= 64 || d.n_kv > 16384;
-        pieces = (long long)d.n_kv * d.head_dim < 96 * 1024 || !few ? 1 : std::min<long long>(256 / heads, (d.n_kv + 511) / 512);
+        // for keys whose walk takes longer than that.  (us, one piece | these.  Heads of 64 x keys: 8 x 1000 8.7 | 9.8, 8 x 2000 11.8 | 10.1,
+        // 8 x 8192 30.2 | 10.9, 32 x 8192 30.8 | 17.7; of 128: 128 x 8192 86 | 66.  4 workgroups a unit instead of one: 256 x 8192 92 | 100.)
+        pieces = (long long)d.n_kv * d.head_dim < 96 * 1024 ? 1 : std::min<long long>(256 / heads, (d.n_kv + 511) / 512);
     } else {
-        p.waves = hdt_rel_row_waves(heads * ((rows + 127) / 128), heads * ((rows + 31) / 32), d);
+        // Keys many times the rows (a chunk behind a long cache): tiles of 128 rows and pieces; otherwise the tile that hdt_rel_row_waves()
+        // gives, and pieces only where that leaves units without work.  (us, such tiles | 64 rows: 48 heads x 200 rows x 4096 keys of 64 25 | 34,
+        // 96 x 200 x 4096 of 128 62 | 88, but 32 x 1000 x 2048 of 64 30 | 24; pieces from 512 | 1024 keys: 1 x 200 x 4096 12.8 | 14.4, of 128
+        // 16.2 | 21.3; up to 256 | 1024 workgroups: 16 x 512 x 8192 43 | 63.)
+        p.waves = hdt_rel_row_waves(heads * ((rows + 63) / 64), heads * ((rows + 31) / 32), d);
+        const bool chunk = rows > 64 && d.n_kv >= 8 * rows;
+        if (chunk && d.n_kv >= 2048) p.waves = 4;
         p.tiles = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
-        // a second kernel pays where workgroups are few: up to one a compute unit.  (us, bf16, heads x rows x keys of 64, 256 | 1024
-        // workgroups: 32 x 200 x 4096 25 | 45, 16 x 512 x 8192 43 | 63; pieces from 512 | 1024 keys: 1 x 64 x 1024 12.2 | 10.5,
-        // 1 x 200 x 4096 12.8 | 14.4, of 128 16.2 | 21.3)
-        pieces = d.n_kv < 2048 ? 1 : std::min<long long>(256 / (heads * p.tiles), d.n_kv / 512);
+        pieces = d.n_kv < 2048 ? 1 : std::min<long long>((!chunk ? 256 : d.head_dim == 64 ? 768 : 512) / (heads * p.tiles), d.n_kv / 512);
     }
     p.pieces = pieces < 1 ? 1 : (unsigned)pieces;
     const size_t all = (size_t)d.batch * d.heads * d.n_q;
