@@ -8,7 +8,9 @@
 // Philox4x32-10 (Salmon, Moraes, Dror and Shaw, SC 2011), 16 bits each; an element is kept iff its 16 bits are at least
 // t = round(65536 p), and what is kept is multiplied by 65536 / (65536 - t), the inverse of the probability that 16 bits really give.
 //
-// All of it is bound by memory: a row is read once, held in registers between its statistics and its result, and written once.
+// All of it is bound by memory: a row is read once, held in registers between its statistics and its result, and written once.  On 32768
+// bf16 rows of 768 columns: dropout with residual 26 us (151 MB, 5.7 TB/s), norm forward and backward 92 us (453 MB, 4.9 TB/s); a copy
+// of 200 MB reaches 5.4 TB/s, one of 2 GB 4.9.
 // Sums and statistics are in fp32; h is rounded once, when it is written (the norm is taken of the unrounded sum).
 #include <algorithm>
 
@@ -372,7 +374,8 @@ __global__ __launch_bounds__(kPartColumns * kPartRuns) void k_norm_parts(NormArg
 constexpr int kMostWidth = 32768, kMostParts = 512;
 constexpr long long kMostElements = 1ll << 35;  // 2^32 blocks of eight
 
-// threads a row and chunks a thread: a wave up to 2048 columns, then a workgroup of 256 or 1024
+// threads a row and chunks a thread: a wave up to 2048 columns, then a workgroup of 256 or 1024 (us at 32768 bf16 rows, wave | workgroup of
+// 256: 768 columns 36 | 91 forward, 48 | 93 backward; 2048 columns 99 | 129, 137 | 135; 4096 rows of 2048 14.7 | 17.7, 26 | 25)
 struct RowShape {
     int tpr, nch;
 };
@@ -384,7 +387,8 @@ RowShape row_shape(int width)
     if (chunks <= 256) return {64, 4};
     return chunks <= 1024 ? RowShape{256, 4} : RowShape{1024, 4};
 }
-// workgroups of the backward: two or more per compute unit, and no more sums to add up behind it than that takes
+// workgroups of the backward: two per compute unit, and no more sums to add up behind it than that takes (us at 32768 bf16 rows, 256 | 512 |
+// 1024 workgroups: 768 columns 46 | 48 | 54, 2048 columns 184 | 137 | 143)
 int norm_parts(int rows, int width)
 {
     const RowShape s = row_shape(width);

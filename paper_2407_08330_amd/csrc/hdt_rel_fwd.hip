@@ -1,9 +1,20 @@
 // Forward pass of self-attention with a relative position bias (hdt_rel.h has the mathematics and the block kinds).
 //
-// Work split: one workgroup per (sample, head block, tile of 128 rows, piece of the keys); wave w owns rows 32w .. 32w + 31 of the
-// tile.  Rows are the queries of one head, or, where a head has fewer queries than a tile has rows, the queries of all heads that
-// share a key head, so that the keys are read once for them (PACK: row r is query r / gp of head r % gp).  Key tiles of BN rows
-// go through a ring of two stages in LDS.
+// Work split: one workgroup per (sample, head block, tile of rows, piece of the keys); a wave owns 32 rows, whose S, P and O stay in its
+// registers: S^T = K Q^T leaves a row's pairs in one lane pair, so that the softmax needs one exchange a tile, and P^T is already the operand
+// of O^T += V^T P^T.  A tile is 128 rows of 4 waves, or 64 or 32 rows whose workgroup has as many waves, which take every second or fourth
+// key tile and join in LDS (hdt_rel_row_waves).  Rows are the queries of one head, or, where a head has fewer queries than a tile has rows,
+// the queries of all heads that share a key head, so that the keys are read once for them (row r is query r / gp of head r % gp).  Key tiles
+// of BN rows go through a ring of two stages in LDS, loaded directly.
+//
+// P is rounded to bf16 for its product with V (as the operand of the fast contraction has to be), after its sum is taken in fp32; the
+// reference of the exponentials follows the maximum only from a factor 2^8 on, which saves rescaling and costs nothing in fp32 or bf16.
+//
+// What bounds it: vector instructions (an exponential, a fused multiply-add, a sum, half a maximum and half a conversion for each pair) next
+// to the matrix ones.  24 heads x 8192 x 64, causal: 231 us, 0.89 PFLOP/s, vector pipe issuing 68 % and matrix pipe busy 41 % of all
+// clocks.  32 heads x 4096 x 128: 150 us, 0.91.  (Tried on the first: no maximum unless a row's sum is large, with the contraction taken
+// again then, 170 registers and a wave less a SIMD: 231 -> 243; sums by dot products of the rounded weights: 2 % quicker, but LSE then has
+// bf16's errors; more operands ahead, wave priorities around the contractions: within 1 %.)
 #include <algorithm>
 #include <type_traits>
 
@@ -208,7 +219,8 @@ __global__ __launch_bounds__(NW_ * KS_ * 64, sizeof(T) == 4 && D == 128 ? 1 : 2)
 
 // Few rows (at most 32 in a head block: new tokens): the waves of a workgroup divide the keys instead of the rows.  Each walks blocks of
 // 32 keys through a ring of its own (no barriers; two blocks in flight a wave, 64 KB a workgroup, which the stream from memory
-// wants) and they join what they have in LDS.
+// wants) and they join what they have in LDS.  Bound by reading K and V once: 32 x 4 key heads of 128, 8192 ragged keys (403 MB), 80 us and
+// 4 for joining the pieces, 4.8 TB/s.  One token over 1000 keys of 12 heads: 8 us, a launch and the latency of four dependent loads.
 template <typename T, int D>
 struct FewShape {
     static constexpr int ROWB = Rows<T, D>::ROWB, NW = 1024 / ROWB, NI = 32 * ROWB / 1024;
