@@ -532,6 +532,7 @@ def hdt_rel_table(n_buckets: int, max_distance: int, both_ways: bool = False, de
     not causal."""
     import torch
     table = torch.empty(2 * max(int(max_distance), 0) + 1, dtype=torch.int32, device=device)
+    _same_device((table,))
     _check(load_library().hdt_rel_table(int(n_buckets), int(max_distance), int(both_ways), _ptr(table), _stream_ptr(stream)))
     return table
 

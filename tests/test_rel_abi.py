@@ -139,3 +139,21 @@ def test_norm_refuses(lib):
                dict(dx=136), dict(rows=-1)):
         assert g(**kw) == INVALID, kw
     assert g(width=0) == SHAPE and g(dt=4) == UNSUPPORTED
+
+
+def test_binding_refuses_host_tensors():
+    """What would hand a host address to a kernel is an error before the call."""
+    import torch
+    import paper_2407_08330_amd as hdt
+    with pytest.raises(ValueError):
+        hdt.hdt_rel_table(32, 128, device="cpu")
+    q, table, bias = torch.zeros(1, 1, 4, 64), torch.zeros(257, dtype=torch.int32), torch.zeros(32, 1)
+    with pytest.raises(ValueError):
+        hdt.hdt_rel_attn_fwd(q, q, q, bias, table, 1.0)
+    with pytest.raises(ValueError):
+        hdt.hdt_rel_attn_bwd(q, q, q, bias, table, q, torch.zeros(1, 1, 4), q, 1.0)
+    x, w, rng = torch.zeros(2, 8), torch.zeros(8), torch.zeros(2, dtype=torch.int64)
+    for call in (lambda: hdt.hdt_dropout_add(x, 0.1, rng), lambda: hdt.hdt_add_norm_fwd(x, w, w),
+                 lambda: hdt.hdt_add_norm_bwd(x, x, w, torch.zeros(2), torch.zeros(2))):
+        with pytest.raises(ValueError):
+            call()
