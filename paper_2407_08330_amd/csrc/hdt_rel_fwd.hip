@@ -218,15 +218,19 @@ __global__ __launch_bounds__(NW_ * KS_ * 64, sizeof(T) == 4 && D == 128 ? 1 : 2)
 }
 
 // Few rows (at most 32 in a head block: new tokens): the waves of a workgroup divide the keys instead of the rows.  Each walks blocks of
-// 32 keys through a ring of its own (no barriers; two blocks in flight a wave, 64 KB a workgroup, which the stream from memory
-// wants) and they join what they have in LDS.  Bound by reading K and V once: 32 x 4 key heads of 128, 8192 ragged keys (403 MB), 80 us and
-// 4 for joining the pieces, 4.8 TB/s.  One token over 1000 keys of 12 heads: 8 us, a launch and the latency of four dependent loads.
+// 32 keys through a ring of its own (no barriers; 128 KB of blocks in flight a workgroup, which the stream from memory wants) and they join
+// what they have in LDS.  8 waves with two blocks of 128-byte rows each, or one of 256: those take turns (us, rows of 256 bytes, 4 waves of
+// two | 8 of one: 1000 keys of 1 head 14.2 | 12.3, 8192 keys of 256 186 | 186; rows of 128, 8 of two | 16 of one: 8.2 | 8.4, 92 | 95).
+// Bound by reading K and V once: 32 x 4 key heads of 128, 8192 ragged keys (403 MB), 80 us and 4 for joining the pieces, 4.8 TB/s.  One
+// token over 1000 keys of 12 heads of 64: 8 us: arguments and lengths 1.2, bias by distance and first keys 1.5, four blocks a wave 2.6,
+// the join 1.9.
 template <typename T, int D>
 struct FewShape {
-    static constexpr int ROWB = Rows<T, D>::ROWB, NW = 1024 / ROWB, NI = 32 * ROWB / 1024;
-    static constexpr int TILE = 32 * ROWB, STAGE = 2 * TILE, RING = NW * 2 * STAGE;  // 128 KB
-    static constexpr int OROW = D + 4;                                               // floats of a row of partial O in LDS
-    static_assert(NW * 32 * (OROW + 2) * 4 <= RING, "the partial results fit the rings");
+    static constexpr int ROWB = Rows<T, D>::ROWB, NI = 32 * ROWB / 1024, TILE = 32 * ROWB, STAGE = 2 * TILE;
+    static constexpr int NW = ROWB <= 256 ? 8 : 4, STAGES = 128 * 1024 / (NW * STAGE), RING = STAGES * STAGE;
+    static_assert(STAGES == 1 || STAGES == 2, "as the kernel's waits count");
+    static_assert(NW * 32 * (D + 2) * 4 <= NW * RING + 8192, "the waves' references, sums and O fit");
+    static constexpr int LDS = NW * RING + 8192;
 };
 
 template <typename T, int D, bool CAUSAL>
@@ -236,7 +240,7 @@ __global__ __launch_bounds__((FewShape<T, D>::NW * 64)) void k_rel_few(RelFwdArg
     using RowsT = Rows<T, D>;
     constexpr int NW = S::NW, NI = S::NI;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    float *const tab = reinterpret_cast<float *>(smem + S::RING);
+    float *const tab = reinterpret_cast<float *>(smem + S::LDS);
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5;
     const unsigned heads = (unsigned)(a.batch * a.head_blocks), piece = blockIdx.x / heads;
@@ -266,12 +270,12 @@ __global__ __launch_bounds__((FewShape<T, D>::NW * 64)) void k_rel_few(RelFwdArg
         const char *kb = (const char *)((const T *)a.k + (size_t)b * a.sk.batch + kvh * a.sk.head);
         const char *vb = (const char *)((const T *)a.v + (size_t)b * a.sv.batch + kvh * a.sv.head);
         const uint32_t krow = (uint32_t)a.sk.row * sizeof(T), vrow = (uint32_t)a.sv.row * sizeof(T);
-        const char *const mine = smem + wave * 2 * S::STAGE;
+        const char *const mine = smem + wave * S::RING;
         const uint32_t lds = lds_addr(mine);
         auto request = [&](int blk, int stage) {
+            const uint32_t at = lds + (uint32_t)(stage * S::STAGE);
             const char *pk = kb + (size_t)blk * 32 * krow, *pv = vb + (size_t)blk * 32 * vrow;
             const int left = seen - 1 - blk * 32, c = lane % RowsT::CPR;
-            const uint32_t at = lds + (uint32_t)(stage * S::STAGE);
 #pragma unroll
             for (int i = 0; i < NI; i++) {
                 const int r = i * RowsT::RPI + lane / RowsT::CPR;
@@ -296,12 +300,20 @@ __global__ __launch_bounds__((FewShape<T, D>::NW * 64)) void k_rel_few(RelFwdArg
         const float c_behind = tab[g * len] * a.scale_log2, c_ahead = CAUSAL ? 0.f : tab[g * len + len - 1] * a.scale_log2;
 
         int stage = 0;
-        for (int blk = block0 + wave; blk < block1; blk += NW, stage ^= 1) {
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the block before last has been read)
-            if (blk + NW < block1) {
-                request(blk + NW, stage ^ 1);
-                wait_vmcnt<2 * NI>();
+        for (int blk = block0 + wave; blk < block1; blk += NW, stage ^= S::STAGES - 1) {
+            if (S::STAGES == 2) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the block before last has been read)
+                if (blk + NW < block1) {
+                    request(blk + NW, stage ^ 1);
+                    wait_vmcnt<2 * NI>();
+                } else {
+                    wait_vmcnt<0>();
+                }
             } else {
+                if (blk != block0 + wave) {
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the block before has been read)
+                    request(blk, 0);
+                }
                 wait_vmcnt<0>();
             }
             const char *sK = mine + stage * S::STAGE, *sV = sK + S::TILE;
@@ -353,18 +365,18 @@ __global__ __launch_bounds__((FewShape<T, D>::NW * 64)) void k_rel_few(RelFwdArg
         }
     }
 
-    // the waves' results: references and sums [wave][32], O [wave][row][OROW], in their order
+    // the waves' results: references and sums [wave][32], O [wave][row][D], chunk c of four at c ^ (row & 15); joined in their order
     float *const ms = reinterpret_cast<float *>(smem), *const ls = ms + NW * 32, *const os = ls + NW * 32;
     const float l_tot = sum_halves(l_part);
     __syncthreads();
     if (hf == 0) ms[wave * 32 + row] = m_ref, ls[wave * 32 + row] = l_tot;
     if (row < n_rows) {
-        float *const o = os + (wave * 32 + row) * S::OROW + 4 * hf;
+        float *const o = os + (wave * 32 + row) * D;
 #pragma unroll
         for (int j = 0; j < RowsT::BLOCKS; j++)
 #pragma unroll
             for (int q4 = 0; q4 < 4; q4++)
-                *reinterpret_cast<f32x4 *>(o + 32 * j + 8 * q4) = f32x4{acc[j][4 * q4], acc[j][4 * q4 + 1], acc[j][4 * q4 + 2], acc[j][4 * q4 + 3]};
+                *reinterpret_cast<f32x4 *>(o + (((8 * j + 2 * q4 + hf) ^ (row & 15)) << 2)) = f32x4{acc[j][4 * q4], acc[j][4 * q4 + 1], acc[j][4 * q4 + 2], acc[j][4 * q4 + 3]};
     }
     __syncthreads();
     for (int x = tid; x < n_rows * (D / 4); x += NW * 64) {
@@ -377,7 +389,7 @@ __global__ __launch_bounds__((FewShape<T, D>::NW * 64)) void k_rel_few(RelFwdArg
 #pragma unroll
         for (int w = 0; w < NW; w++) {
             const float m = ms[w * 32 + r], weight = m == -INFINITY ? 0.f : fast_exp2(m - top);
-            const f32x4 y = *reinterpret_cast<const f32x4 *>(os + (w * 32 + r) * S::OROW + 4 * c);
+            const f32x4 y = *reinterpret_cast<const f32x4 *>(os + (w * 32 + r) * D + ((c ^ (r & 15)) << 2));
             sum = fmaf(weight, ls[w * 32 + r], sum);
 #pragma unroll
             for (int e = 0; e < 4; e++) o[e] = fmaf(weight, y[e], o[e]);
@@ -471,7 +483,7 @@ hdt_status_t launch(const RelFwdArgs &a, int waves, bool causal, hipStream_t st)
     hdt_status_t r;
     if (waves == 0)
         r = launch_kernel(causal ? k_rel_few<T, D, true> : k_rel_few<T, D, false>, "hdt_rel_few", grid, FewShape<T, D>::NW * 64,
-                          FewShape<T, D>::RING + table, a, st);
+                          FewShape<T, D>::LDS + table, a, st);
     else if (waves == 4)
         r = launch_rows<T, D, 4, 1>(a, causal, grid, table, st);
     else if (waves == 2)
