@@ -375,3 +375,24 @@ def test_a_cache_beyond_32_bit_offsets():
     assert bool(((o[-1].double() - want).abs() <= most).all())
     assert float((lse[-1].double() - torch.logsumexp(a, -1)).abs().max()) <= 1e-5 * 20
     assert bool((o[1:-1] == 0).all()) and bool(torch.isneginf(lse[1:-1]).all())
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("B,H,KV", [(10, 6, 3), (11, 10, 10), (25, 7, 7)])
+def test_many_heads(B, H, KV, dtype, D, causal):
+    """60, 110 and 175 heads of 140 rows: the tile shapes that calls take as their heads become many (tiles of 32, 64 and 128 rows in the
+    forward, 64 and 128 in the backward)."""
+    say(f"[rel] {B} x {H}/{KV} heads x 140 {dtype} d={D} causal={causal}")
+    lengths = [140 - 9 * b % 141 for b in range(B)]
+    Problem(B, H, KV, 140, 140, D, dtype=dtype, causal=causal, lengths=lengths, distance=20, poison=True).check()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("B,H,KV,nq,nk,lengths", [(2, 2, 2, 100, 2200, [2200, 700]), (1, 3, 3, 40, 2100, None), (2, 4, 2, 150, 2049, [2049, 149]),
+                                                  (1, 1, 1, 2100, 2100, None), (1, 30, 1, 9, 2500, None)])
+def test_pieces_of_the_keys(B, H, KV, nq, nk, lengths, dtype, D, causal):
+    """Many keys, few rows or heads: the keys divided among workgroups, some of which may have none, in every tile shape that does so."""
+    say(f"[rel] {B} x {H}/{KV} heads x {nq} of {nk} {dtype} d={D} causal={causal}")
+    Problem(B, H, KV, nq, nk, D, dtype=dtype, causal=causal, lengths=lengths, starts=[n - nq for n in (lengths or [nk] * B)], poison=True).check(backward=nq < 200)
