@@ -14,7 +14,8 @@
 // to the matrix ones.  24 heads x 8192 x 64, causal: 231 us, 0.89 PFLOP/s, vector pipe issuing 68 % and matrix pipe busy 41 % of all
 // clocks.  32 heads x 4096 x 128: 150 us, 0.91.  (Tried on the first: no maximum unless a row's sum is large, with the contraction taken
 // again then, 170 registers and a wave less a SIMD: 231 -> 243; sums by dot products of the rounded weights: 2 % quicker, but LSE then has
-// bf16's errors; more operands ahead, wave priorities around the contractions: within 1 %.)
+// bf16's errors; two blocks of rows a wave, which share the operands from LDS,
+// at two waves a SIMD: 241 -> 257; more operands ahead, wave priorities around the contractions: within 1 %.)
 #include <algorithm>
 #include <type_traits>
 
