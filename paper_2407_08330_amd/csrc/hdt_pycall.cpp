@@ -386,7 +386,7 @@ PyObject *rel_attn_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
             (g[1] && !strides_of(*g[1], ks, type, &r.c.dk)) || (g[2] && !strides_of(*g[2], ks, type, &r.c.dv)) || (g[3] && !like(*g[3], *r.bias)))
             return nullptr;
         at::Tensor dq = g[0] ? *g[0] : at::empty(qs, r.q->options()), dk = g[1] ? *g[1] : at::empty(ks, r.q->options());
-        at::Tensor dv = g[2] ? *g[2] : at::empty(ks, r.q->options()), db = g[3] ? *g[3] : at::empty_like(*r.bias);
+        at::Tensor dv = g[2] ? *g[2] : at::empty(ks, r.q->options()), db = g[3] ? *g[3] : at::empty(r.bias->sizes(), r.bias->options());
         const Room w(a[16], rel_bwd_bytes_fn(&r.c), *r.q);
         const void *pq = r.q->data_ptr(), *pk = r.k->data_ptr(), *pv = r.v->data_ptr(), *po = o->data_ptr(), *pd = d_o->data_ptr();
         const float *pl = (const float *)lse->data_ptr();
@@ -427,7 +427,7 @@ PyObject *dropout_add(PyObject *, PyObject *const *a, Py_ssize_t n)
             !site_of(a[3], &site) || !optional(a[4], device, &x) || !optional(a[5], device, &given) || !stream_of(a[6], &st))
             return nullptr;
         if ((x && !like(*x, *y)) || (given && !like(*given, *y))) return nullptr;
-        at::Tensor out = given ? *given : at::empty_like(*y);
+        at::Tensor out = given ? *given : at::empty(y->sizes(), y->options());
         const void *py = y->data_ptr(), *px = data(x);
         const int64_t *pr = (const int64_t *)data(rng);
         void *po = out.data_ptr();
@@ -480,7 +480,7 @@ PyObject *add_norm_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
             (g[2] && !c.statistic(*g[2])) || (g[3] && !c.statistic(*g[3])))
             return nullptr;
         const auto lead = c.x->sizes().slice(0, c.x->dim() - 1);
-        at::Tensor h = g[0] ? *g[0] : at::empty_like(*c.x), out = g[1] ? *g[1] : at::empty_like(*c.x);
+        at::Tensor h = g[0] ? *g[0] : at::empty(c.x->sizes(), c.x->options()), out = g[1] ? *g[1] : at::empty(c.x->sizes(), c.x->options());
         at::Tensor mean = g[2] ? *g[2] : at::empty(lead, c.x->options().dtype(at::kFloat)), rstd = g[3] ? *g[3] : at::empty(lead, c.x->options().dtype(at::kFloat));
         const void *px = c.x->data_ptr(), *py = y->data_ptr(), *pw = c.weight->data_ptr(), *pb = data(bias);
         const int64_t *pr = (const int64_t *)data(rng);
@@ -511,8 +511,8 @@ PyObject *add_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
             return nullptr;
         for (int i = 0; i < 4; i++)
             if (!optional(a[10 + i], c.device, &g[i]) || (g[i] && !like(*g[i], i < 2 ? *c.x : *c.weight))) return nullptr;
-        at::Tensor dx = g[0] ? *g[0] : at::empty_like(*c.x), dy = g[1] ? *g[1] : at::empty_like(*c.x);
-        at::Tensor dw = g[2] ? *g[2] : at::empty_like(*c.weight), db = g[3] ? *g[3] : at::empty_like(*c.weight);
+        at::Tensor dx = g[0] ? *g[0] : at::empty(c.x->sizes(), c.x->options()), dy = g[1] ? *g[1] : at::empty(c.x->sizes(), c.x->options());
+        at::Tensor dw = g[2] ? *g[2] : at::empty(c.weight->sizes(), c.weight->options()), db = g[3] ? *g[3] : at::empty(c.weight->sizes(), c.weight->options());
         const Room w(a[14], norm_bwd_bytes_fn(c.rows, c.width), *c.x);
         const void *pn = dn->data_ptr(), *pd = data(dh), *ph = c.x->data_ptr(), *pw = c.weight->data_ptr();
         const float *pm = (const float *)mean->data_ptr(), *ps = (const float *)rstd->data_ptr();
