@@ -40,14 +40,12 @@ template <>
 struct Op<__bf16> {
     typedef bf16x8 Frag;
     static constexpr int PER_STEP = 16;  // values of the contraction a step covers
-    static __device__ __forceinline__ Frag zero() { return zero_bf16x8(); }
     static __device__ __forceinline__ f32x16 mma(Frag a, Frag b, f32x16 c) { return mfma_32x32x16(a, b, c); }
 };
 template <>
 struct Op<float> {
     typedef f32x4 Frag;
     static constexpr int PER_STEP = 8;
-    static __device__ __forceinline__ Frag zero() { return f32x4{0.f, 0.f, 0.f, 0.f}; }
     static __device__ __forceinline__ f32x16 mma(Frag a, Frag b, f32x16 c)
     {
 #pragma unroll

@@ -396,3 +396,12 @@ def test_pieces_of_the_keys(B, H, KV, nq, nk, lengths, dtype, D, causal):
     """Many keys, few rows or heads: the keys divided among workgroups, some of which may have none, in every tile shape that does so."""
     say(f"[rel] {B} x {H}/{KV} heads x {nq} of {nk} {dtype} d={D} causal={causal}")
     Problem(B, H, KV, nq, nk, D, dtype=dtype, causal=causal, lengths=lengths, starts=[n - nq for n in (lengths or [nk] * B)], poison=True).check(backward=nq < 200)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("H,nq,distance", [(16, 1, 128), (16, 1, 127), (17, 1, 128), (16, 9, 128), (2, 1, 1024), (2, 140, 1024)])
+def test_tables_that_fill_the_lds(H, nq, distance, dtype, D, causal):
+    """Query heads of one key head, each with its bias by distance in LDS beside the rings: up to the last bytes there are, and beyond."""
+    say(f"[rel] {H}/1 heads x {nq} of 300, distances up to {distance}, {dtype} d={D} causal={causal}")
+    Problem(2, H, 1, nq, 300, D, dtype=dtype, causal=causal, lengths=[300, 150], starts=[300 - nq, 150 - nq], distance=distance, poison=True).check()
