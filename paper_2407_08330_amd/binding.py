@@ -568,6 +568,8 @@ def _rel_attn_call(q, k, v, bias, table, softmax_scale, causal, lengths, q_start
             raise ValueError(f"{name} must be {tuple(shape)} of {q.dtype}")
         if t.stride(3) != 1 and t.numel() > 0:
             raise ValueError(f"{name}: the values of a row must be consecutive")
+        if shape[2] > 1 and t.numel() > 0 and t.stride(2) < D:  # (one row expanded over all three would be described as dense)
+            raise ValueError(f"{name}: rows must not overlap (row stride {t.stride(2)}, rows of {D})")
         if not t.is_contiguous():  # (a stride of a dimension of one element says nothing)
             dense = (shape[1] * shape[2] * D, shape[2] * D, D)
             setattr(c, name, _Strides(*(t.stride(i) if shape[i] > 1 else dense[i] for i in range(3))))

@@ -280,8 +280,8 @@ bool strides_of(const at::Tensor &t, at::IntArrayRef shape, at::ScalarType type,
 {
     if (t.scalar_type() != type || t.sizes() != shape) return false;
     if (t.is_contiguous()) return true;
-    if (t.stride(3) != 1) return false;
     const int64_t d = shape[3], n = shape[2], h = shape[1];
+    if (t.stride(3) != 1 || (n > 1 && t.stride(2) < d)) return false;  // (one row expanded over all three would be described as dense)
     s->batch = shape[0] > 1 ? t.stride(0) : h * n * d;
     s->head = h > 1 ? t.stride(1) : n * d;
     s->row = n > 1 ? t.stride(2) : d;
