@@ -22,7 +22,8 @@ HIPCC_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     # no NaN-quieting v_max(x, x) in front of every fmaxf: wherever a NaN can stand (rows of pad positions may
     # hold anything) it is removed by a select before any arithmetic looks at it, and the kernels produce none
-    # on their own (infinities are still honoured)
+    # on their own (infinities are still honoured).  A NaN of a real row goes through the arithmetic as it does anyway;
+    # no branch or select may ask for one but by its bits, behind an empty asm (hdt_rel.h: no_weight, minus_infinity)
     "-fno-honor-nans",
     "-Wno-unused-command-line-argument",
     # the direct-to-LDS loads set M0 inside their asm block and list it as clobbered

@@ -240,6 +240,11 @@ __device__ __forceinline__ void store_rows(char *wave_lds, int lane, const f32x1
     }
 }
 
+// By their bits, which the compiler cannot see through: the sources are compiled on the assumption that no value is a NaN
+// (-fno-honor-nans), and a real row of the caller's may make one.  Nothing but zero weights, so that a row has no key; a NaN sum is not that.
+__device__ __forceinline__ bool no_weight(float sum) { return hidden(__builtin_bit_cast(unsigned, sum)) << 1 == 0; }
+__device__ __forceinline__ bool minus_infinity(float x) { return hidden(__builtin_bit_cast(unsigned, x)) == 0xff800000u; }
+
 // The rows of a sample that stand for positions, and its keys
 struct Sample {
     int start, length;  // position of query 0; keys

@@ -66,7 +66,7 @@ __global__ __launch_bounds__(256) void k_rel_rows(RelBwdArgs a, long long rows, 
         if (c != 0 || r >= rows) continue;
         const int b = bh[u] / a.heads, h = bh[u] - b * a.heads;
         const Sample smp = sample_of(a.lengths, a.starts, b, a.n_q, a.n_kv);
-        const bool dead = ri[u] < smp.lo || ri[u] >= smp.hi || lse[u] == -INFINITY;
+        const bool dead = ri[u] < smp.lo || ri[u] >= smp.hi || minus_infinity(lse[u]);
         const float n = dead ? -INFINITY : -lse[u] * a.bias.inv_scale;
         a.row_scalars[r] = n;
         a.row_scalars[rows + r] = dead ? 0.f : -d;

@@ -192,13 +192,13 @@ __global__ __launch_bounds__(NW_ * KS_ * 64, sizeof(T) == 4 && D == 128 ? 1 : 2)
     char *const out_lds = smem + (KS - 1) * NW * (16 * RowsT::BLOCKS + 2) * 256 + wave * 32 * D * 4;
     static_assert((KS - 1) * NW * (16 * RowsT::BLOCKS + 2) * 256 + NW * 32 * D * 4 <= KS * S::RING, "they fit the rings");
     const float l_tot = sum_halves(l_part);
-    const float inv = real && l_tot > 0.f ? 1.f / l_tot : 0.f;
-    const float lse = real && l_tot > 0.f ? (m_ref + __builtin_amdgcn_logf(l_tot)) * LN2 : -INFINITY;
+    const bool any = real && !no_weight(l_tot);  // (a NaN in the row or in a key it sees: O and LSE are NaN)
+    const float inv = 1.f / l_tot, lse = any ? (m_ref + __builtin_amdgcn_logf(l_tot)) * LN2 : -INFINITY;
     const int oi = row / gp, og = row - oi * gp, head = hb * gp + og;
     if (a.pieces > 1) {
         if (KS == 1) __syncthreads();  // (the ring is free)
         const size_t at = (size_t)bh * n_rows + r0 + wave * 32;
-        store_rows<float, D>(out_lds, lane, acc, real, inv, a.part_o + (at * a.pieces + piece) * D, (int64_t)a.pieces * D, n_rows - r0 - wave * 32);
+        store_rows<float, D>(out_lds, lane, acc, any, inv, a.part_o + (at * a.pieces + piece) * D, (int64_t)a.pieces * D, n_rows - r0 - wave * 32);
         if (own && hf == 0) a.part_lse[(at + (lane & 31)) * a.pieces + piece] = lse;
         return;
     }
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(NW_ * KS_ * 64, sizeof(T) == 4 && D == 128 ? 1 : 2)
     T *const o = (T *)a.o + (size_t)b * a.so.batch;
     if (gp == 1) {
         if (KS == 1) __syncthreads();
-        store_rows<T, D>(out_lds, lane, acc, real, inv, o + (size_t)hb * a.so.head + (size_t)(r0 + wave * 32) * a.so.row, a.so.row, n_rows - r0 - wave * 32);
+        store_rows<T, D>(out_lds, lane, acc, any, inv, o + (size_t)hb * a.so.head + (size_t)(r0 + wave * 32) * a.so.row, a.so.row, n_rows - r0 - wave * 32);
         return;
     }
     if (!own) return;
@@ -215,7 +215,8 @@ __global__ __launch_bounds__(NW_ * KS_ * 64, sizeof(T) == 4 && D == 128 ? 1 : 2)
     for (int j = 0; j < RowsT::BLOCKS; j++)
 #pragma unroll
         for (int q4 = 0; q4 < 4; q4++)
-            store4(to + 32 * j + 8 * q4 + 4 * hf, acc[j][q4 * 4] * inv, acc[j][q4 * 4 + 1] * inv, acc[j][q4 * 4 + 2] * inv, acc[j][q4 * 4 + 3] * inv);
+            store4(to + 32 * j + 8 * q4 + 4 * hf, any ? acc[j][q4 * 4] * inv : 0.f, any ? acc[j][q4 * 4 + 1] * inv : 0.f,
+                   any ? acc[j][q4 * 4 + 2] * inv : 0.f, any ? acc[j][q4 * 4 + 3] * inv : 0.f);
 }
 
 // Few rows (at most 32 in a head block: new tokens): the waves of a workgroup divide the keys instead of the rows.  Each walks blocks of
@@ -395,15 +396,17 @@ __global__ __launch_bounds__((FewShape<T, D>::NW * 64)) void k_rel_few(RelFwdArg
 #pragma unroll
             for (int e = 0; e < 4; e++) o[e] = fmaf(weight, y[e], o[e]);
         }
-        const bool any = r >= first && r <= last && sum > 0.f;
-        const float inv = any ? 1.f / sum : 0.f, lse = any ? (top + __builtin_amdgcn_logf(sum)) * LN2 : -INFINITY;
+        const bool any = r >= first && r <= last && !no_weight(sum);
+        const float inv = 1.f / sum, lse = any ? (top + __builtin_amdgcn_logf(sum)) * LN2 : -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 4; e++) o[e] = any ? o[e] * inv : 0.f;
         const int i = r / gp, head = hb * gp + r - i * gp;
         if (a.pieces > 1) {
             const size_t at = ((size_t)bh * n_rows + r) * a.pieces + piece;
-            *reinterpret_cast<f32x4 *>(a.part_o + at * D + 4 * c) = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+            *reinterpret_cast<f32x4 *>(a.part_o + at * D + 4 * c) = o;
             if (c == 0) a.part_lse[at] = lse;
         } else {
-            store4((T *)a.o + (size_t)b * a.so.batch + (size_t)head * a.so.head + (size_t)i * a.so.row + 4 * c, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+            store4((T *)a.o + (size_t)b * a.so.batch + (size_t)head * a.so.head + (size_t)i * a.so.row + 4 * c, o[0], o[1], o[2], o[3]);
             if (c == 0) a.lse[((size_t)b * a.heads + head) * a.n_q + i] = lse;
         }
     }
@@ -425,6 +428,7 @@ __global__ __launch_bounds__(256) void k_rel_join(RelFwdArgs a, long long rows)
     for (int p0 = 0; p0 < pieces; p0 += U) {
         f32x4 x[U];
         float l[U], most = top;
+        bool any = false;
 #pragma unroll
         for (int u = 0; u < U; u++) {
             const int p = min(p0 + u, pieces - 1);
@@ -434,9 +438,10 @@ __global__ __launch_bounds__(256) void k_rel_join(RelFwdArgs a, long long rows)
 #pragma unroll
         for (int u = 0; u < U; u++) {
             if (p0 + u >= pieces) l[u] = -INFINITY;
-            most = fmaxf(most, l[u]);
+            most = fmaxf(most, l[u]);  // (passes over a NaN; what is made of it below is one)
+            any |= !minus_infinity(l[u]);
         }
-        if (most == -INFINITY) continue;
+        if (!any) continue;
         const float old = fast_exp2((top - most) * LOG2E);  // (nothing so far: 0)
         sum *= old;
 #pragma unroll
@@ -450,12 +455,14 @@ __global__ __launch_bounds__(256) void k_rel_join(RelFwdArgs a, long long rows)
             for (int e = 0; e < 4; e++) acc[e] = fmaf(w, x[u][e], acc[e]);
         }
     }
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    const bool any = !no_weight(sum);
+    const float inv = 1.f / sum;
+#pragma unroll
+    for (int e = 0; e < 4; e++) acc[e] = any ? acc[e] * inv : 0.f;
     const int bh = (int)(r / n_rows), row = (int)(r - (long long)bh * n_rows), b = bh / a.head_blocks, hb = bh - b * a.head_blocks;
     const int i = row / a.gp, head = hb * a.gp + row - i * a.gp;
-    store4((T *)a.o + (size_t)b * a.so.batch + (size_t)head * a.so.head + (size_t)i * a.so.row + 4 * c, acc[0] * inv, acc[1] * inv,
-           acc[2] * inv, acc[3] * inv);
-    if (c == 0) a.lse[((size_t)b * a.heads + head) * a.n_q + i] = sum > 0.f ? top + __builtin_amdgcn_logf(sum) * LN2 : -INFINITY;
+    store4((T *)a.o + (size_t)b * a.so.batch + (size_t)head * a.so.head + (size_t)i * a.so.row + 4 * c, acc[0], acc[1], acc[2], acc[3]);
+    if (c == 0) a.lse[((size_t)b * a.heads + head) * a.n_q + i] = any ? top + __builtin_amdgcn_logf(sum) * LN2 : -INFINITY;
 }
 
 template <typename K>
