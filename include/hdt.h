@@ -386,7 +386,8 @@ hdt_status_t hdt_hpe_add(const int32_t *d_p, int32_t batch, int32_t n_pos, int32
  *   heads, kv_heads   kv_heads divides heads: key head g serves the heads [g heads / kv_heads, (g + 1) heads / kv_heads), and
  *                     dk, dv are the sums over them
  *   d_bias            device, [n_buckets][heads], bias_dtype.  Values from -1e6 down (-inf, the type's lowest) hide a bucket: its pairs
- *                     are not visible, and a query that sees nothing else has O = 0, LSE = -inf; values from 1e6 up count as 1e6
+ *                     are not visible, and a query that sees nothing else has O = 0, LSE = -inf; values from 1e6 up count as 1e6,
+ *                     and a NaN makes the rows that see its bucket NaN
  *   d_table           device, int32 [2 max_distance + 1], of hdt_rel_table or the caller's own; entries outside [0, n_buckets)
  *                     count as the nearest one inside; max_distance 1 .. 1024, n_buckets 1 .. 4096
  *   d_lengths, d_q_start  device, int32 [batch], or NULL (n_kv; 0).  Read by the kernels: they may change between replays of a

@@ -282,7 +282,10 @@ __device__ __forceinline__ float bias_at(const BiasArgs &a, int bucket, int head
     const float x = a.bf16 ? (float)((const __bf16 *)a.bias)[at] : ((const float *)a.bias)[at];
     // Values that stand for a mask are one (kHidden): a row that saw nothing else would have an LSE next to them, in whose fp32 the
     // logarithm of its sum is lost, and with it the row's gradients.
-    return x <= -kHidden ? -INFINITY : fminf(x, kHidden) * a.inv_scale;
+    // (a NaN is kept, told by its bits: the smaller of it and kHidden would be kHidden)
+    const unsigned bits = hidden(__builtin_bit_cast(unsigned, x));
+    const float y = x <= -kHidden ? -INFINITY : fminf(x, kHidden) * a.inv_scale;
+    return __builtin_bit_cast(float, bits << 1 > 0xff000000u ? bits : __builtin_bit_cast(unsigned, y));
 }
 __device__ __forceinline__ float bias_of(const BiasArgs &a, int distance, int head) { return bias_at(a, bucket_of(a, distance), head); }
 __device__ __forceinline__ void fill_table(float *to, const BiasArgs &a, int h0, int heads, bool causal, int tid, int threads)
