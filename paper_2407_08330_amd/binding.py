@@ -645,6 +645,13 @@ def _check_rng(rng, p):
         raise ValueError("rng must be an int64 device tensor (seed, step)")
 
 
+def _check_site(site):
+    site = int(site)
+    if not 0 <= site < 1 << 32:  # (ctypes would cut it, and two calls would drop the same elements)
+        raise ValueError(f"site {site} is outside [0, 2^32)")
+    return site
+
+
 def _check_like(t, ts):
     for x in ts:
         if x is not None and (x.shape != t.shape or x.dtype != t.dtype or not (x.is_cuda and x.is_contiguous())):
@@ -653,7 +660,7 @@ def _check_like(t, ts):
 
 def hdt_dropout_add(y, p: float, rng=None, site: int = 0, x=None, out=None, stream=None):
     """x + dropout(y) (x = None: dropout alone; on a gradient: its backward).  ``rng``: int64 device tensor (seed, step); ``site``: which
-    of the calls with that seed and step.  ``out`` may be x or y.  Returns out."""
+    of the calls with that seed and step, a number of 32 bits.  ``out`` may be x or y.  Returns out."""
     if _lib is None:
         load_library()
     r = _calls.dropout_add(y, p, rng, site, x, out, None if stream is None else stream.cuda_stream)
@@ -662,11 +669,12 @@ def hdt_dropout_add(y, p: float, rng=None, site: int = 0, x=None, out=None, stre
             return r
         _check(r)
     import torch
+    site = _check_site(site)
     out = torch.empty_like(y) if out is None else out
     _check_like(y, (y, x, out))
     _check_rng(rng, p)
     _same_device((y, x, out, rng))
-    _check(load_library().hdt_dropout_add(_ptr(y), _ptr(x), _ptr(out), y.numel(), float(p), _ptr(rng), int(site), _dtype_code(y), _stream_ptr(stream)))
+    _check(load_library().hdt_dropout_add(_ptr(y), _ptr(x), _ptr(out), y.numel(), float(p), _ptr(rng), site, _dtype_code(y), _stream_ptr(stream)))
     return out
 
 
@@ -693,6 +701,7 @@ def hdt_add_norm_fwd(x, weight, bias=None, eps: float = 1e-5, y=None, p: float =
     if r is not None:
         _check(r)
     import torch
+    site = _check_site(site)
     if x.dim() < 1:
         raise ValueError("x must have a last dimension")
     n = torch.empty_like(x) if n is None else n
@@ -709,7 +718,7 @@ def hdt_add_norm_fwd(x, weight, bias=None, eps: float = 1e-5, y=None, p: float =
     if y is None:
         p = 0.0
     _check(load_library().hdt_add_norm_fwd(_ptr(x), _ptr(y), _ptr(weight), _ptr(bias), rows, x.shape[-1], float(eps), float(p), _ptr(rng),
-                                           int(site), _ptr(h) if y is not None else None, _ptr(n), _ptr(mean), _ptr(rstd), _dtype_code(x),
+                                           site, _ptr(h) if y is not None else None, _ptr(n), _ptr(mean), _ptr(rstd), _dtype_code(x),
                                            _dtype_code(weight), _stream_ptr(stream)))
     return n, h, mean, rstd
 
@@ -726,6 +735,7 @@ def hdt_add_norm_bwd(dn, h, weight, mean, rstd, dh=None, p: float = 0.0, rng=Non
     if r is not None:
         _check(r)
     import torch
+    site = _check_site(site)
     lib = _lib
     dx = torch.empty_like(h) if dx is None else dx
     dropped = int(float(p) * 65536 + 0.5) > 0
@@ -743,6 +753,6 @@ def hdt_add_norm_bwd(dn, h, weight, mean, rstd, dh=None, p: float = 0.0, rng=Non
     if workspace is None:
         workspace = _scratch(lib.hdt_add_norm_bwd_workspace_bytes(rows, h.shape[-1]), h.device, stream)
     _check(lib.hdt_add_norm_bwd(_ptr(dn), _ptr(dh), _ptr(h), _ptr(weight), _ptr(mean), _ptr(rstd), rows, h.shape[-1], float(p), _ptr(rng),
-                                int(site), _ptr(dx), _ptr(dy) if dropped else None, _ptr(dweight), _ptr(dbias), _dtype_code(h), _dtype_code(weight),
+                                site, _ptr(dx), _ptr(dy) if dropped else None, _ptr(dweight), _ptr(dbias), _dtype_code(h), _dtype_code(weight),
                                 _ptr(workspace), workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
     return dx, dy, dweight, dbias

@@ -30,3 +30,14 @@ def test_one_row_expanded_over_all(hdt, attention, name):  # noqa: F811
             hdt.hdt_rel_attn_fwd(**{**fwd, name: row})
     with pytest.raises(ValueError, match=name):
         hdt.hdt_rel_attn_bwd(**{**bwd, name: row})
+
+
+def test_sites_outside_32_bits(hdt):  # noqa: F811
+    import torch
+    t = tensors(torch.float32)
+    n, h, mean, rstd = hdt.hdt_add_norm_fwd(t["x"], t["w"], y=t["y"], p=0.1, rng=t["rng"], site=2 ** 32 - 1)
+    for site in (-1, 2 ** 32, 2 ** 32 + 3, 2 ** 70):
+        for call in (lambda: hdt.hdt_dropout_add(t["y"], 0.1, t["rng"], site), lambda: hdt.hdt_add_norm_fwd(t["x"], t["w"], y=t["y"], p=0.1, rng=t["rng"], site=site),
+                     lambda: hdt.hdt_add_norm_bwd(t["dn"], h, t["w"], mean, rstd, p=0.1, rng=t["rng"], site=site)):
+            with pytest.raises(ValueError, match="site"):
+                call()
