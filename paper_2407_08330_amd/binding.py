@@ -527,13 +527,22 @@ def hdt_hpe_add(p, table, x, stream=None):
     return x
 
 
+def _int32(name, v):
+    """A number as the ABI takes it; ctypes would cut a larger one without a word."""
+    v = int(v)
+    if not -1 << 31 <= v < 1 << 31:
+        raise ValueError(f"{name} {v} does not fit 32 bits")
+    return v
+
+
 def hdt_rel_table(n_buckets: int, max_distance: int, both_ways: bool = False, device="cuda", stream=None):
     """int32 device tensor [2 max_distance + 1]: T5's bucket of every distance key - query; ``both_ways`` for attention that is
     not causal."""
     import torch
-    table = torch.empty(2 * max(int(max_distance), 0) + 1, dtype=torch.int32, device=device)
+    n_buckets, max_distance = _int32("n_buckets", n_buckets), _int32("max_distance", max_distance)
+    table = torch.empty(2 * max(max_distance, 0) + 1, dtype=torch.int32, device=device)
     _same_device((table,))
-    _check(load_library().hdt_rel_table(int(n_buckets), int(max_distance), int(both_ways), _ptr(table), _stream_ptr(stream)))
+    _check(load_library().hdt_rel_table(n_buckets, max_distance, int(bool(both_ways)), _ptr(table), _stream_ptr(stream)))
     return table
 
 
@@ -560,7 +569,9 @@ def _rel_attn_call(q, k, v, bias, table, softmax_scale, causal, lengths, q_start
     for name, t in (("lengths", lengths), ("q_start", q_start)):
         if t is not None and (t.dtype != torch.int32 or t.shape != (B,) or not t.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous int32 tensor [batch]")
-    c = _RelAttn(B, H, KV, nq, nk, D, int(causal), bias.shape[0], table.numel() // 2, _dtype_code(q), _dtype_code(bias), float(softmax_scale),
+    for n in (*q.shape, *k.shape, bias.shape[0]):
+        _int32("a size of", n)
+    c = _RelAttn(B, H, KV, nq, nk, D, int(bool(causal)), bias.shape[0], table.numel() // 2, _dtype_code(q), _dtype_code(bias), float(softmax_scale),
                  _ptr(bias), _ptr(table), _ptr(lengths), _ptr(q_start))
     for name, t in dict(others, q=q, k=k, v=v).items():
         shape = k.shape if name in ("k", "v", "dk", "dv") else q.shape
@@ -681,6 +692,7 @@ def hdt_dropout_add(y, p: float, rng=None, site: int = 0, x=None, out=None, stre
 def _check_norm(x, weight, vectors, statistics):
     import torch
     rows = x.shape[:-1].numel()
+    _int32("a width of", x.shape[-1])
     for w in (weight, *vectors):
         if w is not None and (w.shape != x.shape[-1:] or w.dtype != weight.dtype or not (w.is_cuda and w.is_contiguous())):
             raise ValueError("weight and bias must be contiguous device tensors [width] of one dtype")

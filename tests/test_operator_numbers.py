@@ -21,3 +21,33 @@ def test_sites_outside_32_bits(hdt, site):
                  lambda: hdt.hdt_add_norm_bwd(x, x, w, one, one, p=0.1, rng=rng, site=site)):
         with pytest.raises(ValueError, match="site"):
             call()
+
+
+@pytest.mark.parametrize("buckets,distance", [(2 ** 32 + 32, 128), (32, 2 ** 32 + 128), (-2 ** 32 + 32, 128), (2 ** 31, 128), (32, -2 ** 33 + 128)])
+def test_tables_of_more_than_32_bits(hdt, buckets, distance, monkeypatch):
+    """Refused by their numbers, before memory is asked for."""
+    import torch
+    from paper_2407_08330_amd import binding
+    monkeypatch.setattr(torch, "empty", lambda *a, **kw: pytest.fail("memory was asked for"))
+    with pytest.raises(ValueError, match="32 bits"):
+        binding.hdt_rel_table(buckets, distance, device="cpu")
+
+
+def test_sizes_of_more_than_32_bits(hdt, monkeypatch):
+    """Shapes that only an expanded or an empty tensor has here."""
+    import torch
+    from paper_2407_08330_amd import binding
+    monkeypatch.setattr(binding, "_same_device", lambda ts: None)
+    many = 2 ** 32 + 4
+    q, k = torch.zeros(1, 4, 8, 64), torch.zeros(1, 4, 8, 64)
+    bias, table = torch.zeros(32, 4), torch.zeros(257, dtype=torch.int32)
+
+    def describe(q, k, bias):
+        return binding._rel_attn_call(q, k, k, bias, table, 0.125, True, None, None)
+    describe(q, k, bias)
+    for bad in (dict(k=k[:, :1].expand(1, many, 8, 64)), dict(q=q.expand(many, 4, 8, 64), k=k.expand(many, 4, 8, 64))):
+        with pytest.raises(ValueError, match="32 bits"):
+            describe(**{**dict(q=q, k=k, bias=bias), **bad})
+    x = torch.zeros(0, 2 ** 32 + 8)
+    with pytest.raises(ValueError, match="32 bits"):
+        binding._check_norm(x, torch.zeros(0), (), ())
