@@ -554,6 +554,12 @@ def _same_device(ts):
             raise ValueError("tensors must be on the current device")
 
 
+def _check_workspace(w):
+    """Its size is what its elements take: of a tensor that is not contiguous that is not the memory from its address on."""
+    if w is not None and not (w.is_cuda and w.is_contiguous()):
+        raise ValueError("workspace must be a contiguous device tensor")
+
+
 def _rel_attn_call(q, k, v, bias, table, softmax_scale, causal, lengths, q_start, **others):
     """The description of a call; ``others``: name of a strided tensor -> the tensor (shaped like q or k)."""
     import torch
@@ -609,6 +615,7 @@ def hdt_rel_attn_fwd(q, k, v, bias, table, softmax_scale: float, causal: bool = 
     c = _rel_attn_call(q, k, v, bias, table, softmax_scale, causal, lengths, q_start, o=o)
     if lse.shape != q.shape[:3] or lse.dtype != torch.float32 or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous float32 tensor [batch][heads][n_q]")
+    _check_workspace(workspace)
     _same_device((lse, workspace))
     if workspace is None:
         need = lib.hdt_rel_attn_fwd_workspace_bytes(ctypes.byref(c))
@@ -639,6 +646,7 @@ def hdt_rel_attn_bwd(q, k, v, bias, table, o, lse, d_o, softmax_scale: float, ca
         raise ValueError("lse must be a contiguous float32 tensor [batch][heads][n_q]")
     if dbias.shape != bias.shape or dbias.dtype != bias.dtype or not dbias.is_contiguous():
         raise ValueError("dbias must be like bias")
+    _check_workspace(workspace)
     _same_device((lse, dbias, workspace))
     if workspace is None:
         workspace = _scratch(lib.hdt_rel_attn_bwd_workspace_bytes(ctypes.byref(c)), q.device, stream)
@@ -761,6 +769,7 @@ def hdt_add_norm_bwd(dn, h, weight, mean, rstd, dh=None, p: float = 0.0, rng=Non
     _check_like(h, (h, dn, dh, dx, dy))
     rows = _check_norm(h, weight, (dweight, dbias), (mean, rstd))
     _check_rng(rng, p)
+    _check_workspace(workspace)
     _same_device((h, dn, dh, dx, dy, weight, dweight, dbias, mean, rstd, rng, workspace))
     if workspace is None:
         workspace = _scratch(lib.hdt_add_norm_bwd_workspace_bytes(rows, h.shape[-1]), h.device, stream)

@@ -335,11 +335,11 @@ struct Room {
         if (t.defined()) at_ = t.data_ptr(), bytes = (size_t)t.numel() * t.element_size();
     }
 };
-// None or a plain tensor here; and a temporary workspace comes from the stream the kernels run on: the current one, that is
+// None or a plain contiguous tensor here; and a temporary workspace comes from the stream the kernels run on: the current one, that is
 bool workspace_ok(PyObject *w, PyObject *stream, int device)
 {
     const at::Tensor *t;
-    return optional(w, device, &t) && (t || stream == Py_None);
+    return optional(w, device, &t) && (t ? t->is_contiguous() : stream == Py_None);
 }
 
 // (q, k, v, bias, table, scale, causal, lengths, q_start, o, lse, workspace, stream) -> (o, lse), a status, or None

@@ -41,3 +41,16 @@ def test_sites_outside_32_bits(hdt):  # noqa: F811
                      lambda: hdt.hdt_add_norm_bwd(t["dn"], h, t["w"], mean, rstd, p=0.1, rng=t["rng"], site=site)):
             with pytest.raises(ValueError, match="site"):
                 call()
+
+
+def test_workspaces_that_are_not_contiguous(hdt, attention):  # noqa: F811
+    """A byte expanded to any size, and every second byte of a buffer: refused, however large they say they are."""
+    import torch
+    fwd, bwd = attention
+    t = tensors(torch.float32)
+    n, h, mean, rstd = hdt.hdt_add_norm_fwd(t["x"], t["w"], y=t["y"], p=0.1, rng=t["rng"])
+    for w in (torch.zeros(16, dtype=torch.uint8, device="cuda")[:1].expand(1 << 30), torch.zeros(1 << 26, dtype=torch.uint8, device="cuda")[::2]):
+        for call in (lambda: hdt.hdt_rel_attn_fwd(**fwd, workspace=w), lambda: hdt.hdt_rel_attn_bwd(**bwd, workspace=w),
+                     lambda: hdt.hdt_add_norm_bwd(t["dn"], h, t["w"], mean, rstd, p=0.1, rng=t["rng"], workspace=w)):
+            with pytest.raises(ValueError, match="workspace"):
+                call()
