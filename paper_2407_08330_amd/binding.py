@@ -697,6 +697,12 @@ def hdt_dropout_add(y, p: float, rng=None, site: int = 0, x=None, out=None, stre
     return out
 
 
+def _check_copy(out, others):
+    """A result that is made by a copy is none of the call's other tensors."""
+    if out.numel() > 0 and any(t is not None and t.data_ptr() == out.data_ptr() for t in others):
+        raise ValueError("output aliases an input or another output")
+
+
 def _check_norm(x, weight, vectors, statistics):
     import torch
     rows = x.shape[:-1].numel()
@@ -712,7 +718,8 @@ def _check_norm(x, weight, vectors, statistics):
 
 def hdt_add_norm_fwd(x, weight, bias=None, eps: float = 1e-5, y=None, p: float = 0.0, rng=None, site: int = 0, h=None, n=None, mean=None,
                      rstd=None, stream=None):
-    """h = x + dropout(y), n = layer norm of h over the last dimension.  Returns (n, h, mean, rstd); h is x where y is None."""
+    """h = x + dropout(y), n = layer norm of h over the last dimension.  Returns (n, h, mean, rstd); where y is None h is x, and a
+    given ``h`` a copy of it."""
     if _lib is None:
         load_library()
     r = _calls.add_norm_fwd(x, weight, bias, eps, y, p, rng, site, h, n, mean, rstd, None if stream is None else stream.cuda_stream)
@@ -725,10 +732,8 @@ def hdt_add_norm_fwd(x, weight, bias=None, eps: float = 1e-5, y=None, p: float =
     if x.dim() < 1:
         raise ValueError("x must have a last dimension")
     n = torch.empty_like(x) if n is None else n
-    if y is None:
-        h = x
-    elif h is None:
-        h = torch.empty_like(x)
+    if h is None:
+        h = x if y is None else torch.empty_like(x)
     mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if mean is None else mean
     rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if rstd is None else rstd
     _check_like(x, (x, y, h, n))
@@ -737,16 +742,19 @@ def hdt_add_norm_fwd(x, weight, bias=None, eps: float = 1e-5, y=None, p: float =
     _same_device((x, y, h, n, weight, bias, mean, rstd, rng))
     if y is None:
         p = 0.0
+        _check_copy(h, (n, mean, rstd))
     _check(load_library().hdt_add_norm_fwd(_ptr(x), _ptr(y), _ptr(weight), _ptr(bias), rows, x.shape[-1], float(eps), float(p), _ptr(rng),
                                            site, _ptr(h) if y is not None else None, _ptr(n), _ptr(mean), _ptr(rstd), _dtype_code(x),
                                            _dtype_code(weight), _stream_ptr(stream)))
+    if y is None and h.data_ptr() != x.data_ptr():
+        hdt_dropout_add(x, 0.0, out=h, stream=stream)
     return n, h, mean, rstd
 
 
 def hdt_add_norm_bwd(dn, h, weight, mean, rstd, dh=None, p: float = 0.0, rng=None, site: int = 0, bias: bool = True, dx=None, dy=None,
                      dweight=None, dbias=None, workspace=None, stream=None):
     """Gradients of hdt_add_norm_fwd from dn (that of n) and dh (that of h from elsewhere, or None).  Returns (dx, dy, dweight, dbias):
-    dy is dx itself where nothing is dropped, dbias None with ``bias=False``."""
+    where nothing is dropped dy is dx itself, and a given ``dy`` a copy of it; dbias is None with ``bias=False``."""
     if _lib is None:
         load_library()
     r = _calls.add_norm_bwd(dn, h, weight, mean, rstd, dh, p, rng, site, bias, dx, dy, dweight, dbias, workspace, None if stream is None else stream.cuda_stream)
@@ -759,10 +767,8 @@ def hdt_add_norm_bwd(dn, h, weight, mean, rstd, dh=None, p: float = 0.0, rng=Non
     lib = _lib
     dx = torch.empty_like(h) if dx is None else dx
     dropped = int(float(p) * 65536 + 0.5) > 0
-    if not dropped:
-        dy = dx
-    elif dy is None:
-        dy = torch.empty_like(h)
+    if dy is None:
+        dy = torch.empty_like(h) if dropped else dx
     dweight = torch.empty_like(weight) if dweight is None else dweight
     if bias and dbias is None:
         dbias = torch.empty_like(weight)
@@ -771,9 +777,13 @@ def hdt_add_norm_bwd(dn, h, weight, mean, rstd, dh=None, p: float = 0.0, rng=Non
     _check_rng(rng, p)
     _check_workspace(workspace)
     _same_device((h, dn, dh, dx, dy, weight, dweight, dbias, mean, rstd, rng, workspace))
+    if not dropped:
+        _check_copy(dy, (h, dn, dh, weight, mean, rstd, dweight, dbias))
     if workspace is None:
         workspace = _scratch(lib.hdt_add_norm_bwd_workspace_bytes(rows, h.shape[-1]), h.device, stream)
     _check(lib.hdt_add_norm_bwd(_ptr(dn), _ptr(dh), _ptr(h), _ptr(weight), _ptr(mean), _ptr(rstd), rows, h.shape[-1], float(p), _ptr(rng),
                                 site, _ptr(dx), _ptr(dy) if dropped else None, _ptr(dweight), _ptr(dbias), _dtype_code(h), _dtype_code(weight),
                                 _ptr(workspace), workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+    if not dropped and dy.data_ptr() != dx.data_ptr():
+        hdt_dropout_add(dx, 0.0, out=dy, stream=stream)
     return dx, dy, dweight, dbias
