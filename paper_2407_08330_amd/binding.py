@@ -2,7 +2,11 @@
 HIP kernels behind the C ABI declared in ``include/hdt.h``; there is no fallback path, and a
 missing library is an error.  The calls every layer makes (build, forward, backward; relative-bias attention, dropout, norm) go through native code
 (``csrc/hdt_pycall.cpp``) where their arguments are plain tensors and numbers, and through ctypes otherwise; that module is
-compiled for one Python and one torch, and under others, or without it, ctypes takes all calls."""
+compiled for one Python and one torch, and under others, or without it, ctypes takes all calls.
+
+``stream``: a ``torch.cuda.Stream`` for the kernels (None: the current one).  Results that a call makes come from the CURRENT stream's memory, a
+temporary workspace from that of ``stream``: with another stream the caller orders the two, ``stream.wait_stream(current)`` before the call and
+``current.wait_stream(stream)`` before a result is used or dropped, or gives the results."""
 from __future__ import annotations
 
 import ctypes

@@ -10,7 +10,9 @@
 //
 // All of it is bound by memory: a row is read once, held in registers between its statistics and its result, and written once.  On 32768
 // bf16 rows of 768 columns: dropout with residual 26 us (151 MB, 5.7 TB/s), norm forward and backward 92 us (453 MB, 4.9 TB/s); a copy
-// of 200 MB reaches 5.4 TB/s, one of 2 GB 4.9.
+// of 200 MB reaches 5.4 TB/s, one of 2 GB 4.9.  Two things are slower.  Above 8192 columns the backward's row does not fit the registers of
+// its 1024 threads (128 each): 264 to 603 values a thread lie in scratch memory, 1.0-1.9 TB/s.  Widths that are no multiple of eight have
+// their accesses aligned to an element only and every chunk's random numbers from two blocks: bf16 2.2 TB/s, fp32 2.8-3.8.
 // Sums and statistics are in fp32; h is rounded once, when it is written (the norm is taken of the unrounded sum).
 #include <algorithm>
 
@@ -375,7 +377,9 @@ constexpr int kMostWidth = 32768, kMostParts = 512;
 constexpr long long kMostElements = 1ll << 35;  // 2^32 blocks of eight
 
 // threads a row and chunks a thread: a wave up to 2048 columns, then a workgroup of 256 or 1024 (us at 32768 bf16 rows, wave | workgroup of
-// 256: 768 columns 36 | 91 forward, 48 | 93 backward; 2048 columns 99 | 129, 137 | 135; 4096 rows of 2048 14.7 | 17.7, 26 | 25)
+// 256: 768 columns 36 | 91 forward, 48 | 93 backward; 2048 columns 99 | 129, 137 | 135; 4096 rows of 2048 14.7 | 17.7, 26 | 25).  TB/s
+// forward, backward, dropping: bf16 16384 x 4096 5.6, 5.0; 8192 x 8192 5.4, 4.6; 4096 x 12288 4.2, 1.7; 2048 x 32768 4.7, 1.3; 16384 x 2049
+// 2.2, 2.2; 8192 x 8193 2.1, 1.2; fp32 16384 x 4096 5.8, 5.3; 8192 x 8192 5.5, 4.9; 4096 x 12288 4.5, 1.5; 2048 x 32768 4.9, 1.6
 struct RowShape {
     int tpr, nch;
 };

@@ -33,7 +33,7 @@ hdt_status_t hdt_launch_rel_fwd(const hdt_rel_attn_t &d, const RelFwdArgs &a, in
 // (us, 4 | 2 | 1 waves.  Backward bf16, heads x rows of 64: 128 x 512 47.6 | 58.8 | 136, 64 x 512 35.8 | 36.1 | 71, 32 x 512 27.5 | 26.5 | 39.9,
 // 16 x 512 27.1 | 22.2 | 25.9, 8 x 512 26.7 | 22.4 | 19.3; of 128: 32 x 512 36.0 | 41.9, 16 x 512 34.5 | 29.2.  fp32 of 64: 64 x 512
 // 112 | 116 | 152, 32 x 512 88 | 64 | 82, 16 x 512 87 | 54 | 47.  Forward bf16 of 64: 128 x 512 13.8 | 18.1 | 51, 64 x 512 12.2 | 10.9 | 26,
-// 16 x 512 11.6 | 9.6 | 8.8.)
+// 16 x 512 11.6 | 9.6 | 8.8.  Calls of more rows take the rule as it is: its figures are of 512.)
 inline int hdt_rel_row_waves(long long tiles64, long long tiles32, const hdt_rel_attn_t &d)
 {
     if (d.head_dim == 64 && tiles32 <= (d.dtype == HDT_BF16 ? 256 : 512)) return 1;

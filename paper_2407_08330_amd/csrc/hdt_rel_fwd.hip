@@ -11,7 +11,7 @@
 // reference of the exponentials follows the maximum only from a factor 2^8 on, which saves rescaling and costs nothing in fp32 or bf16.
 //
 // What bounds it: vector instructions (an exponential, a fused multiply-add, a sum, half a maximum and half a conversion for each pair) next
-// to the matrix ones.  24 heads x 8192 x 64, causal: 231 us, 0.89 PFLOP/s, vector pipe issuing 68 % and matrix pipe busy 41 % of all
+// to the matrix ones.  24 heads x 8192 x 64, causal: 232-243 us, 0.85-0.89 PFLOP/s, vector pipe issuing 68 % and matrix pipe busy 41 % of all
 // clocks.  32 heads x 4096 x 128: 150 us, 0.91.  (Tried on the first: no maximum unless a row's sum is large, with the contraction taken
 // again then, 170 registers and a wave less a SIMD: 231 -> 243; sums by dot products of the rounded weights: 2 % quicker, but LSE then has
 // bf16's errors; two blocks of rows a wave, which share the operands from LDS,
@@ -524,6 +524,8 @@ RelFwdPlan hdt_rel_fwd_plan(const hdt_rel_attn_t &d)
         // Pieces of the keys in workgroups of their own, one a compute unit (its rings fill the LDS), and a second kernel that joins them:
         // for keys whose walk takes longer than that.  (us, one piece | these.  Heads of 64 x keys: 8 x 1000 8.7 | 9.8, 8 x 2000 11.8 | 10.1,
         // 8 x 8192 30.2 | 10.9, 32 x 8192 30.8 | 17.7; of 128: 128 x 8192 86 | 66.  4 workgroups a unit instead of one: 256 x 8192 92 | 100.)
+        // (A launch is made of whole rounds of one workgroup a unit, which shows where heads are just above a multiple of 256: heads of 64 x
+        // 8192 keys, 192 72 us, 252 102, 264 131 (4.2 TB/s), 384 149 (5.4), 504 192, 516 217 (5.0).)
         pieces = (long long)d.n_kv * d.head_dim < 96 * 1024 ? 1 : std::min<long long>(256 / heads, (d.n_kv + 511) / 512);
     } else {
         // Keys many times the rows (a chunk behind a long cache): tiles of 128 rows and pieces; otherwise the tile that hdt_rel_row_waves()
