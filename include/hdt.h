@@ -377,8 +377,8 @@ hdt_status_t hdt_hpe_add(const int32_t *d_p, int32_t batch, int32_t n_pos, int32
  * lies in [0, d_lengths[sample]): the queries are a window of the sequence whose keys are given.  A training step has the whole of
  * it (d_q_start NULL: 0), a step of generation its last n_q positions (d_q_start = length - n_q, the new keys already in the cache).
  * Rows that are not real get O = 0, LSE = -inf and gradients of 0, and so do keys from the length on; what such rows of Q, K, V,
- * O, dO hold may be anything, NaN included.  A NaN in a REAL row reaches the rows that see it: their O and LSE are NaN (LSE = -inf
- * is only said of rows without a weight), and so are the gradients it goes into.  A score of plus infinity counts as NaN, one of minus
+ * O, dO hold may be anything, NaN included.  A NaN in a REAL row reaches the rows that see it: their O and, unless it is V's, their LSE
+ * are NaN (LSE = -inf is only said of rows without a weight), and so are the gradients it goes into.  A score of plus infinity counts as NaN, one of minus
  * infinity is a weight of zero, and a row that has no other is like one that sees nothing.  A non-finite value may also reach rows
  * and keys of its tile of 128 x 64 pairs (one way or the other) that the causal mask hides it from, and rows that a hidden bucket hides
  * it from: zero weights are applied by multiplication.
