@@ -157,7 +157,7 @@ def _run_ffn(st, case):
         y, *kept = hdt.hdt_ffn_fwd(st["x"], *weights, case["act"], train=case["backward"])
         if not case["backward"]:
             return {"y": y}
-        dx, dwg, dwu, dwd = hdt.hdt_ffn_bwd(st["dy"], st["x"], *weights, *kept, case["act"])
+        dx, dwg, dwu, dwd = hdt.hdt_ffn_bwd(st["dy"], st["x"], *weights, *kept)
         return {"y": y, "dx": dx, "dw_gate": dwg, "dw_up": dwu, "dw_down": dwd}
     return _plain_ffn(st, case)
 
