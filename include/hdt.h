@@ -466,6 +466,73 @@ hdt_status_t hdt_add_norm_bwd(const void *dn, const void *dh, const void *h, con
                               int64_t rows, int32_t width, double p, const int64_t *d_rng, uint32_t site, void *dx, void *dy, void *d_weight,
                               void *d_bias, hdt_dtype_t dt, hdt_dtype_t weight_dt, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Token embeddings, which stand in front of hdt_hpe_add, and the gradient of their table.
+ *
+ * hdt_embed_fwd -- out[t] = scale table[d_ids[t]] for `tokens` ids; ids outside [0, vocab) (pads) give rows of 0.
+ * hdt_embed_bwd -- grad[v] = scale times the sum of the rows d_out[t] with d_ids[t] = v, 0 where there is none; with `accumulate` that is
+ *   added to what stands in grad, whose other rows are left as they are (gradients of several steps, or of a table that is also the output
+ *   projection).  Rows of d_out whose ids lie outside [0, vocab) may hold anything.  Sums are in fp32, in an order that the ids alone decide.
+ *
+ *   d_ids     device, int32 [tokens]
+ *   table     device, [vocab][width] of table_dt; grad alike.  out, d_out: device, [tokens][width] of dt.  Dense, 16-byte aligned (ids: 4).
+ *   workspace device, hdt_embed_bwd_workspace_bytes bytes, 16-byte aligned, scratch only
+ * width 1 .. 32768, vocab 1 .. 2^24, at most 2^30 tokens and 2^35 elements.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED (dtype), HDT_ERR_HIP.
+ */
+hdt_status_t hdt_embed_fwd(const int32_t *d_ids, int64_t tokens, const void *table, int32_t vocab, int32_t width, float scale, void *out,
+                           hdt_dtype_t table_dt, hdt_dtype_t dt, void *stream);
+size_t hdt_embed_bwd_workspace_bytes(int64_t tokens, int32_t width);
+hdt_status_t hdt_embed_bwd(const void *d_out, const int32_t *d_ids, int64_t tokens, int32_t vocab, int32_t width, float scale, int32_t accumulate,
+                           void *grad, hdt_dtype_t table_dt, hdt_dtype_t dt, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The gated feed-forward block of a layer ("FFN" of Sec. 3.2, with a gate):
+ *     G = X Wg^T,  U = X Wu^T,  H = act(G) o U,  Y = H Wd^T;   X [rows][width], Wg, Wu [inner][width], Wd [width][inner]
+ *
+ * hdt_ffn_fwd -- x and the weights -> y; and what the backward reads, [rows][inner] each: by_gate = U o act'(G) and by_up = act(G), the derivatives
+ *   of H by G and U, and hidden = H.  All three, or all NULL (H then goes to the workspace).
+ * hdt_ffn_bwd -- from dy, the gradient of y: dx, dw_gate, dw_up, dw_down, each like what it is the gradient of.  Every output is written whole.
+ * All tensors are dense, of dtype dt, 16-byte aligned.  Sums are in fp32, in an order that the sizes decide; in HDT_BF16 H, its derivatives and the
+ * gradients of G and U are rounded to bf16 when they are written.  A row of y or dx depends on that row of the inputs alone.  `workspace`: ..._workspace_bytes bytes, 16-byte
+ * aligned, scratch only (0: none needed).
+ * width, inner 1 .. 65536, at most 2^28 rows and 2^35 elements a tensor.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED (dtype, act), HDT_ERR_HIP.
+ */
+typedef enum {
+    HDT_SILU = 0,     /* g / (1 + exp(-g)) */
+    HDT_GELU = 1,     /* g Phi(g), Phi the normal distribution's */
+    HDT_GELU_TANH = 2 /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 */
+} hdt_act_t;
+size_t hdt_ffn_fwd_workspace_bytes(int64_t rows, int32_t width, int32_t inner, int32_t train, hdt_dtype_t dt);
+hdt_status_t hdt_ffn_fwd(const void *x, const void *w_gate, const void *w_up, const void *w_down, int64_t rows, int32_t width, int32_t inner,
+                         hdt_act_t act, void *y, void *by_gate, void *by_up, void *hidden, hdt_dtype_t dt, void *workspace, size_t workspace_bytes, void *stream);
+size_t hdt_ffn_bwd_workspace_bytes(int64_t rows, int32_t width, int32_t inner, hdt_dtype_t dt);
+hdt_status_t hdt_ffn_bwd(const void *dy, const void *x, const void *w_gate, const void *w_up, const void *w_down, const void *by_gate,
+                         const void *by_up, const void *hidden, int64_t rows, int32_t width, int32_t inner, void *dx, void *dw_gate, void *dw_up,
+                         void *dw_down, hdt_dtype_t dt, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The norms before and after a block, its gate and the residual in one pass, where hdt_add_norm_fwd has the norm in front of the next
+ * block alone:
+ *     c = norm(y; post_weight, post_bias),  h = scale x + gate o c,  n = norm(h; weight, bias)
+ * norm(v) = (v - mean) rstd weight + bias over rows of `width`, rstd = 1 / sqrt(variance + eps); with `rms` the mean counts as 0 (T5's norm).
+ *
+ * hdt_gate_norm_fwd -- x (the residual stream) and y (the block's output) -> h, n, and stats, float [4][rows]: mean and rstd of y, of h.
+ *   Statistics of h are those of the unrounded h.  post_bias, bias and gate [width] may be NULL (0, 0, 1).
+ * hdt_gate_norm_bwd -- from dn, the gradient of n, and dh, that of h from elsewhere (may be NULL); h and stats are the forward's: dx, dy and
+ *   the gradients [width], of weight_dt, of post_weight, post_bias (may be NULL), gate (may be NULL), weight, bias (may be NULL).
+ * Tensors are dense, of dtype dt; post_weight, post_bias, gate, weight, bias of weight_dt; 16-byte aligned (stats: 4).  `workspace`:
+ * hdt_gate_norm_bwd_workspace_bytes bytes, 16-byte aligned, scratch only.  Sums are in fp32 in a fixed order.  width 1 .. 32768, at most
+ * 2^31 - 1 rows and 2^35 elements.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED (dtype), HDT_ERR_HIP.
+ */
+hdt_status_t hdt_gate_norm_fwd(const void *x, const void *y, const void *post_weight, const void *post_bias, const void *gate, const void *weight,
+                               const void *bias, int64_t rows, int32_t width, float eps, float scale, int32_t rms, void *h, void *n, float *stats,
+                               hdt_dtype_t dt, hdt_dtype_t weight_dt, void *stream);
+size_t hdt_gate_norm_bwd_workspace_bytes(int64_t rows, int32_t width);
+hdt_status_t hdt_gate_norm_bwd(const void *dn, const void *dh, const void *h, const void *y, const float *stats, const void *post_weight,
+                               const void *post_bias, const void *gate, const void *weight, int64_t rows, int32_t width, float scale, int32_t rms, void *dx,
+                               void *dy, void *d_post_weight, void *d_post_bias, void *d_gate, void *d_weight, void *d_bias, hdt_dtype_t dt,
+                               hdt_dtype_t weight_dt, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Text of a status code / of the last error on this thread (never NULL). */
 const char *hdt_status_string(hdt_status_t status);
 const char *hdt_last_error(void);

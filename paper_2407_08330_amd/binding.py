@@ -32,6 +32,8 @@ EXPORTED_SYMBOLS = [
     "hdt_parents_from_levels", "hdt_index_vectors_workspace_bytes", "hdt_index_vectors", "hdt_hpe_table", "hdt_hpe_add",
     "hdt_rel_table", "hdt_rel_attn_fwd_workspace_bytes", "hdt_rel_attn_fwd", "hdt_rel_attn_bwd_workspace_bytes", "hdt_rel_attn_bwd",
     "hdt_dropout_add", "hdt_add_norm_fwd", "hdt_add_norm_bwd_workspace_bytes", "hdt_add_norm_bwd",
+    "hdt_embed_fwd", "hdt_embed_bwd_workspace_bytes", "hdt_embed_bwd", "hdt_ffn_fwd_workspace_bytes", "hdt_ffn_fwd", "hdt_ffn_bwd_workspace_bytes",
+    "hdt_ffn_bwd", "hdt_gate_norm_fwd", "hdt_gate_norm_bwd_workspace_bytes", "hdt_gate_norm_bwd",
 ]
 
 
@@ -75,6 +77,7 @@ def library_path() -> str:
 class _NoCalls:
     """In the place of csrc/hdt_pycall.cpp: takes no call."""
     build_layout = attn_fwd = attn_bwd = rel_attn_fwd = rel_attn_bwd = dropout_add = add_norm_fwd = add_norm_bwd = staticmethod(lambda *a: None)
+    embed_fwd = embed_bwd = ffn_fwd = ffn_bwd = gate_norm_fwd = gate_norm_bwd = staticmethod(lambda *a: None)
 
 
 def _native_calls(lib, torch_version: str):
@@ -92,7 +95,9 @@ def _native_calls(lib, torch_version: str):
                                                                  lib.hdt_attn_bwd, lib.hdt_attn_bwd_workspace_bytes)))
     calls.bind_operators(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
         lib.hdt_rel_attn_fwd_workspace_bytes, lib.hdt_rel_attn_fwd, lib.hdt_rel_attn_bwd_workspace_bytes, lib.hdt_rel_attn_bwd, lib.hdt_dropout_add,
-        lib.hdt_add_norm_fwd, lib.hdt_add_norm_bwd_workspace_bytes, lib.hdt_add_norm_bwd)))
+        lib.hdt_add_norm_fwd, lib.hdt_add_norm_bwd_workspace_bytes, lib.hdt_add_norm_bwd, lib.hdt_embed_fwd, lib.hdt_embed_bwd_workspace_bytes,
+        lib.hdt_embed_bwd, lib.hdt_ffn_fwd_workspace_bytes, lib.hdt_ffn_fwd, lib.hdt_ffn_bwd_workspace_bytes, lib.hdt_ffn_bwd, lib.hdt_gate_norm_fwd,
+        lib.hdt_gate_norm_bwd_workspace_bytes, lib.hdt_gate_norm_bwd)))
     return calls
 
 
@@ -176,9 +181,21 @@ def load_library():
     lib.hdt_add_norm_fwd.argtypes = [vp, vp, vp, vp, i64, i32, f32, f64, vp, ctypes.c_uint32, vp, vp, vp, vp, code, code, vp]
     lib.hdt_add_norm_bwd_workspace_bytes.argtypes = [i64, i32]
     lib.hdt_add_norm_bwd.argtypes = [vp] * 6 + [i64, i32, f64, vp, ctypes.c_uint32] + [vp] * 4 + [code, code, vp, size, vp]
-    for f in (lib.hdt_rel_table, lib.hdt_rel_attn_fwd, lib.hdt_rel_attn_bwd, lib.hdt_dropout_add, lib.hdt_add_norm_fwd, lib.hdt_add_norm_bwd):
+    lib.hdt_embed_fwd.argtypes = [vp, i64, vp, i32, i32, f32, vp, code, code, vp]
+    lib.hdt_embed_bwd_workspace_bytes.argtypes = [i64, i32]
+    lib.hdt_embed_bwd.argtypes = [vp, vp, i64, i32, i32, f32, i32, vp, code, code, vp, size, vp]
+    lib.hdt_ffn_fwd_workspace_bytes.argtypes = [i64, i32, i32, i32, code]
+    lib.hdt_ffn_fwd.argtypes = [vp] * 4 + [i64, i32, i32, code] + [vp] * 4 + [code, vp, size, vp]
+    lib.hdt_ffn_bwd_workspace_bytes.argtypes = [i64, i32, i32, code]
+    lib.hdt_ffn_bwd.argtypes = [vp] * 8 + [i64, i32, i32] + [vp] * 4 + [code, vp, size, vp]
+    lib.hdt_gate_norm_fwd.argtypes = [vp] * 7 + [i64, i32, f32, f32, i32] + [vp] * 3 + [code, code, vp]
+    lib.hdt_gate_norm_bwd_workspace_bytes.argtypes = [i64, i32]
+    lib.hdt_gate_norm_bwd.argtypes = [vp] * 9 + [i64, i32, f32, i32] + [vp] * 7 + [code, code, vp, size, vp]
+    for f in (lib.hdt_rel_table, lib.hdt_rel_attn_fwd, lib.hdt_rel_attn_bwd, lib.hdt_dropout_add, lib.hdt_add_norm_fwd, lib.hdt_add_norm_bwd,
+              lib.hdt_embed_fwd, lib.hdt_embed_bwd, lib.hdt_ffn_fwd, lib.hdt_ffn_bwd, lib.hdt_gate_norm_fwd, lib.hdt_gate_norm_bwd):
         f.restype = code
-    for f in (lib.hdt_rel_attn_fwd_workspace_bytes, lib.hdt_rel_attn_bwd_workspace_bytes, lib.hdt_add_norm_bwd_workspace_bytes):
+    for f in (lib.hdt_rel_attn_fwd_workspace_bytes, lib.hdt_rel_attn_bwd_workspace_bytes, lib.hdt_add_norm_bwd_workspace_bytes,
+              lib.hdt_embed_bwd_workspace_bytes, lib.hdt_ffn_fwd_workspace_bytes, lib.hdt_ffn_bwd_workspace_bytes, lib.hdt_gate_norm_bwd_workspace_bytes):
         f.restype = size
     _calls = _native_calls(lib, str(torch.__version__))
     _lib = lib  # the last step: whoever sees it, in another thread too, uses _calls
@@ -791,3 +808,240 @@ def hdt_add_norm_bwd(dn, h, weight, mean, rstd, dh=None, p: float = 0.0, rng=Non
     if not dropped and dy.data_ptr() != dx.data_ptr():
         hdt_dropout_add(dx, 0.0, out=dy, stream=stream)
     return dx, dy, dweight, dbias
+
+
+def _check_ids(ids):
+    import torch
+    if ids.dtype != torch.int32 or not (ids.is_cuda and ids.is_contiguous()):
+        raise ValueError("ids must be a contiguous int32 device tensor")
+
+
+def _check_table(t, vocab, width, name):
+    if t.dim() != 2 or tuple(t.shape) != (vocab, width) or not (t.is_cuda and t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous device tensor [vocab][width] ({vocab}, {width})")
+
+
+def hdt_embed_fwd(ids, table, scale: float = 1.0, dtype=None, out=None, stream=None):
+    """scale * table[ids] (hdt_embed_fwd in include/hdt.h); ids outside the table give rows of 0.  ids: int32, of any shape; table [vocab][width];
+    ``dtype``: of the result (None: the table's).  Returns out [*ids.shape][width]."""
+    if _lib is None:
+        load_library()
+    r = _calls.embed_fwd(ids, table, scale, dtype, out, None if stream is None else stream.cuda_stream)
+    if r is not None:
+        if r.__class__ is not int:
+            return r
+        _check(r)
+    import torch
+    _check_ids(ids)
+    if table.dim() != 2:
+        raise ValueError("table must be [vocab][width]")
+    vocab, width = table.shape
+    _check_table(table, vocab, width, "table")
+    _int32("a size of", vocab), _int32("a width of", width)
+    if out is None:
+        out = torch.empty((*ids.shape, width), dtype=dtype or table.dtype, device=table.device)
+    if out.shape != (*ids.shape, width) or (dtype is not None and out.dtype != dtype) or not (out.is_cuda and out.is_contiguous()):
+        raise ValueError(f"out must be a contiguous device tensor {(*ids.shape, width)} of {dtype or 'bf16 or fp32'}")
+    _same_device((ids, table, out))
+    _check(_lib.hdt_embed_fwd(_ptr(ids), ids.numel(), _ptr(table), vocab, width, float(scale), _ptr(out), _dtype_code(table), _dtype_code(out),
+                              _stream_ptr(stream)))
+    return out
+
+
+def hdt_embed_bwd(d_out, ids, vocab: int, scale: float = 1.0, dtype=None, grad=None, accumulate: bool = False, workspace=None, stream=None):
+    """The gradient of hdt_embed_fwd's table, [vocab][width] of ``dtype`` (None: d_out's).  ``accumulate``: added to what stands in ``grad``.  Returns
+    grad."""
+    if _lib is None:
+        load_library()
+    r = _calls.embed_bwd(d_out, ids, vocab, scale, dtype, grad, accumulate, workspace, None if stream is None else stream.cuda_stream)
+    if r is not None:
+        if r.__class__ is not int:
+            return r
+        _check(r)
+    import torch
+    _check_ids(ids)
+    vocab = _int32("vocab", vocab)
+    if d_out.dim() < 1 or d_out.shape[:-1] != ids.shape or not (d_out.is_cuda and d_out.is_contiguous()):
+        raise ValueError("d_out must be a contiguous device tensor [*ids.shape][width]")
+    width = _int32("a width of", d_out.shape[-1])
+    if grad is None:
+        if accumulate:
+            raise ValueError("accumulate needs a grad to add to")
+        if vocab < 0:
+            raise ValueError(f"vocab {vocab} is negative")
+        grad = torch.empty((vocab, width), dtype=dtype or d_out.dtype, device=d_out.device)
+    _check_table(grad, vocab, width, "grad")
+    if dtype is not None and grad.dtype != dtype:
+        raise ValueError(f"grad must be of {dtype}")
+    _check_workspace(workspace)
+    _same_device((d_out, ids, grad, workspace))
+    if workspace is None:
+        workspace = _scratch(_lib.hdt_embed_bwd_workspace_bytes(ids.numel(), width), d_out.device, stream)
+    _check(_lib.hdt_embed_bwd(_ptr(d_out), _ptr(ids), ids.numel(), vocab, width, float(scale), int(bool(accumulate)), _ptr(grad), _dtype_code(grad),
+                              _dtype_code(d_out), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+    return grad
+
+
+_ACTS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
+
+
+def _act_code(act):
+    if act not in _ACTS:
+        raise ValueError(f"act must be one of {sorted(_ACTS)}, not {act!r}")
+    return _ACTS[act]
+
+
+def _check_ffn(x, w_gate, w_up, w_down):
+    if x.dim() < 1 or w_gate.dim() != 2:
+        raise ValueError("x must be [..][width], w_gate and w_up [inner][width], w_down [width][inner]")
+    inner, width = w_gate.shape
+    for t, shape in ((w_gate, (inner, width)), (w_up, (inner, width)), (w_down, (width, inner))):
+        if tuple(t.shape) != shape:
+            raise ValueError(f"w_gate and w_up must be [inner][width], w_down [width][inner]: {tuple(t.shape)} is not {shape}")
+    if x.shape[-1] != width:
+        raise ValueError(f"rows of {x.shape[-1]} do not fit weights of width {width}")
+    for t in (x, w_gate, w_up, w_down):
+        if t.dtype != x.dtype or not (t.is_cuda and t.is_contiguous()):
+            raise ValueError(f"tensors must be contiguous device tensors of {x.dtype}")
+    _int32("a width of", width), _int32("an inner size of", inner)
+    return x.shape[:-1].numel(), width, inner
+
+
+def _check_results(ts, shape, like):
+    for t in ts:
+        if t.shape != shape or t.dtype != like.dtype or not (t.is_cuda and t.is_contiguous()):
+            raise ValueError(f"tensors must be contiguous device tensors {tuple(shape)} of {like.dtype}")
+
+
+def hdt_ffn_fwd(x, w_gate, w_up, w_down, act: str = "silu", train: bool = True, y=None, by_gate=None, by_up=None, hidden=None, workspace=None, stream=None):
+    """Gated feed-forward block (hdt_ffn_fwd in include/hdt.h): y = (act(x w_gate^T) * (x w_up^T)) w_down^T.  x [..][width], w_gate, w_up
+    [inner][width], w_down [width][inner]; act: "silu", "gelu" or "gelu_tanh".  Returns (y, by_gate, by_up, hidden), the last three [..][inner] for
+    hdt_ffn_bwd (the derivatives of hidden = act(..) * (..) by its two factors' products, and hidden), or None with ``train=False``."""
+    if _lib is None:
+        load_library()
+    r = _calls.ffn_fwd(x, w_gate, w_up, w_down, act, train, y, by_gate, by_up, hidden, workspace, None if stream is None else stream.cuda_stream)
+    if r.__class__ is tuple:
+        return r if len(r) == 4 else (*r, None, None, None)
+    if r is not None:
+        _check(r)
+    import torch
+    code = _act_code(act)
+    rows, width, inner = _check_ffn(x, w_gate, w_up, w_down)
+    y = torch.empty_like(x) if y is None else y
+    _check_results((y,), x.shape, x)
+    kept = (by_gate, by_up, hidden)
+    if train:
+        shape = torch.Size((*x.shape[:-1], inner))
+        kept = tuple(torch.empty(shape, dtype=x.dtype, device=x.device) if t is None else t for t in kept)
+        _check_results(kept, shape, x)
+    elif any(t is not None for t in kept):
+        raise ValueError("by_gate, by_up and hidden are results of a call with train=True")
+    _check_workspace(workspace)
+    _same_device((x, w_gate, w_up, w_down, y, workspace, *kept))
+    if workspace is None:
+        need = _lib.hdt_ffn_fwd_workspace_bytes(rows, width, inner, int(bool(train)), _dtype_code(x))
+        workspace = _scratch(need, x.device, stream) if need else None
+    nbytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _check(_lib.hdt_ffn_fwd(_ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), rows, width, inner, code, _ptr(y), *(_ptr(t) for t in kept), _dtype_code(x),
+                            _ptr(workspace), nbytes, _stream_ptr(stream)))
+    return (y, *kept)
+
+
+def hdt_ffn_bwd(dy, x, w_gate, w_up, w_down, by_gate, by_up, hidden, dx=None, dw_gate=None, dw_up=None, dw_down=None, workspace=None, stream=None):
+    """The gradients of hdt_ffn_fwd from dy and what the forward kept: (dx, dw_gate, dw_up, dw_down), like x and the weights."""
+    if _lib is None:
+        load_library()
+    r = _calls.ffn_bwd(dy, x, w_gate, w_up, w_down, by_gate, by_up, hidden, dx, dw_gate, dw_up, dw_down, workspace, None if stream is None else stream.cuda_stream)
+    if r.__class__ is tuple:
+        return r
+    if r is not None:
+        _check(r)
+    import torch
+    rows, width, inner = _check_ffn(x, w_gate, w_up, w_down)
+    dx = torch.empty_like(x) if dx is None else dx
+    dw_gate, dw_up, dw_down = (torch.empty_like(w) if g is None else g for g, w in ((dw_gate, w_gate), (dw_up, w_up), (dw_down, w_down)))
+    _check_results((dy, dx), x.shape, x)
+    _check_results((by_gate, by_up, hidden), torch.Size((*x.shape[:-1], inner)), x)
+    _check_results((dw_gate, dw_up), w_gate.shape, x)
+    _check_results((dw_down,), w_down.shape, x)
+    _check_workspace(workspace)
+    _same_device((dy, x, w_gate, w_up, w_down, by_gate, by_up, hidden, dx, dw_gate, dw_up, dw_down, workspace))
+    if workspace is None:
+        workspace = _scratch(_lib.hdt_ffn_bwd_workspace_bytes(rows, width, inner, _dtype_code(x)), x.device, stream)
+    _check(_lib.hdt_ffn_bwd(_ptr(dy), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(by_gate), _ptr(by_up), _ptr(hidden), rows, width, inner,
+                            _ptr(dx), _ptr(dw_gate), _ptr(dw_up), _ptr(dw_down), _dtype_code(x), _ptr(workspace),
+                            workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+    return dx, dw_gate, dw_up, dw_down
+
+
+def _check_gate_norm(x, weight, vectors, stats):
+    import torch
+    if x.dim() < 1:
+        raise ValueError("tensors must have a last dimension")
+    rows = x.shape[:-1].numel()
+    _int32("a width of", x.shape[-1])
+    for w in (weight, *vectors):
+        if w is not None and (w.shape != x.shape[-1:] or w.dtype != weight.dtype or not (w.is_cuda and w.is_contiguous())):
+            raise ValueError("weights, biases and gate must be contiguous device tensors [width] of one dtype")
+    if stats.shape != (4, *x.shape[:-1]) or stats.dtype != torch.float32 or not (stats.is_cuda and stats.is_contiguous()):
+        raise ValueError("stats must be a contiguous float32 device tensor [4][rows]")
+    return rows
+
+
+def hdt_gate_norm_fwd(x, y, post_weight, weight, gate=None, post_bias=None, bias=None, scale: float = 1.0, eps: float = 1e-5, rms: bool = False, h=None,
+                      n=None, stats=None, stream=None):
+    """c = norm(y; post_weight, post_bias), h = scale x + gate * c, n = norm(h; weight, bias) over the last dimension (hdt_gate_norm_fwd in
+    include/hdt.h); ``rms``: norms without means.  Returns (n, h, stats)."""
+    if _lib is None:
+        load_library()
+    r = _calls.gate_norm_fwd(x, y, post_weight, weight, gate, post_bias, bias, scale, eps, rms, h, n, stats, None if stream is None else stream.cuda_stream)
+    if r.__class__ is tuple:
+        return r
+    if r is not None:
+        _check(r)
+    import torch
+    h = torch.empty_like(x) if h is None else h
+    n = torch.empty_like(x) if n is None else n
+    stats = torch.empty((4, *x.shape[:-1]), dtype=torch.float32, device=x.device) if stats is None else stats
+    _check_like(x, (x, y, h, n))
+    rows = _check_gate_norm(x, weight, (post_weight, gate, post_bias, bias), stats)
+    _same_device((x, y, post_weight, weight, gate, post_bias, bias, h, n, stats))
+    _check(_lib.hdt_gate_norm_fwd(_ptr(x), _ptr(y), _ptr(post_weight), _ptr(post_bias), _ptr(gate), _ptr(weight), _ptr(bias), rows, x.shape[-1], float(eps),
+                                  float(scale), int(bool(rms)), _ptr(h), _ptr(n), _ptr(stats), _dtype_code(x), _dtype_code(weight), _stream_ptr(stream)))
+    return n, h, stats
+
+
+def hdt_gate_norm_bwd(dn, h, y, stats, post_weight, weight, gate=None, post_bias=None, bias: bool = False, dh=None, scale: float = 1.0, rms: bool = False,
+                      dx=None, dy=None, dpost_weight=None, dweight=None, dgate=None, dpost_bias=None, dbias=None, workspace=None, stream=None):
+    """Gradients of hdt_gate_norm_fwd from dn (that of n) and dh (that of h from elsewhere, or None); ``bias``: whether the forward had one.
+    Returns (dx, dy, dpost_weight, dweight, dgate, dpost_bias, dbias), the last three None where the forward had no such vector."""
+    if _lib is None:
+        load_library()
+    r = _calls.gate_norm_bwd(dn, h, y, stats, post_weight, weight, gate, post_bias, bias, dh, scale, rms, dx, dy, dpost_weight, dweight, dgate, dpost_bias, dbias,
+                             workspace, None if stream is None else stream.cuda_stream)
+    if r.__class__ is tuple:
+        return r
+    if r is not None:
+        _check(r)
+    import torch
+    dx = torch.empty_like(h) if dx is None else dx
+    dy = torch.empty_like(h) if dy is None else dy
+    dpost_weight = torch.empty_like(post_weight) if dpost_weight is None else dpost_weight
+    dweight = torch.empty_like(weight) if dweight is None else dweight
+    for name, there, g in (("gate", gate is not None, dgate), ("post_bias", post_bias is not None, dpost_bias), ("bias", bool(bias), dbias)):
+        if g is not None and not there:
+            raise ValueError(f"a gradient of {name}, which the forward did not have")
+    dgate = torch.empty_like(gate) if gate is not None and dgate is None else dgate
+    dpost_bias = torch.empty_like(post_bias) if post_bias is not None and dpost_bias is None else dpost_bias
+    dbias = torch.empty_like(weight) if bias and dbias is None else dbias
+    _check_like(h, (h, y, dn, dh, dx, dy))
+    rows = _check_gate_norm(h, weight, (post_weight, gate, post_bias, dpost_weight, dweight, dgate, dpost_bias, dbias), stats)
+    _check_workspace(workspace)
+    _same_device((dn, h, y, stats, post_weight, weight, gate, post_bias, dh, dx, dy, dpost_weight, dweight, dgate, dpost_bias, dbias, workspace))
+    if workspace is None:
+        workspace = _scratch(_lib.hdt_gate_norm_bwd_workspace_bytes(rows, h.shape[-1]), h.device, stream)
+    _check(_lib.hdt_gate_norm_bwd(_ptr(dn), _ptr(dh), _ptr(h), _ptr(y), _ptr(stats), _ptr(post_weight), _ptr(post_bias), _ptr(gate), _ptr(weight), rows,
+                                  h.shape[-1], float(scale), int(bool(rms)), _ptr(dx), _ptr(dy), _ptr(dpost_weight), _ptr(dpost_bias), _ptr(dgate),
+                                  _ptr(dweight), _ptr(dbias), _dtype_code(h), _dtype_code(weight), _ptr(workspace),
+                                  workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+    return dx, dy, dpost_weight, dweight, dgate, dpost_bias, dbias

@@ -19,10 +19,11 @@
 #include "hdt_internal.h"
 #include "hdt_lanes.h"
 #include "hdt_mfma.h"
+#include "hdt_rows.h"
 
 namespace {
 
-typedef __attribute__((ext_vector_type(4))) float f32x4;
+using namespace hdt_rows;
 
 struct Drop {
     const long long *rng;  // device: seed, step
@@ -83,54 +84,6 @@ __device__ __forceinline__ float factor(const Block &b, int e, const Drop &d)
     return u >= d.threshold ? d.keep_scale : 0.f;
 }
 
-// 8 consecutive elements as they are in memory; `left` of them exist (WHOLE: all).  The address is aligned to an element only.
-template <typename T>
-struct Vec {
-    typedef T V __attribute__((ext_vector_type(8)));
-    typedef V Any __attribute__((aligned(sizeof(T))));
-};
-template <bool WHOLE, typename T>
-__device__ __forceinline__ typename Vec<T>::V load8(const T *p, int left)
-{
-    if (WHOLE || left >= 8) return *reinterpret_cast<const typename Vec<T>::Any *>(p);
-    typename Vec<T>::V r;
-#pragma unroll
-    for (int e = 0; e < 8; e++) r[e] = e < left ? p[e] : (T)0.f;
-    return r;
-}
-struct Eight {
-    float x[8];
-};
-template <bool WHOLE, typename T>
-__device__ __forceinline__ void store8(T *p, const Eight &r, int left)
-{
-    if (WHOLE || left >= 8) {
-        typename Vec<T>::V v;
-#pragma unroll
-        for (int e = 0; e < 8; e++) v[e] = (T)r.x[e];
-        *reinterpret_cast<typename Vec<T>::Any *>(p) = v;
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; e++)
-        if (e < left) p[e] = (T)r.x[e];
-}
-template <bool WHOLE>
-__device__ __forceinline__ Eight load_weight(const void *p, int bf16, int at, int left)
-{
-    Eight r;
-    if (bf16) {
-        const auto v = load8<WHOLE>((const __bf16 *)p + at, left);
-#pragma unroll
-        for (int e = 0; e < 8; e++) r.x[e] = (float)v[e];
-    } else {
-        const auto v = load8<WHOLE>((const float *)p + at, left);
-#pragma unroll
-        for (int e = 0; e < 8; e++) r.x[e] = v[e];
-    }
-    return r;
-}
-
 // ------------------------------------------------------------------------------------------ dropout + residual
 template <typename T>
 __global__ __launch_bounds__(256) void k_dropout_add(const T *y, const T *x, T *out, unsigned long long n, Drop d)
@@ -154,23 +107,7 @@ __global__ __launch_bounds__(256) void k_dropout_add(const T *y, const T *x, T *
     }
 }
 
-// ------------------------------------------------------------------------------------------ sums over a row
-// the sum over the threads of a row: a wave, or (TPR > 64) the whole workgroup
-template <int TPR>
-__device__ __forceinline__ float row_sum(float x, float *lds)
-{
-    x = hdt_lanes::wave_sum(x);
-    if (TPR > 64) {
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
-        __syncthreads();
-        x = 0.f;
-#pragma unroll
-        for (int i = 0; i < TPR / 64; i++) x += lds[i];
-    }
-    return x;
-}
-
+// ------------------------------------------------------------------------------------------ norms
 struct NormArgs {
     const void *x, *y, *weight, *bias, *dn, *dh, *h;
     void *h_out, *n, *dx, *dy, *d_weight, *d_bias;

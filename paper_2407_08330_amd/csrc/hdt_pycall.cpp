@@ -1,5 +1,5 @@
 // The calls that every layer of a model makes, for Python: hdt_build_layout, hdt_attn_fwd and hdt_attn_bwd, the relative-bias
-// attention, dropout and norm, on plain torch tensors.  Checks, output tensors, addresses, stream and the call into libhdt in one piece of native code.
+// attention, dropout, norms, embeddings and the feed-forward block, on plain torch tensors.  Checks, output tensors, addresses, stream and the call into libhdt in one piece of native code.
 //
 // A layer of a thousand positions is bound by the host: its kernels take 8 us each, and a call from the interpreter took 8.1 us
 // (forward: two outputs 3.0, the launch 3.0, checks 1.0, ctypes 0.7), 11.5 (backward) and 6.7 (deferred build with its
@@ -12,6 +12,7 @@
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "hdt.h"
@@ -31,6 +32,16 @@ decltype(&hdt_dropout_add) dropout_fn;
 decltype(&hdt_add_norm_fwd) norm_fwd_fn;
 decltype(&hdt_add_norm_bwd_workspace_bytes) norm_bwd_bytes_fn;
 decltype(&hdt_add_norm_bwd) norm_bwd_fn;
+decltype(&hdt_embed_fwd) embed_fwd_fn;
+decltype(&hdt_embed_bwd_workspace_bytes) embed_bwd_bytes_fn;
+decltype(&hdt_embed_bwd) embed_bwd_fn;
+decltype(&hdt_ffn_fwd_workspace_bytes) ffn_fwd_bytes_fn;
+decltype(&hdt_ffn_fwd) ffn_fwd_fn;
+decltype(&hdt_ffn_bwd_workspace_bytes) ffn_bwd_bytes_fn;
+decltype(&hdt_ffn_bwd) ffn_bwd_fn;
+decltype(&hdt_gate_norm_fwd) gate_norm_fwd_fn;
+decltype(&hdt_gate_norm_bwd_workspace_bytes) gate_norm_bwd_bytes_fn;
+decltype(&hdt_gate_norm_bwd) gate_norm_bwd_fn;
 
 // What is not plain is refused by return values: a C++ exception takes 1.5 us, and the calls that the general path takes then
 // pay for it (us, no native form - refused by an exception - by return values: forward with a numpy scale 9.0 - 10.8 - 9.1, backward
@@ -526,15 +537,281 @@ PyObject *add_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- embeddings, feed-forward block, norms around a block: the same rules ----
+// None, or a torch dtype
+bool dtype_or_none(PyObject *o, bool *given, at::ScalarType *t)
+{
+    *given = o != Py_None;
+    if (!*given) return true;
+    if (!THPDtype_Check(o)) return false;
+    *t = ((THPDtype *)o)->scalar_type;
+    return true;
+}
+bool is_ids(const at::Tensor *t, int device) { return t && here(*t, device) && t->scalar_type() == at::kInt && t->is_contiguous(); }
+// the shape of ids with a last dimension
+c10::SmallVector<int64_t, 6> with_last(at::IntArrayRef lead, int64_t width)
+{
+    c10::SmallVector<int64_t, 6> s(lead.begin(), lead.end());
+    s.push_back(width);
+    return s;
+}
+
+// (ids, table, scale, dtype, out, stream) -> out, a status, or None
+PyObject *embed_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 6) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject * {
+        const int device = c10::hip::current_device();
+        const at::Tensor *ids = plain(a[0]), *table = plain(a[1]), *given;
+        double scale;
+        bool typed;
+        at::ScalarType type;
+        hdt_dtype_t dt, tdt;
+        hipStream_t st;
+        if (!is_ids(ids, device) || !table || !here(*table, device) || table->dim() != 2 || !table->is_contiguous() || !dtype_of(*table, &tdt) || !number(a[2], &scale) ||
+            !dtype_or_none(a[3], &typed, &type) || !optional(a[4], device, &given) || !stream_of(a[5], &st) || table->size(0) > INT32_MAX || table->size(1) > INT32_MAX)
+            return nullptr;
+        const auto shape = with_last(ids->sizes(), table->size(1));
+        if (given && (given->sizes() != at::IntArrayRef(shape) || !given->is_contiguous() || (typed && given->scalar_type() != type))) return nullptr;
+        if (!given && typed && type != at::kBFloat16 && type != at::kFloat) return nullptr;
+        at::Tensor out = given ? *given : at::empty(shape, typed ? table->options().dtype(type) : table->options());
+        if (!dtype_of(out, &dt)) return nullptr;
+        const int32_t *pi = (const int32_t *)ids->data_ptr();
+        const void *pt = table->data_ptr();
+        void *po = out.data_ptr();
+        const int64_t tokens = ids->numel();
+        const int32_t vocab = (int32_t)table->size(0), width = (int32_t)table->size(1);
+        hdt_status_t s;
+        Py_BEGIN_ALLOW_THREADS
+        s = embed_fwd_fn(pi, tokens, pt, vocab, width, (float)scale, po, tdt, dt, st);
+        Py_END_ALLOW_THREADS
+        return s != HDT_OK ? PyLong_FromLong(s) : THPVariable_Wrap(out);
+    });
+}
+
+// (d_out, ids, vocab, scale, dtype, grad, accumulate, workspace, stream) -> grad, a status, or None
+PyObject *embed_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 9) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject * {
+        const int device = c10::hip::current_device();
+        const at::Tensor *d = plain(a[0]), *ids = plain(a[1]), *given;
+        double scale;
+        int32_t vocab;
+        bool typed;
+        at::ScalarType type;
+        hdt_dtype_t dt, tdt;
+        hipStream_t st;
+        if (!d || !here(*d, device) || !d->is_contiguous() || !dtype_of(*d, &dt) || !is_ids(ids, device) || !whole32(a[2], &vocab) || vocab < 0 || !number(a[3], &scale) ||
+            !dtype_or_none(a[4], &typed, &type) || !optional(a[5], device, &given) || !PyBool_Check(a[6]) || (!given && a[6] == Py_True) ||
+            !workspace_ok(a[7], a[8], device) || !stream_of(a[8], &st))
+            return nullptr;
+        if (d->dim() < 1 || d->size(-1) > INT32_MAX || d->sizes().slice(0, d->dim() - 1) != ids->sizes()) return nullptr;
+        const int64_t tokens = ids->numel(), width = d->size(-1);
+        if (given && (given->dim() != 2 || given->size(0) != vocab || given->size(1) != width || !given->is_contiguous() || (typed && given->scalar_type() != type)))
+            return nullptr;
+        if (!given && typed && type != at::kBFloat16 && type != at::kFloat) return nullptr;
+        at::Tensor grad = given ? *given : at::empty({vocab, width}, typed ? d->options().dtype(type) : d->options());
+        if (!dtype_of(grad, &tdt)) return nullptr;
+        const Room w(a[7], embed_bwd_bytes_fn(tokens, (int32_t)width), *d);
+        const void *pd = d->data_ptr();
+        const int32_t *pi = (const int32_t *)ids->data_ptr();
+        void *pg = grad.data_ptr();
+        hdt_status_t s;
+        Py_BEGIN_ALLOW_THREADS
+        s = embed_bwd_fn(pd, pi, tokens, vocab, (int32_t)width, (float)scale, a[6] == Py_True, pg, tdt, dt, w.at_, w.bytes, st);
+        Py_END_ALLOW_THREADS
+        return s != HDT_OK ? PyLong_FromLong(s) : THPVariable_Wrap(grad);
+    });
+}
+
+// what feed-forward calls have in common: rows of x, three weights
+struct FfnCall {
+    const at::Tensor *x, *wg, *wu, *wd;
+    int64_t rows;
+    int32_t width, inner;
+    hdt_act_t act = HDT_SILU;
+    hdt_dtype_t dt;
+    int device;
+    // x, w_gate, w_up, w_down
+    bool plain_case(PyObject *const *a)
+    {
+        device = c10::hip::current_device();
+        if (!(x = plain(a[0])) || !(wg = plain(a[1])) || !(wu = plain(a[2])) || !(wd = plain(a[3])) || !dtype_of(*x, &dt)) return false;
+        for (const at::Tensor *t : {x, wg, wu, wd})
+            if (!here(*t, device) || t->scalar_type() != x->scalar_type() || !t->is_contiguous()) return false;
+        if (x->dim() < 1 || wg->dim() != 2 || wd->dim() != 2 || wu->sizes() != wg->sizes()) return false;
+        const int64_t f = wg->size(0), d = wg->size(1);
+        if (x->size(-1) != d || wd->size(0) != d || wd->size(1) != f || d > INT32_MAX || f > INT32_MAX || d == 0) return false;
+        width = (int32_t)d, inner = (int32_t)f, rows = x->numel() / d;
+        return true;
+    }
+    bool activation(PyObject *name)
+    {
+        if (!PyUnicode_CheckExact(name)) return false;
+        if (PyUnicode_CompareWithASCIIString(name, "silu") == 0) act = HDT_SILU;
+        else if (PyUnicode_CompareWithASCIIString(name, "gelu") == 0) act = HDT_GELU;
+        else if (PyUnicode_CompareWithASCIIString(name, "gelu_tanh") == 0) act = HDT_GELU_TANH;
+        else return false;
+        return true;
+    }
+    // None or a tensor of x's type: like x, or [..][inner]
+    bool result(PyObject *o, const at::Tensor **t, at::IntArrayRef shape) const
+    {
+        return optional(o, device, t) && (!*t || ((*t)->scalar_type() == x->scalar_type() && (*t)->is_contiguous() && (*t)->sizes() == shape));
+    }
+    c10::SmallVector<int64_t, 6> kept() const { return with_last(x->sizes().slice(0, x->dim() - 1), inner); }
+};
+
+// (x, w_gate, w_up, w_down, act, train, y, by_gate, by_up, hidden, workspace, stream) -> (y, by_gate, by_up, hidden), (y,) without train, a status, or None
+PyObject *ffn_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 12) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject * {
+        FfnCall c;
+        hipStream_t st;
+        const at::Tensor *gy, *g[3];
+        if (!c.plain_case(a) || !c.activation(a[4]) || !PyBool_Check(a[5]) || !c.result(a[6], &gy, c.x->sizes()) || !workspace_ok(a[10], a[11], c.device) || !stream_of(a[11], &st)) return nullptr;
+        const bool train = a[5] == Py_True;
+        const auto shape = c.kept();
+        for (int i = 0; i < 3; i++)
+            if (!c.result(a[7 + i], &g[i], shape) || (g[i] && !train)) return nullptr;
+        at::Tensor y = gy ? *gy : at::empty(c.x->sizes(), c.x->options()), k[3];
+        void *pk[3] = {};
+        if (train)
+            for (int i = 0; i < 3; i++) {
+                k[i] = g[i] ? *g[i] : at::empty(shape, c.x->options());
+                pk[i] = k[i].data_ptr();
+            }
+        const Room w(a[10], ffn_fwd_bytes_fn(c.rows, c.width, c.inner, train, c.dt), *c.x);
+        const void *px = c.x->data_ptr(), *pg = c.wg->data_ptr(), *pu = c.wu->data_ptr(), *pd = c.wd->data_ptr();
+        void *py = y.data_ptr();
+        hdt_status_t s;
+        Py_BEGIN_ALLOW_THREADS
+        s = ffn_fwd_fn(px, pg, pu, pd, c.rows, c.width, c.inner, c.act, py, pk[0], pk[1], pk[2], c.dt, w.at_, w.bytes, st);
+        Py_END_ALLOW_THREADS
+        return train ? results(s, {y, k[0], k[1], k[2]}) : results(s, {y});
+    });
+}
+
+// (dy, x, w_gate, w_up, w_down, by_gate, by_up, hidden, dx, dw_gate, dw_up, dw_down, workspace, stream) -> (dx, dw_gate, dw_up, dw_down), a
+// status, or None
+PyObject *ffn_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 14) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject * {
+        FfnCall c;
+        hipStream_t st;
+        const at::Tensor *dy, *kept[3], *g[4];
+        if (!c.plain_case(a + 1) || !c.result(a[0], &dy, c.x->sizes()) || !dy || !workspace_ok(a[12], a[13], c.device) || !stream_of(a[13], &st)) return nullptr;
+        const auto shape = c.kept();
+        for (int i = 0; i < 3; i++)
+            if (!c.result(a[5 + i], &kept[i], shape) || !kept[i]) return nullptr;
+        const at::Tensor *like_[4] = {c.x, c.wg, c.wu, c.wd};
+        at::Tensor out[4];
+        for (int i = 0; i < 4; i++) {
+            if (!c.result(a[8 + i], &g[i], like_[i]->sizes())) return nullptr;
+        }
+        for (int i = 0; i < 4; i++) out[i] = g[i] ? *g[i] : at::empty(like_[i]->sizes(), c.x->options());
+        const Room w(a[12], ffn_bwd_bytes_fn(c.rows, c.width, c.inner, c.dt), *c.x);
+        const void *p[8] = {dy->data_ptr(), c.x->data_ptr(), c.wg->data_ptr(), c.wu->data_ptr(), c.wd->data_ptr(), kept[0]->data_ptr(), kept[1]->data_ptr(), kept[2]->data_ptr()};
+        void *o[4] = {out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), out[3].data_ptr()};
+        hdt_status_t s;
+        Py_BEGIN_ALLOW_THREADS
+        s = ffn_bwd_fn(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], c.rows, c.width, c.inner, o[0], o[1], o[2], o[3], c.dt, w.at_, w.bytes, st);
+        Py_END_ALLOW_THREADS
+        return results(s, {out[0], out[1], out[2], out[3]});
+    });
+}
+
+bool is_stats(const at::Tensor &t, const at::Tensor &x, int device)
+{
+    return here(t, device) && t.scalar_type() == at::kFloat && t.is_contiguous() && t.dim() == x.dim() && t.size(0) == 4 && t.sizes().slice(1) == x.sizes().slice(0, x.dim() - 1);
+}
+
+// (x, y, post_weight, weight, gate, post_bias, bias, scale, eps, rms, h, n, stats, stream) -> (n, h, stats), a status, or None
+PyObject *gate_norm_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 14) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject * {
+        NormCall c;
+        const at::Tensor *y = plain(a[1]), *pw = plain(a[2]), *v[3], *g[2], *gs;
+        double scale, eps;
+        hipStream_t st;
+        if (!c.plain_case(a[0], a[3]) || !y || !here(*y, c.device) || !like(*y, *c.x) || !pw || !here(*pw, c.device) || !like(*pw, *c.weight) || !number(a[7], &scale) ||
+            !number(a[8], &eps) || !PyBool_Check(a[9]) || !optional(a[12], c.device, &gs) || (gs && !is_stats(*gs, *c.x, c.device)) || !stream_of(a[13], &st))
+            return nullptr;
+        for (int i = 0; i < 3; i++)
+            if (!optional(a[4 + i], c.device, &v[i]) || (v[i] && !like(*v[i], *c.weight))) return nullptr;
+        for (int i = 0; i < 2; i++)
+            if (!optional(a[10 + i], c.device, &g[i]) || (g[i] && !like(*g[i], *c.x))) return nullptr;
+        at::Tensor h = g[0] ? *g[0] : at::empty(c.x->sizes(), c.x->options()), out = g[1] ? *g[1] : at::empty(c.x->sizes(), c.x->options()), stats;
+        if (gs) {
+            stats = *gs;
+        } else {
+            c10::SmallVector<int64_t, 6> shape = {4};
+            const auto lead = c.x->sizes().slice(0, c.x->dim() - 1);
+            shape.append(lead.begin(), lead.end());
+            stats = at::empty(shape, c.x->options().dtype(at::kFloat));
+        }
+        const void *px = c.x->data_ptr(), *py = y->data_ptr(), *pp = pw->data_ptr(), *pw_ = c.weight->data_ptr(), *pg = data(v[0]), *pb = data(v[1]), *pc = data(v[2]);
+        void *ph = h.data_ptr(), *pn = out.data_ptr();
+        float *ps = (float *)stats.data_ptr();
+        hdt_status_t s;
+        Py_BEGIN_ALLOW_THREADS
+        s = gate_norm_fwd_fn(px, py, pp, pb, pg, pw_, pc, c.rows, c.width, (float)eps, (float)scale, a[9] == Py_True, ph, pn, ps, c.dt, c.wdt, st);
+        Py_END_ALLOW_THREADS
+        return results(s, {out, h, stats});
+    });
+}
+
+// (dn, h, y, stats, post_weight, weight, gate, post_bias, bias, dh, scale, rms, dx, dy, dpost_weight, dweight, dgate, dpost_bias, dbias, workspace,
+// stream) -> (dx, dy, dpost_weight, dweight, dgate, dpost_bias, dbias), a status, or None
+PyObject *gate_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 21) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject * {
+        NormCall c;
+        const at::Tensor *dn = plain(a[0]), *y = plain(a[2]), *stats = plain(a[3]), *pw = plain(a[4]), *gate, *pb, *dh, *g[7];
+        double scale;
+        hipStream_t st;
+        if (!c.plain_case(a[1], a[5]) || !dn || !here(*dn, c.device) || !like(*dn, *c.x) || !y || !here(*y, c.device) || !like(*y, *c.x) || !stats || !is_stats(*stats, *c.x, c.device) ||
+            !pw || !here(*pw, c.device) || !like(*pw, *c.weight) || !optional(a[6], c.device, &gate) || (gate && !like(*gate, *c.weight)) || !optional(a[7], c.device, &pb) ||
+            (pb && !like(*pb, *c.weight)) || !PyBool_Check(a[8]) || !optional(a[9], c.device, &dh) || (dh && !like(*dh, *c.x)) || !number(a[10], &scale) || !PyBool_Check(a[11]) ||
+            !workspace_ok(a[19], a[20], c.device) || !stream_of(a[20], &st))
+            return nullptr;
+        const bool there[7] = {true, true, true, true, gate != nullptr, pb != nullptr, a[8] == Py_True};
+        for (int i = 0; i < 7; i++)
+            if (!optional(a[12 + i], c.device, &g[i]) || (g[i] && (!there[i] || !like(*g[i], i < 2 ? *c.x : *c.weight)))) return nullptr;
+        at::Tensor out[7];
+        void *po[7] = {};
+        for (int i = 0; i < 7; i++) {
+            if (!there[i]) continue;
+            const at::Tensor &as = i < 2 ? *c.x : *c.weight;
+            out[i] = g[i] ? *g[i] : at::empty(as.sizes(), as.options());
+            po[i] = out[i].data_ptr();
+        }
+        const Room w(a[19], gate_norm_bwd_bytes_fn(c.rows, c.width), *c.x);
+        const void *pn = dn->data_ptr(), *pd = data(dh), *ph = c.x->data_ptr(), *py = y->data_ptr(), *pp = pw->data_ptr(), *pq = data(pb), *pg = data(gate), *pw_ = c.weight->data_ptr();
+        const float *ps = (const float *)stats->data_ptr();
+        hdt_status_t s;
+        Py_BEGIN_ALLOW_THREADS
+        s = gate_norm_bwd_fn(pn, pd, ph, py, ps, pp, pq, pg, pw_, c.rows, c.width, (float)scale, a[11] == Py_True, po[0], po[1], po[2], po[5], po[4], po[3], po[6], c.dt, c.wdt,
+                             w.at_, w.bytes, st);
+        Py_END_ALLOW_THREADS
+        return results(s, {out[0], out[1], out[2], out[3], out[4], out[5], out[6]});
+    });
+}
+
 // the addresses of the operators' functions, in the order of their pointers above
 PyObject *bind_operators(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    if (n != 8) {
-        PyErr_SetString(PyExc_TypeError, "bind_operators takes eight addresses");
+    if (n != 18) {
+        PyErr_SetString(PyExc_TypeError, "bind_operators takes eighteen addresses");
         return nullptr;
     }
-    void *p[8];
-    for (int i = 0; i < 8; i++)
+    void *p[18];
+    for (int i = 0; i < 18; i++)
         if (!(p[i] = PyLong_AsVoidPtr(a[i]))) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind_operators: NULL");
             return nullptr;
@@ -547,6 +824,16 @@ PyObject *bind_operators(PyObject *, PyObject *const *a, Py_ssize_t n)
     norm_fwd_fn = (decltype(norm_fwd_fn))p[5];
     norm_bwd_bytes_fn = (decltype(norm_bwd_bytes_fn))p[6];
     norm_bwd_fn = (decltype(norm_bwd_fn))p[7];
+    embed_fwd_fn = (decltype(embed_fwd_fn))p[8];
+    embed_bwd_bytes_fn = (decltype(embed_bwd_bytes_fn))p[9];
+    embed_bwd_fn = (decltype(embed_bwd_fn))p[10];
+    ffn_fwd_bytes_fn = (decltype(ffn_fwd_bytes_fn))p[11];
+    ffn_fwd_fn = (decltype(ffn_fwd_fn))p[12];
+    ffn_bwd_bytes_fn = (decltype(ffn_bwd_bytes_fn))p[13];
+    ffn_bwd_fn = (decltype(ffn_bwd_fn))p[14];
+    gate_norm_fwd_fn = (decltype(gate_norm_fwd_fn))p[15];
+    gate_norm_bwd_bytes_fn = (decltype(gate_norm_bwd_bytes_fn))p[16];
+    gate_norm_bwd_fn = (decltype(gate_norm_bwd_fn))p[17];
     Py_RETURN_NONE;
 }
 
@@ -582,6 +869,12 @@ PyMethodDef methods[] = {
     {"dropout_add", (PyCFunction)(void (*)(void))dropout_add, METH_FASTCALL, nullptr},
     {"add_norm_fwd", (PyCFunction)(void (*)(void))add_norm_fwd, METH_FASTCALL, nullptr},
     {"add_norm_bwd", (PyCFunction)(void (*)(void))add_norm_bwd, METH_FASTCALL, nullptr},
+    {"embed_fwd", (PyCFunction)(void (*)(void))embed_fwd, METH_FASTCALL, nullptr},
+    {"embed_bwd", (PyCFunction)(void (*)(void))embed_bwd, METH_FASTCALL, nullptr},
+    {"ffn_fwd", (PyCFunction)(void (*)(void))ffn_fwd, METH_FASTCALL, nullptr},
+    {"ffn_bwd", (PyCFunction)(void (*)(void))ffn_bwd, METH_FASTCALL, nullptr},
+    {"gate_norm_fwd", (PyCFunction)(void (*)(void))gate_norm_fwd, METH_FASTCALL, nullptr},
+    {"gate_norm_bwd", (PyCFunction)(void (*)(void))gate_norm_bwd, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_hdt_pycall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
