@@ -9,9 +9,9 @@
 //
 // Products are C[m][n] = sum over k of A(m, k) B(n, k), of operands whose k is consecutive in memory ("fast": [m][k]) or not ("slow": [k][m]):
 //   GATE    A = X fast, B = Wg and Wu fast; both sums of a pair (m, n) come together, and Pg, Pu, H leave     (forward)
-//   STORE   A = H fast, B = Wd fast: Y (forward);  A = dG then dU fast, B = Wg then Wu slow: dX, k going through both
 //   DGATE   A = dY fast, B = Wd slow: dH, which is not stored: dG and dU leave                                  (backward)
-//   WEIGHT  A = dG, dU or dY slow, B = X, X or H slow: the weights' gradients, k going over the rows
+//   STORE   A = H fast, B = Wd fast: Y;  A = dG then dU fast, B = Wg then Wu slow: dX, k going through both;  A = dG, dU or dY slow, B = X, X
+//           or H slow: the weights' gradients, k going over the rows
 #pragma once
 
 #include "hdt_internal.h"
@@ -19,7 +19,7 @@
 
 namespace hdt_ffn {
 
-enum { GATE, STORE, DGATE, WEIGHT };
+enum { GATE, STORE, DGATE };
 
 // act(g) and its derivative
 struct Act {
@@ -61,7 +61,7 @@ struct Product {
     int64_t lda, ldb;            // elements from row to row
     int m, n, k;                 // k: of one range
     int ranges;                  // of k: 1 or 2
-    void *out[3];                // GATE: Pg, Pu (both may be NULL), H; STORE, WEIGHT: C; DGATE: dG, dU
+    void *out[3];                // GATE: Pg, Pu (both may be NULL), H; STORE: C; DGATE: dG, dU
     const void *by_gate, *by_up; // DGATE: Pg, Pu
     int64_t ldo;                 // of out, by_gate, by_up
     int act;
