@@ -31,29 +31,42 @@ struct Sigmoid {
 };
 __device__ __forceinline__ Sigmoid sigmoid(float x)
 {
-    const float t = fast_exp2(fminf(-1.4426950408889634f * x, 126.f)), s = 1.f / (1.f + t);
+    const float t = fast_exp2(fminf(-1.4426950408889634f * x, 126.f)), s = __builtin_amdgcn_rcpf(1.f + t);
     return {s, t * s};
 }
-template <bool SLOPE>
-__device__ __forceinline__ Act activate(float g, int act)
+template <bool SLOPE, int ACT>
+__device__ __forceinline__ Act activate(float g)
 {
-    if (act == HDT_SILU) {
+    if (ACT == HDT_SILU) {
         const Sigmoid s = sigmoid(g);
         return {g * s.value, SLOPE ? s.value * fmaf(g, s.rest, 1.f) : 0.f};
     }
-    if (act == HDT_GELU) {
-        const float cdf = 0.5f * (1.f + erff(g * 0.70710678118654752f));
-        return {g * cdf, SLOPE ? fmaf(g * 0.3989422804014327f, fast_exp2(-0.72134752044448170f * g * g), cdf) : 0.f};
+    if (ACT == HDT_GELU) {
+        // Phi by erf(x) = 1 - (a1 t + .. + a5 t^5) exp(-x^2), t = 1 / (1 + p x), x >= 0, within 1.5e-7 (Hastings; Abramowitz and Stegun 7.1.26)
+        const float e = fast_exp2(-0.72134752044448170f * g * g), t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, fabsf(g), 1.f));
+        const float poly = fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f);
+        const float q = 0.5f * t * poly * e, cdf = g < 0.f ? q : 1.f - q;
+        return {g * cdf, SLOPE ? fmaf(g * 0.3989422804014327f, e, cdf) : 0.f};
     }
-    // (1 + tanh z) / 2 = sigmoid(2 z); beyond 15 the derivative is 0 or 1, and its factors overflow
-    const float q = g * g;
-    const Sigmoid s = sigmoid(1.5957691216057308f * g * fmaf(0.044715f, q, 1.f));
-    float slope = 0.f;
-    if (SLOPE) {
-        const float inner = fmaf(g * s.value * s.rest, 1.5957691216057308f * fmaf(0.134145f, q, 1.f), s.value);
-        slope = g < -15.f ? 0.f : g > 15.f ? 1.f : inner;
-    }
-    return {g * s.value, slope};
+    // (1 + tanh z) / 2 = sigmoid(2 z).  Beyond |g| = 15 both are what they are there, but g^2 would overflow.
+    const float q = fminf(g * g, 225.f);
+    const Sigmoid s = sigmoid(g * fmaf(1.5957691216057308f * 0.044715f, q, 1.5957691216057308f));
+    return {g * s.value, SLOPE ? fmaf(g * s.value * s.rest, fmaf(1.5957691216057308f * 0.134145f, q, 1.5957691216057308f), s.value) : 0.f};
+}
+// f(activation as a constant)
+template <int N>
+struct Constant {
+    static constexpr int value = N;
+};
+template <typename F>
+__device__ __forceinline__ void by_act(int act, F f)
+{
+    if (act == HDT_SILU)
+        f(Constant<HDT_SILU>());
+    else if (act == HDT_GELU)
+        f(Constant<HDT_GELU>());
+    else
+        f(Constant<HDT_GELU_TANH>());
 }
 
 struct Product {

@@ -2,6 +2,7 @@
 #include <algorithm>
 
 #include "hdt_ffn.h"
+#include "hdt_ffn_few.h"
 #include "hdt_ffn_plain.h"
 #include "hdt_ffn_tile.h"
 
@@ -26,14 +27,14 @@ hdt_status_t check_sizes(const char *fn, int64_t rows, int32_t width, int32_t in
     return HDT_OK;
 }
 
-using Large = Shape<2, 4, 4, 2>;  // 256 x 256, a workgroup a compute unit
-using Small = Shape<2, 2, 2, 2>;  // 128 x 128, two of them
+using Large = Shape<2, 4, 4, 2, 32, 4>;  // 256 x 256, a workgroup a compute unit
+using Small = Shape<2, 2, 2, 2, 64, 2>;  // 128 x 128, two
 
-// Products that one launch makes in tiles, and how: the shape, and the pieces of k that are joined afterwards.
+// Products that one launch makes in tiles, and how (TileArgs has the meanings).
 struct Plan {
-    bool large;
-    int splits, per;   // tiles of k a piece
-    unsigned tiles;    // of all products
+    int shape;  // 0 Large, 1 Small
+    unsigned direct, tiles, piece_items, sharers;
+    int pieces, per, rest;
     size_t parts_bytes;
 };
 struct Dims {
@@ -41,33 +42,38 @@ struct Dims {
 };
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
+// slots: workgroups the chip holds; step, around: clocks of 64 of k with every unit full, and of what stands around a tile's walk
 template <typename S>
-void consider(const Dims *of, int products, int k_tiles, bool divisible, bool large, Plan *best, double *best_cost)
+void consider(const Dims *of, int products, int k, int ranges, bool divisible, int shape, unsigned slots, double step, double around, Plan *best, double *best_cost)
 {
     int64_t tiles = 0;
     for (int i = 0; i < products; i++) tiles += (int64_t)ceil_div(of[i].m, S::BM) * ceil_div(of[i].n, S::BN);
-    // clocks of a tile of k with every unit full, and of what stands around a tile's walk
-    const int slots = large ? 256 : 512;
-    const double step = large ? 2600 : 1500, around = large ? 9000 : 6000;
-    for (int splits = 1; splits <= (divisible ? 32 : 1); splits++) {
-        const int per = ceil_div(k_tiles, splits);
-        if (splits > 1 && (ceil_div(k_tiles, per) != splits || per < 4)) continue;
-        const double rounds = (double)((tiles * splits + slots - 1) / slots);
-        // pieces: their sums written and read at about 2000 bytes a clock, and a launch
-        const double join = splits > 1 ? (double)tiles * splits * S::BM * S::BN * 8 / 2000 + 8000 : 0;
-        const double cost = rounds * (per * step + around) + join;
-        if (*best_cost >= 0 && cost >= *best_cost) continue;
+    const int k_tiles = ranges * ceil_div(k, S::BK);
+    step *= S::BK / 64.;
+    auto offer = [&](const Plan &plan, double cost) {
+        if (*best_cost >= 0 && cost >= *best_cost) return;
         *best_cost = cost;
-        *best = {large, splits, per, (unsigned)tiles, splits > 1 ? (size_t)tiles * splits * S::BM * S::BN * sizeof(float) : 0};
-    }
+        *best = plan;
+    };
+    const double rounds = (double)((tiles + slots - 1) / slots);
+    offer({shape, (unsigned)tiles, (unsigned)tiles, 0, 0, 0, 0, 0, 0}, rounds * (k_tiles * step + around));
+    const int64_t direct = tiles / slots * slots, cut = tiles - direct;
+    if (!divisible || cut == 0) return;
+    const int least = 256 / S::BK;  // (shorter walks are their beginning and end)
+    const int per = std::max(ceil_div(cut * k_tiles, slots), std::min(least, k_tiles)), pieces = k_tiles / per, rest = k_tiles - pieces * per;
+    if (pieces == 1 && rest == 0) return;
+    const unsigned piece_items = (unsigned)(cut * pieces + 7) / 8 * 8, sharers = (unsigned)(ceil_div(cut * rest, per) + 7) / 8 * 8;
+    // parts are written and read at about 3000 bytes a clock; and a launch
+    const size_t parts = (size_t)(cut * pieces + (rest ? sharers + cut : 0)) * S::BM * S::BN * sizeof(float);
+    offer({shape, (unsigned)direct, (unsigned)tiles, piece_items, sharers, pieces, per, rest, parts},
+          (double)(direct / slots) * (k_tiles * step + around) + per * step + 1.3 * around + parts * 2. / 3000 + 8000);
 }
 Plan plan_of(const Dims *of, int products, int k, int ranges, bool divisible)
 {
     Plan best = {};
     double cost = -1;
-    const int k_tiles = ranges * ceil_div(k, BK);
-    consider<Large>(of, products, k_tiles, divisible, true, &best, &cost);
-    consider<Small>(of, products, k_tiles, divisible, false, &best, &cost);
+    consider<Large>(of, products, k, ranges, divisible, 0, 256, 4000, 9000, &best, &cost);
+    consider<Small>(of, products, k, ranges, divisible, 1, 512, 2800, 7000, &best, &cost);
     return best;
 }
 
@@ -78,6 +84,7 @@ struct Sizes {
     size_t hidden_bytes() const { return padded((size_t)rows * inner * (dt == HDT_BF16 ? 2 : 4)); }
     // whether rows begin at multiples of 16 bytes, as direct loads need it
     bool tiled() const { return dt == HDT_BF16 && width % 8 == 0 && inner % 8 == 0; }
+    bool few() const { return tiled() && rows <= kFew; }  // (the forward's products)
     Plan plan_gate() const
     {
         const Dims d = {(int)rows, 2 * inner};
@@ -103,7 +110,7 @@ struct Sizes {
         const Dims d[] = {{inner, width}, {inner, width}, {width, inner}};
         return plan_of(d, 3, (int)rows, 1, true);
     }
-    size_t fwd_bytes(bool train) const { return (train ? 0 : hidden_bytes()) + (tiled() ? plan_down().parts_bytes : 0); }
+    size_t fwd_bytes(bool train) const { return (train ? 0 : hidden_bytes()) + (tiled() && !few() ? plan_down().parts_bytes : 0); }
     size_t bwd_bytes() const { return 2 * hidden_bytes() + (tiled() ? std::max(plan_dx().parts_bytes, plan_weights().parts_bytes) : 0); }
 };
 
@@ -111,8 +118,12 @@ template <int KIND, typename S, bool A_SLOW, bool B_SLOW>
 hdt_status_t launch_tiles(const char *name, const Product *of, int products, const Plan &plan, void *parts, hipStream_t st)
 {
     TileArgs a = {};
-    a.products = products, a.k = of[0].k, a.ranges = of[0].ranges, a.splits = plan.splits, a.per = plan.per, a.tiles = plan.tiles, a.parts = (float *)parts;
-    a.act = of[0].act, a.group = 8;
+    a.products = products, a.k = of[0].k, a.ranges = of[0].ranges, a.parts = (float *)parts;
+    const unsigned chunk = hdt_tile::xcd_chunk(plan.direct, 64, 1);
+    a.chunk = hdt_tile::FastDiv(chunk);
+    a.direct = plan.direct, a.spread = hdt_tile::padded_grid(plan.direct, chunk), a.tiles = plan.tiles;
+    a.piece_items = plan.piece_items, a.sharers = plan.sharers, a.pieces = plan.pieces, a.per = plan.per, a.rest = plan.rest;
+    a.act = of[0].act, a.group = 4;
     unsigned first = 0;
     for (int i = 0; i < products; i++) {
         const Product &p = of[i];
@@ -122,19 +133,25 @@ hdt_status_t launch_tiles(const char *name, const Product *of, int products, con
                   p.lda, p.ldb, p.ldo, p.m, p.n, tiles_m, tiles_n, first};
         first += (unsigned)tiles_m * tiles_n;
     }
-    const unsigned items = plan.tiles * plan.splits, chunk = hdt_tile::xcd_chunk(items, 64, 1);
-    a.chunk = hdt_tile::FastDiv(chunk);
-    a.by_split = hdt_tile::FastDiv(plan.splits);
     const auto kernel = k_ffn_tile<KIND, S, A_SLOW, B_SLOW>;
     if (S::LDS > 65536) HDT_HIP_TRY(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS));
     {
         HdtTimer t(name, st);
-        hipLaunchKernelGGL(kernel, dim3(hdt_tile::padded_grid(items, chunk)), dim3(S::THREADS), S::LDS, st, a);
+        hipLaunchKernelGGL(kernel, dim3(a.spread + plan.piece_items + plan.sharers), dim3(S::THREADS), S::LDS, st, a);
         HDT_HIP_TRY(hipGetLastError());
     }
-    if (plan.splits == 1) return HDT_OK;
+    if (plan.direct == plan.tiles) return HDT_OK;
     HdtTimer t("hdt_ffn_join", st);
-    hipLaunchKernelGGL(k_ffn_join<S>, dim3(plan.tiles * S::MB), dim3(S::THREADS), 0, st, a);
+    hipLaunchKernelGGL(k_ffn_join<S>, dim3((plan.tiles - plan.direct) * S::MB * S::NB), dim3(S::THREADS), 0, st, a);
+    HDT_HIP_TRY(hipGetLastError());
+    return HDT_OK;
+}
+
+template <int KIND>
+hdt_status_t make_few(const char *name, const Product &p, hipStream_t st)
+{
+    HdtTimer t(name, st);
+    launch_few<KIND>(p, st);
     HDT_HIP_TRY(hipGetLastError());
     return HDT_OK;
 }
@@ -144,8 +161,8 @@ hdt_status_t make(const char *name, const Product *of, int products, const Sizes
 {
     if (s.tiled() && of[0].m > 0 && of[0].k > 0) {
         const Plan plan = (s.*plan_fn)();
-        return plan.large ? launch_tiles<KIND, Large, A_SLOW, B_SLOW>(name, of, products, plan, parts, st)
-                          : launch_tiles<KIND, Small, A_SLOW, B_SLOW>(name, of, products, plan, parts, st);
+        if (plan.shape == 0) return launch_tiles<KIND, Large, A_SLOW, B_SLOW>(name, of, products, plan, parts, st);
+        return launch_tiles<KIND, Small, A_SLOW, B_SLOW>(name, of, products, plan, parts, st);
     }
     for (int i = 0; i < products; i++) {
         HdtTimer t(name, st);
@@ -196,10 +213,10 @@ HDT_EXPORT hdt_status_t hdt_ffn_fwd(const void *x, const void *w_gate, const voi
     Product p = {};
     p.a[0] = x, p.b[0] = w_gate, p.b[1] = w_up, p.lda = width, p.ldb = width, p.m = (int)rows, p.n = inner, p.k = width, p.ranges = 1;
     p.out[0] = by_gate, p.out[1] = by_up, p.out[2] = h, p.ldo = inner, p.act = act;
-    if (hdt_status_t r = make<GATE, false, false>("hdt_ffn_gate", &p, 1, s, &Sizes::plan_gate, nullptr, st)) return r;
+    if (hdt_status_t r = s.few() ? make_few<GATE>("hdt_ffn_gate", p, st) : make<GATE, false, false>("hdt_ffn_gate", &p, 1, s, &Sizes::plan_gate, nullptr, st)) return r;
     p = {};
     p.a[0] = h, p.b[0] = w_down, p.lda = inner, p.ldb = inner, p.m = (int)rows, p.n = width, p.k = inner, p.ranges = 1, p.out[0] = y, p.ldo = width;
-    return make<STORE, false, false>("hdt_ffn_down", &p, 1, s, &Sizes::plan_down, parts, st);
+    return s.few() ? make_few<STORE>("hdt_ffn_down", p, st) : make<STORE, false, false>("hdt_ffn_down", &p, 1, s, &Sizes::plan_down, parts, st);
 }
 
 HDT_EXPORT size_t hdt_ffn_bwd_workspace_bytes(int64_t rows, int32_t width, int32_t inner, hdt_dtype_t dt)

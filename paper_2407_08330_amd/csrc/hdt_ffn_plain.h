@@ -76,14 +76,13 @@ __global__ __launch_bounds__(256) void k_ffn_plain(Product p)
         const int64_t at = (int64_t)m * p.ldo + n;
         if (KIND == GATE) {
             const float g = acc[0][e], u = acc[NB - 1][e];
+            Act f;
+            by_act(p.act, [&](auto act) { f = activate<true, decltype(act)::value>(g); });
             if (p.out[0]) {
-                const Act f = activate<true>(g, p.act);
                 ((T *)p.out[0])[at] = (T)(u * f.slope);
                 ((T *)p.out[1])[at] = (T)f.value;
-                ((T *)p.out[2])[at] = (T)(f.value * u);
-            } else {
-                ((T *)p.out[2])[at] = (T)(activate<false>(g, p.act).value * u);
             }
+            ((T *)p.out[2])[at] = (T)(f.value * u);
         } else if (KIND == DGATE) {
             ((T *)p.out[0])[at] = (T)(acc[0][e] * (float)((const T *)p.by_gate)[at]);
             ((T *)p.out[1])[at] = (T)(acc[0][e] * (float)((const T *)p.by_up)[at]);

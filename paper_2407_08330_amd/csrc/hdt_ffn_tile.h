@@ -19,12 +19,20 @@
 
 namespace hdt_ffn {
 
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
 using hdt_tile::dma16;
 using hdt_tile::lds_addr;
 using hdt_tile::wait_vmcnt;
 using hdt_tile::wg_barrier;
 
-constexpr int BK = 64;
+// a pointer that is the same for the whole wave, in scalar registers
+__device__ __forceinline__ const __bf16 *uniform(const __bf16 *p)
+{
+    const uint64_t u = (uint64_t)(uintptr_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u), hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
+    return (const __bf16 *)(uintptr_t)((uint64_t)hi << 32 | lo);
+}
 
 // One product of a launch: tiles of C beginning at number `first`
 struct TileProduct {
@@ -38,30 +46,53 @@ struct TileProduct {
 struct TileArgs {
     TileProduct p[3];
     int products, k, ranges;    // k of a range
-    int splits, per;            // the tiles of k are divided into `splits` pieces of `per`
-    unsigned tiles;             // of all products
-    float *parts;               // [tiles][splits][BM BN] where splits > 1
-    hdt_tile::FastDiv chunk, by_split;
+    // The first `direct` tiles have a workgroup each (`spread` of them, a multiple of 8).  Each of the others is cut along k into `pieces` of `per` tiles of
+    // k, which workgroups make side by side, all tiles' first pieces before the second: what an XCD does at a time is at one place of k, and its
+    // tiles share what they read.  What is left of the tiles, `rest` each, one behind the other, is divided among `sharers` further
+    // workgroups, `per` each.  Sums that are not all of a tile go to `parts`, and k_ffn_join adds them up.
+    unsigned direct, spread, tiles, piece_items, sharers;
+    int pieces, per, rest;
+    hdt_tile::FastDiv chunk;
+    float *parts;               // [pieces][tiles - direct], then [number of a sharer + number of the tile], of [BM BN]
     int act, group;             // group: tiles along m that are taken side by side
 };
+// item number b of n (a multiple of 8) in an order in which an XCD, which gets every eighth workgroup, has consecutive items
+__device__ __forceinline__ unsigned by_xcd(unsigned b, unsigned n) { return (b & 7u) * (n >> 3) + (b >> 3); }
+struct TilePlace {
+    int which, m, n;  // product, first row, tile of columns
+};
+template <typename S, bool SEVERAL>
+__device__ __forceinline__ TilePlace place_of(const TileArgs &a, unsigned tile)
+{
+    TilePlace at = {0, 0, 0};
+    if (SEVERAL && a.products > 1) at.which = tile >= a.p[2].first ? 2 : tile >= a.p[1].first ? 1 : 0;
+    const TileProduct &p = a.p[at.which];
+    // `group` tiles along m, then the next n: what runs at the same time on an XCD shares operands in its L2
+    const unsigned local = tile - p.first, wide = (unsigned)(a.group * p.tiles_n), g = local / wide, in = local - g * wide;
+    const int rows = min(a.group, p.tiles_m - (int)g * a.group);
+    at.n = (int)(in / (unsigned)rows);
+    at.m = ((int)g * a.group + (int)(in - (unsigned)at.n * rows)) * S::BM;
+    return at;
+}
 
-template <int WM_, int WN_, int MB_, int NB_>
+template <int WM_, int WN_, int MB_, int NB_, int BK_, int STAGES_>
 struct Shape {
     static constexpr int WM = WM_, WN = WN_, MB = MB_, NB = NB_, NW = WM * WN, THREADS = NW * 64;
-    static constexpr int BM = WM * MB * 32, BN = WN * NB * 32;
-    static constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE = A_BYTES + B_BYTES, LDS = 2 * STAGE;
+    static constexpr int BM = WM * MB * 32, BN = WN * NB * 32, BK = BK_, STEPS = BK / 16, STAGES = STAGES_;
+    static constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE = A_BYTES + B_BYTES, LDS = STAGES * STAGE;
+    static constexpr int LOADS = (BM + BN) * BK / 8 / 64 / NW;  // direct loads of a stage, for each wave
 };
 
 // One operand of R rows: how it comes to LDS, and how its blocks of 32 rows are read.  PERMUTED: in the order of the sums' rows.
-template <int R, int NW, bool SLOW, bool PERMUTED>
+template <int R, int NW, int BK, bool SLOW, bool PERMUTED>
 struct Operand {
-    static constexpr int CPR = SLOW ? R / 8 : 8;        // chunks of 16 bytes a row in LDS
-    static constexpr int LOADS = R * 8 / 64 / NW;       // wave-level loads of a tile, for each wave
-    static_assert(R * 8 % (64 * NW) == 0, "tile");
+    static constexpr int CPR = (SLOW ? R : BK) / 8;     // chunks of 16 bytes a row in LDS
+    static constexpr int LOADS = R * BK / 8 / 64 / NW;  // wave-level loads of a tile, for each wave
+    static_assert(R * BK / 8 % (64 * NW) == 0, "tile");
 
     static __device__ __forceinline__ int swizzle(int row)
     {
-        if (!SLOW) return hdt_tile::swz<8>(row);
+        if (!SLOW) return CPR == 8 ? hdt_tile::swz<8>(row) : (row >> 2) & 3;
         return CPR % 16 == 0 ? (row & 3) << 2 : ((row >> 1) & 1) << 2;
     }
     // row and chunk (as in memory) of load i of this wave and lane
@@ -88,21 +119,16 @@ struct Operand {
                 off[i] = (uint32_t)row * (uint32_t)(ld * 2) + (uint32_t)(min(first + chunk * 8, count - 8) - first) * 2;
         }
     }
-    // base: of the tile's first row or column, at k0
-    __device__ __forceinline__ void request(const __bf16 *base, uint32_t to, int wave) const
-    {
-#pragma unroll
-        for (int i = 0; i < LOADS; i++) dma16(base, off[i], to + (uint32_t)(i * NW + wave) * 1024u);
-    }
-    // the same with zeros from `left` of k on
-    __device__ __forceinline__ void fill(const __bf16 *base, char *to, int left, int wave, int lane) const
+    // the tile without direct loads, with zeros from `left` of k on.  base: of its first row or column; other: from there to the second
+    // weight, whose rows are every second block of 32
+    __device__ __forceinline__ void fill(const __bf16 *base, int64_t other, char *to, int left, int wave, int lane) const
     {
 #pragma unroll
         for (int i = 0; i < LOADS; i++) {
             int row, chunk;
             place(i, wave, lane, &row, &chunk);
             bf16x8 v = zero_bf16x8();
-            if ((SLOW ? row : chunk * 8) < left) v = *reinterpret_cast<const bf16x8 *>((const char *)base + off[i]);
+            if ((SLOW ? row : chunk * 8) < left) v = *reinterpret_cast<const bf16x8 *>((const char *)(base + (row >> 5 & 1 ? other : 0)) + off[i]);
             *reinterpret_cast<bf16x8 *>(to + (i * NW + wave) * 1024 + lane * 16) = v;
         }
     }
@@ -115,7 +141,7 @@ struct Operand {
         const int hf = lane >> 5;
         if (!SLOW) {
             const int i = lane & 31, r = PERMUTED ? (i & 0x13) | (i & 4) << 1 | (i & 8) >> 1 : i;
-            at[0] = (uint32_t)((first + r) * 128 + ((hf ^ swizzle(r)) * 16));
+            at[0] = (uint32_t)((first + r) * (CPR * 16) + ((hf ^ swizzle(r)) * 16));
         } else {
             const int t = lane & 15, piece = t & 3, k = hf * 8 + (t >> 2);
             const int low = 2 * ((lane >> 4) & 1) + (PERMUTED ? piece & 1 : piece >> 1), half = PERMUTED ? piece >> 1 : piece & 1;
@@ -125,32 +151,33 @@ struct Operand {
     }
     __device__ __forceinline__ bf16x8 read(const char *tile, int block, int step) const
     {
-        if (!SLOW) return lds_read_8(tile + ((at[0] ^ (uint32_t)(step * 32)) + block * 4096));
+        if (!SLOW) return lds_read_8(tile + ((at[0] ^ (uint32_t)(step * 32)) + block * (32 * CPR * 16)));
         const char *p = tile + at[block] + step * 16 * CPR * 16;
         return lds_read_tr_8(p, p + 4 * CPR * 16);
     }
 };
 
-template <int KIND, typename S, bool A_SLOW, bool B_SLOW>
-__global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 2) void k_ffn_tile(TileArgs a)
+// Where chunk c of row r of a block row of results is, rows of CH chunks of 16 bytes: a chunk of 16 consecutive rows, and the chunks of a row,
+// without a conflict.
+template <int CH>
+__device__ __forceinline__ int result_at(int r, int c)
 {
-    constexpr int MB = S::MB, NB = S::NB, NW = S::NW;
-    extern __shared__ __attribute__((aligned(1024))) char smem[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const unsigned item = hdt_tile::logical_block(blockIdx.x, a.chunk);
-    if (item >= a.tiles * (unsigned)a.splits) return;
-    const unsigned tile = a.splits > 1 ? a.by_split.div(item) : item, piece = item - tile * a.splits;
-    int which = 0;
-    if (a.products > 1) which = tile >= a.p[2].first ? 2 : tile >= a.p[1].first ? 1 : 0;
-    const TileProduct &p = a.p[which];
-    // `group` tiles along m, then the next n: what runs at the same time on an XCD shares operands in its L2
-    const unsigned local = tile - p.first, wide = (unsigned)(a.group * p.tiles_n), g = local / wide, in = local - g * wide;
-    const int rows = min(a.group, p.tiles_m - (int)g * a.group), tn = (int)(in / (unsigned)rows), tm = (int)g * a.group + (int)(in - (unsigned)tn * rows);
-    const int m0 = tm * S::BM, n0 = tn * (KIND == GATE ? S::BN / 2 : S::BN);
+    return (r * CH + (CH % 16 == 0 ? c ^ (r & 15) : CH == 8 ? c ^ hdt_tile::swz<8>(r) : c ^ ((r >> 1) & 7))) * 16;
+}
 
-    const int per_range = (a.k + BK - 1) / BK, whole = a.k / BK, t0 = (int)piece * a.per, t1 = min(t0 + a.per, a.ranges * per_range);
-    Operand<S::BM, NW, A_SLOW, false> oa;
-    Operand<S::BN, NW, B_SLOW, true> ob;
+// tiles of k t0 .. t1 - 1 of a tile; part: where sums go that are not all of it
+template <int KIND, typename S, bool A_SLOW, bool B_SLOW>
+__device__ __forceinline__ void make_tile(const TileArgs &a, char *smem, unsigned tile, int t0, int t1, float *part)
+{
+    constexpr int MB = S::MB, NB = S::NB, NW = S::NW, BK = S::BK;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const TilePlace at = place_of<S, KIND == STORE>(a, tile);
+    const TileProduct &p = a.p[at.which];
+    const int m0 = at.m, n0 = at.n * (KIND == GATE ? S::BN / 2 : S::BN);
+
+    const int per_range = (a.k + BK - 1) / BK, whole = a.k / BK;
+    Operand<S::BM, NW, BK, A_SLOW, false> oa;
+    Operand<S::BN, NW, BK, B_SLOW, true> ob;
     oa.init(p.lda, m0, p.m, wave, lane);
     if (KIND != GATE) {
         ob.init(p.ldb, n0, p.n, wave, lane);
@@ -168,39 +195,40 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 2) void k_ffn_t
     oa.template reader<MB>(wm, lane);
     ob.template reader<NB>(wn, lane);
 
-    auto load = [&](int t, int stage) {
-        const int range = t >= per_range, kt = t - range * per_range, k0 = kt * BK;
-        const __bf16 *pa = (range ? p.a[1] : p.a[0]) + (A_SLOW ? (int64_t)k0 * p.lda + m0 : (int64_t)m0 * p.lda + k0);
-        const __bf16 *pb = (range && KIND != GATE ? p.b[1] : p.b[0]) + (B_SLOW ? (int64_t)k0 * p.ldb + n0 : (int64_t)n0 * p.ldb + k0);
-        char *to = smem + stage * S::STAGE;
-        if (kt < whole) {
-            oa.request(pa, lds_addr(to), wave);
-            if (KIND != GATE) {
-                ob.request(pb, lds_addr(to) + S::A_BYTES, wave);
-            } else {
-                const int64_t up = (p.b[1] - p.b[0]);
-#pragma unroll
-                for (int i = 0; i < ob.LOADS; i++) {
-                    const int block = ((i * NW + wave) * 8) >> 5;  // (a load's eight rows are of one block)
-                    dma16(pb + (block & 1 ? up : 0), ob.off[i], lds_addr(to) + S::A_BYTES + (uint32_t)(i * NW + wave) * 1024u);
-                }
-            }
+    auto is_whole = [&](int t) { return (t >= per_range ? t - per_range : t) < whole; };
+    struct From {
+        const __bf16 *a, *b;
+        int left;  // of k
+    };
+    const int64_t up = KIND == GATE ? p.b[1] - p.b[0] : 0;
+    auto from = [&](int t) {
+        const int range = t >= per_range, k0 = (t - range * per_range) * BK;
+        return From{(range ? p.a[1] : p.a[0]) + (A_SLOW ? (int64_t)k0 * p.lda + m0 : (int64_t)m0 * p.lda + k0),
+                    (range && KIND != GATE ? p.b[1] : p.b[0]) + (B_SLOW ? (int64_t)k0 * p.ldb + n0 : (int64_t)n0 * p.ldb + k0), a.k - k0};
+    };
+    // load number i of a whole tile, of A's and then of B's
+    auto request = [&](const From &f, int stage, int i) __attribute__((always_inline)) {
+        const uint32_t to = lds_addr(smem) + (uint32_t)(stage * S::STAGE);
+        if (i < oa.LOADS) {
+            dma16(uniform(f.a), oa.off[i], __builtin_amdgcn_readfirstlane(to + (uint32_t)(i * NW + wave) * 1024u));
         } else {
-            const int left = a.k - k0;
-            oa.fill(pa, to, left, wave, lane);
-            if (KIND != GATE) {
-                ob.fill(pb, to + S::A_BYTES, left, wave, lane);
-            } else {
-                const int64_t up = (p.b[1] - p.b[0]);
+            const int j = i - oa.LOADS, block = (j * NW + wave) * (512 / BK) >> 5;  // GATE: a load's rows are of one block
+            dma16(uniform(f.b + (KIND == GATE && (block & 1) ? up : 0)), ob.off[j],
+                  __builtin_amdgcn_readfirstlane(to + S::A_BYTES + (uint32_t)(j * NW + wave) * 1024u));
+        }
+    };
+    auto fill = [&](const From &f, int stage) {
+        char *to = smem + stage * S::STAGE;
+        oa.fill(f.a, 0, to, f.left, wave, lane);
+        ob.fill(f.b, up, to + S::A_BYTES, f.left, wave, lane);
+    };
+    auto load = [&](int t, int stage) {
+        const From f = from(t);
+        if (is_whole(t)) {
 #pragma unroll
-                for (int i = 0; i < ob.LOADS; i++) {
-                    int row, chunk;
-                    ob.place(i, wave, lane, &row, &chunk);
-                    bf16x8 v = zero_bf16x8();
-                    if (chunk * 8 < left) v = *reinterpret_cast<const bf16x8 *>((const char *)(pb + (row >> 5 & 1 ? up : 0)) + ob.off[i]);
-                    *reinterpret_cast<bf16x8 *>(to + S::A_BYTES + (i * NW + wave) * 1024 + lane * 16) = v;
-                }
-            }
+            for (int i = 0; i < S::LOADS; i++) request(f, stage, i);
+        } else {
+            fill(f, stage);
         }
     };
 
@@ -222,132 +250,245 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 2) void k_ffn_t
 #pragma unroll
         for (int j = 0; j < NB; j++) to.b[j] = ob.read(tb, j, step);
     };
-    auto multiply = [&](const Frags &x) {
+    // the products of one step, rows of blocks one after the other; between them between(i)
+    auto multiply = [&](const Frags &x, auto between) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < MB; i++)
+        for (int i = 0; i < MB; i++) {
 #pragma unroll
             for (int j = 0; j < NB; j++) acc[i][j] = mfma_32x32x16(x.b[j], x.a[i], acc[i][j]);
+            between(i);
+        }
+    };
+    // a stage is requested STAGES - 1 ahead; before it is read, those behind it may still be on their way
+    auto arrived = [&](int t) {  // tile t has, for this wave
+        constexpr int MORE = (S::STAGES - 2) * S::LOADS;
+        bool direct = t + S::STAGES - 2 < t1;
+#pragma unroll
+        for (int u = 1; u < S::STAGES - 1; u++) direct = direct && is_whole(t + u);
+        if (direct)
+            wait_vmcnt<MORE>();
+        else
+            wait_vmcnt<0>();
     };
     if (t0 < t1) {
-        load(t0, 0);
-        wait_vmcnt<0>();
+#pragma unroll
+        for (int u = 0; u < S::STAGES - 1; u++)
+            if (t0 + u < t1) load(t0 + u, u);
+        arrived(t0);
         wg_barrier();
-        if (t0 + 1 < t1) load(t0 + 1, 1);
         read(f[0], 0, 0);
-        int stage = 0;
-        for (int t = t0; t < t1; t++, stage ^= 1) {
-            read(f[1], stage, 1);
-            multiply(f[0]);
-            read(f[0], stage, 2);
-            multiply(f[1]);
-            read(f[1], stage, 3);
-            multiply(f[0]);
-            if (t + 1 < t1) {
-                wait_vmcnt<0>();
-                wg_barrier();
-                if (t + 2 < t1) load(t + 2, stage);
-                read(f[0], stage ^ 1, 0);
+        int stage = 0, before = S::STAGES - 1;
+        for (int t = t0; t < t1; t++) {
+            const int next = stage + 1 == S::STAGES ? 0 : stage + 1, ahead = t + S::STAGES - 1;
+            const From fr = from(min(ahead, t1 - 1));
+            const bool direct = ahead < t1 && is_whole(ahead);
+            if (ahead < t1 && !direct) fill(fr, before);
+#pragma unroll
+            for (int s = 0; s < S::STEPS; s++) {
+                if (s + 1 < S::STEPS) {
+                    read(f[(s + 1) & 1], stage, s + 1);
+                } else if (t + 1 < t1) {
+                    arrived(t + 1);
+                    wg_barrier();
+                    read(f[0], next, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(f[s & 1], [&](int i) __attribute__((always_inline)) {
+                    if (s == 0 && direct) {
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int q = i * S::LOADS / MB; q < (i + 1) * S::LOADS / MB; q++) request(fr, before, q);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                });
+                __builtin_amdgcn_sched_barrier(0);
             }
-            multiply(f[1]);
+            before = stage;
+            stage = next;
         }
     }
 
     // a lane's sums: row m of its block, columns of eight
     const int hf = lane >> 5;
-    if (KIND == STORE && a.splits > 1) {
-        float *part = a.parts + (size_t)item * S::BM * S::BN;
+    if (KIND == STORE && part) {
 #pragma unroll
         for (int i = 0; i < MB; i++)
 #pragma unroll
             for (int j = 0; j < NB; j++)
 #pragma unroll
                 for (int q = 0; q < 4; q++) {
-                    typedef __attribute__((ext_vector_type(4))) float f32x4;
                     const f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
                     *reinterpret_cast<f32x4 *>(part + ((size_t)((i * NB + j) * 4 + q) * S::THREADS + tid) * 4) = v;
                 }
         return;
     }
+    // Results leave by LDS, block row by block row of all waves, so that a wave stores whole rows of the tile: by itself it has 32 or 64
+    // columns of 32 rows, and as many requests of a piece of a row each.
+    wg_barrier();  // (the stages are no longer read)
+    constexpr int GROUP = S::WM * 32;  // rows of a block row
+    auto row_of = [&](int r, int i) { return m0 + (r >> 5) * MB * 32 + i * 32 + (r & 31); };
+    const int my_row = wave / S::WN * 32 + (lane & 31);
+    if constexpr (KIND != DGATE) {
+        constexpr int OUTS = KIND == GATE ? 3 : 1, COLS = KIND == GATE ? NB / 2 : NB, WIDE = KIND == GATE ? S::BN / 2 : S::BN, CH = WIDE / 8;
+        constexpr int BUFFER = GROUP * WIDE * 2;  // of one result
+        static_assert(2 * OUTS * BUFFER <= S::LDS, "room for two block rows");
+        auto finish = [&](auto act, auto keep) __attribute__((always_inline)) {
+            constexpr int FIRST = KIND == GATE && !decltype(keep)::value ? 2 : 0;
 #pragma unroll
-    for (int i = 0; i < MB; i++) {
-        const int m = m0 + wm + i * 32 + (lane & 31);
-        if (m >= p.m) continue;
+            for (int i = 0; i < MB; i++) {
+                char *buf = smem + (i & 1) * OUTS * BUFFER;
 #pragma unroll
-        for (int j = 0; j < (KIND == GATE ? NB / 2 : NB); j++)
+                for (int c = 0; c < COLS * 2; c++) {
+                    const int j = c >> 1, h = c & 1, to = result_at<CH>(my_row, wave % S::WN * (COLS * 4) + j * 4 + h * 2 + hf);
+                    if constexpr (KIND == GATE) {
+                        bf16x8 v[3];
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const int n = n0 + (KIND == GATE ? wn / 2 : wn) + j * 32 + h * 16 + hf * 8;
-                if (n >= p.n) continue;
-                const int64_t at = (int64_t)m * p.ldo + n;
-                if (KIND == GATE) {
-                    bf16x8 vg, vu, vh;
-#pragma unroll
-                    for (int e = 0; e < 8; e++) {
-                        const float g = acc[i][2 * j][h * 8 + e], u = acc[i][2 * j + 1][h * 8 + e];
-                        if (p.out[0]) {
-                            const Act f = activate<true>(g, a.act);
-                            vg[e] = (__bf16)(u * f.slope), vu[e] = (__bf16)f.value, vh[e] = (__bf16)(f.value * u);
-                        } else {
-                            vh[e] = (__bf16)(activate<false>(g, a.act).value * u);
+                        for (int e = 0; e < 8; e++) {
+                            const float g = acc[i][2 * j][h * 8 + e], u = acc[i][2 * j + 1][h * 8 + e];
+                            const Act f = activate<decltype(keep)::value, decltype(act)::value>(g);
+                            v[0][e] = (__bf16)(u * f.slope), v[1][e] = (__bf16)f.value, v[2][e] = (__bf16)(f.value * u);
                         }
-                    }
-                    if (p.out[0]) {
-                        *reinterpret_cast<bf16x8 *>(p.out[0] + at) = vg;
-                        *reinterpret_cast<bf16x8 *>(p.out[1] + at) = vu;
-                    }
-                    *reinterpret_cast<bf16x8 *>(p.out[2] + at) = vh;
-                } else if (KIND == DGATE) {
-                    const bf16x8 pg = *reinterpret_cast<const bf16x8 *>(p.by_gate + at), pu = *reinterpret_cast<const bf16x8 *>(p.by_up + at);
-                    bf16x8 vg, vu;
 #pragma unroll
-                    for (int e = 0; e < 8; e++) {
-                        const float dh = acc[i][j][h * 8 + e];
-                        vg[e] = (__bf16)(dh * (float)pg[e]), vu[e] = (__bf16)(dh * (float)pu[e]);
+                        for (int o = FIRST; o < OUTS; o++) *reinterpret_cast<bf16x8 *>(buf + o * BUFFER + to) = v[o];
+                    } else {
+                        *reinterpret_cast<bf16x8 *>(buf + to) = pack_bf16x8(acc[i][j], h * 8);
                     }
-                    *reinterpret_cast<bf16x8 *>(p.out[0] + at) = vg;
-                    *reinterpret_cast<bf16x8 *>(p.out[1] + at) = vu;
-                } else {
-                    *reinterpret_cast<bf16x8 *>(p.out[0] + at) = pack_bf16x8(acc[i][j], h * 8);
+                }
+                wg_barrier();
+#pragma unroll
+                for (int o = FIRST; o < OUTS; o++)
+#pragma unroll
+                    for (int q = 0; q < GROUP * CH / S::THREADS; q++) {
+                        const int r = (q * S::THREADS + tid) / CH, chunk = (q * S::THREADS + tid) % CH, m = row_of(r, i), n = n0 + chunk * 8;
+                        const bf16x8 v = *reinterpret_cast<const bf16x8 *>(buf + o * BUFFER + result_at<CH>(r, chunk));
+                        if (m < p.m && n < p.n) *reinterpret_cast<bf16x8 *>(p.out[o] + (int64_t)m * p.ldo + n) = v;
+                    }
+            }
+        };
+        if constexpr (KIND == GATE)
+            by_act(a.act, [&](auto act) __attribute__((always_inline)) {
+                if (p.out[0])
+                    finish(act, Constant<1>());
+                else
+                    finish(act, Constant<0>());
+            });
+        else
+            finish(Constant<0>(), Constant<0>());
+    } else {
+        // dH goes through LDS in fp32
+        constexpr int CH = S::BN / 8, BUFFER = GROUP * S::BN * 4, EACH = GROUP * CH / S::THREADS;
+        static_assert(2 * BUFFER <= S::LDS, "room for two block rows");
+        struct Factors {
+            bf16x8 g[EACH], u[EACH];
+        } with[2];
+        auto factors = [&](int i) {
+#pragma unroll
+            for (int q = 0; q < EACH; q++) {
+                const int r = (q * S::THREADS + tid) / CH, chunk = (q * S::THREADS + tid) % CH;
+                const int64_t at = (int64_t)min(row_of(r, i), p.m - 1) * p.ldo + min(n0 + chunk * 8, p.n - 8);
+                with[i & 1].g[q] = *reinterpret_cast<const bf16x8 *>(p.by_gate + at);
+                with[i & 1].u[q] = *reinterpret_cast<const bf16x8 *>(p.by_up + at);
+            }
+        };
+        factors(0);
+#pragma unroll
+        for (int i = 0; i < MB; i++) {
+            char *buf = smem + (i & 1) * BUFFER;
+#pragma unroll
+            for (int c = 0; c < NB * 4; c++)  // four columns
+                *reinterpret_cast<f32x4 *>(buf + result_at<CH * 2>(my_row, wave % S::WN * (NB * 8) + (c >> 2) * 8 + (c >> 1 & 1) * 4 + hf * 2 + (c & 1))) =
+                    f32x4{acc[i][c >> 2][(c & 3) * 4], acc[i][c >> 2][(c & 3) * 4 + 1], acc[i][c >> 2][(c & 3) * 4 + 2], acc[i][c >> 2][(c & 3) * 4 + 3]};
+            if (i + 1 < MB) factors(i + 1);
+            wg_barrier();
+#pragma unroll
+            for (int q = 0; q < EACH; q++) {
+                const int r = (q * S::THREADS + tid) / CH, chunk = (q * S::THREADS + tid) % CH, m = row_of(r, i), n = n0 + chunk * 8;
+                bf16x8 vg, vu;
+#pragma unroll
+                for (int half = 0; half < 2; half++) {
+                    const f32x4 dh = *reinterpret_cast<const f32x4 *>(buf + result_at<CH * 2>(r, chunk * 2 + half));
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        vg[half * 4 + e] = (__bf16)(dh[e] * (float)with[i & 1].g[q][half * 4 + e]);
+                        vu[half * 4 + e] = (__bf16)(dh[e] * (float)with[i & 1].u[q][half * 4 + e]);
+                    }
+                }
+                if (m < p.m && n < p.n) {
+                    *reinterpret_cast<bf16x8 *>(p.out[0] + (int64_t)m * p.ldo + n) = vg;
+                    *reinterpret_cast<bf16x8 *>(p.out[1] + (int64_t)m * p.ldo + n) = vu;
                 }
             }
+        }
     }
 }
 
-// The pieces of k added up in order: a workgroup has one row of blocks of a tile.
+template <int KIND, typename S, bool A_SLOW, bool B_SLOW>
+__global__ __launch_bounds__(S::THREADS, 2) void k_ffn_tile(TileArgs a)
+{
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    const int k_tiles = a.ranges * ((a.k + S::BK - 1) / S::BK);
+    if (KIND != STORE || blockIdx.x < a.spread) {
+        const unsigned tile = hdt_tile::logical_block(blockIdx.x, a.chunk);
+        if (tile < a.direct) make_tile<KIND, S, A_SLOW, B_SLOW>(a, smem, tile, 0, k_tiles, nullptr);
+        return;
+    }
+    const unsigned cut = a.tiles - a.direct, block = blockIdx.x - a.spread;
+    constexpr size_t SIZE = (size_t)S::BM * S::BN;
+    if (block < a.piece_items) {
+        const unsigned item = by_xcd(block, a.piece_items), piece = item / cut, tile = item - piece * cut;
+        if (piece < (unsigned)a.pieces) make_tile<KIND, S, A_SLOW, B_SLOW>(a, smem, a.direct + tile, piece * a.per, (piece + 1) * a.per, a.parts + item * SIZE);
+        return;
+    }
+    const unsigned me = by_xcd(block - a.piece_items, a.sharers);
+    int64_t at = (int64_t)me * a.per;
+    const int64_t end = min(at + a.per, (int64_t)cut * a.rest);
+    while (at < end) {
+        const int64_t tile = at / a.rest;
+        const int t0 = (int)(at - tile * a.rest), t1 = (int)min((int64_t)a.rest, t0 + (end - at)), from = a.pieces * a.per;
+        wg_barrier();  // (the LDS of the tile before is no longer read)
+        make_tile<KIND, S, A_SLOW, B_SLOW>(a, smem, a.direct + (unsigned)tile, from + t0, from + t1,
+                                           t1 - t0 == k_tiles ? nullptr : a.parts + ((size_t)a.pieces * cut + me + tile) * SIZE);
+        at += t1 - t0;
+    }
+}
+
+// The parts of the tiles that were cut, added up in the order of k: a workgroup has a block of each of a tile's waves.
 template <typename S>
 __global__ __launch_bounds__(S::THREADS) void k_ffn_join(TileArgs a)
 {
     constexpr int MB = S::MB, NB = S::NB;
-    typedef __attribute__((ext_vector_type(4))) float f32x4;
+    constexpr size_t SIZE = (size_t)S::BM * S::BN;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5;
-    const unsigned tile = blockIdx.x / MB;
-    const int i = blockIdx.x % MB;
-    int which = 0;
-    if (a.products > 1) which = tile >= a.p[2].first ? 2 : tile >= a.p[1].first ? 1 : 0;
-    const TileProduct &p = a.p[which];
-    const unsigned local = tile - p.first, wide = (unsigned)(a.group * p.tiles_n), g = local / wide, in = local - g * wide;
-    const int rows = min(a.group, p.tiles_m - (int)g * a.group), tn = (int)(in / (unsigned)rows), tm = (int)g * a.group + (int)(in - (unsigned)tn * rows);
-    const int m = tm * S::BM + wave / S::WN * MB * 32 + i * 32 + (lane & 31), n0 = tn * S::BN + wave % S::WN * NB * 32;
-    const float *part = a.parts + (size_t)tile * a.splits * S::BM * S::BN;
-#pragma unroll
-    for (int j = 0; j < NB; j++)
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-            f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+    const unsigned tile = blockIdx.x / (MB * NB), cut = a.tiles - a.direct;
+    const int i = blockIdx.x / NB % MB, j = blockIdx.x % NB;
+    const int64_t first = (int64_t)tile * a.rest / a.per, last = a.rest ? ((int64_t)(tile + 1) * a.rest - 1) / a.per : first - 1;
+    const int parts = a.pieces + (int)(last - first + 1);
+    if (parts == 1) return;  // (one workgroup had all of it)
+    const TilePlace at = place_of<S, true>(a, a.direct + tile);
+    const TileProduct &p = a.p[at.which];
+    const int m = at.m + wave / S::WN * MB * 32 + i * 32 + (lane & 31), n0 = at.n * S::BN + wave % S::WN * NB * 32;
+    f32x4 sum[4] = {};
 #pragma unroll 4
-            for (int s = 0; s < a.splits; s++) {
-                const float *q = part + (size_t)s * S::BM * S::BN + ((size_t)((i * NB + j) * 4 + 2 * h) * S::THREADS + tid) * 4;
-                const f32x4 x = *reinterpret_cast<const f32x4 *>(q), y = *reinterpret_cast<const f32x4 *>(q + (size_t)S::THREADS * 4);
+    for (int s = 0; s < parts; s++) {
+        const size_t slot = s < a.pieces ? (size_t)s * cut + tile : (size_t)a.pieces * cut + (size_t)(first + s - a.pieces) + tile;
+        const float *q = a.parts + slot * SIZE + ((size_t)((i * NB + j) * 4) * S::THREADS + tid) * 4;
+        f32x4 x[4];
 #pragma unroll
-                for (int e = 0; e < 4; e++) lo[e] += x[e], hi[e] += y[e];
-            }
-            const int n = n0 + j * 32 + h * 16 + hf * 8;
-            if (m >= p.m || n >= p.n) continue;
-            bf16x8 v;
+        for (int h = 0; h < 4; h++) x[h] = *reinterpret_cast<const f32x4 *>(q + (size_t)h * S::THREADS * 4);
 #pragma unroll
-            for (int e = 0; e < 4; e++) v[e] = (__bf16)lo[e], v[4 + e] = (__bf16)hi[e];
-            *reinterpret_cast<bf16x8 *>(p.out[0] + (int64_t)m * p.ldo + n) = v;
-        }
+        for (int h = 0; h < 4; h++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) sum[h][e] += x[h][e];
+    }
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+        const int n = n0 + j * 32 + h * 16 + hf * 8;
+        if (m >= p.m || n >= p.n) continue;
+        bf16x8 v;
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] = (__bf16)sum[2 * h + (e >> 2)][e & 3];
+        *reinterpret_cast<bf16x8 *>(p.out[0] + (int64_t)m * p.ldo + n) = v;
+    }
 }
 
 }  // namespace hdt_ffn
