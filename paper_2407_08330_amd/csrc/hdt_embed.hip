@@ -5,7 +5,7 @@
 //                  0 for rows without a token, or (accumulate) added to what stands there
 //
 // Both are bound by memory.  The backward has no atomics on values: k_embed_sort puts the tokens of each row side by side, in the order in
-// which they came; k_embed_sum adds up kBlock consecutive ones a wave, so that a word that is a tenth of a text keeps no workgroup longer
+// which they came; k_embed_sum adds up a block of consecutive ones a wave, so that a word that is a tenth of a text keeps no workgroup longer
 // than one that comes twice; k_embed_join adds up the rows that span several blocks.  Sums are in fp32 in a fixed order.
 #include <algorithm>
 
@@ -58,17 +58,18 @@ struct BwdArgs {
     Entry *entries;   // [tokens], ordered by (id mod shares, id, token); the rest of them is not written
     int32_t *n_real;  // how many there are
     float *parts;     // [blocks][2][width]: of a block's first row where that began before it, of its last where that goes on behind it
-    int tokens, vocab, width, shares_log2, rows, accumulate;  // rows: of a share
+    int tokens, vocab, width, shares_log2, rows, accumulate, block;  // rows: of a share; block: entries that a wave adds up
     float scale;
 };
 
-constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kMostRows = 512, kBlock = 32, kAhead = 8;
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kMostRows = 512, kAhead = 8;
 
 // Share s of the rows are those whose number is s modulo the number of shares (frequent words, which stand side by side in a vocabulary
 // made by frequency, go to different ones).  Its workgroup reads all ids, twice, from the caches: the first time it counts, its waves by
 // themselves and row by row, so that each wave knows where its tokens of a row go, and the second time it puts them there.  Nothing is
 // shared between workgroups.
-template <typename W>
+// HELD: a wave's STEPS x 64 ids are all it has, and stay in registers in between.
+template <typename W, int STEPS, bool HELD>
 __global__ __launch_bounds__(kSortThreads) void k_embed_sort(BwdArgs a)
 {
     extern __shared__ int count[];  // [waves][rows], [rows]
@@ -85,17 +86,28 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(BwdArgs a)
         const int t = step * 64 + lane;
         return t < a.tokens && step < last ? a.ids[t] : -1;
     };
+    int id[STEPS];
+    auto take = [&](int s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < STEPS; u++) id[u] = id_at(s + u);
+    };
     int below = 0;
-    for (int s = first; s < last; s += kAhead) {
-        int id[kAhead];
+    auto count_them = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < kAhead; u++) id[u] = id_at(s + u);
-#pragma unroll
-        for (int u = 0; u < kAhead; u++) {
-            if ((unsigned)id[u] >= (unsigned)a.vocab) continue;
-            const int of = id[u] & mask;
+        for (int u = 0; u < STEPS; u++) {
+            if (s + u >= last) break;  // (code that is not run is not fetched)
+            const int of = (unsigned)id[u] < (unsigned)a.vocab ? id[u] & mask : mask + 1;
             if (of < share) below++;
             if (of == share) atomicAdd(&mine[id[u] >> a.shares_log2], 1);
+        }
+    };
+    if (HELD) {
+        take(first);
+        count_them(first);
+    } else {
+        for (int s = first; s < last; s += STEPS) {
+            take(s);
+            count_them(s);
         }
     }
 #pragma unroll
@@ -132,12 +144,11 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(BwdArgs a)
         }
     __syncthreads();
 
-    for (int s = first; s < last; s += kAhead) {
-        int id[kAhead];
+    for (int s = first; s < last; s += STEPS) {
+        if (!HELD) take(s);
 #pragma unroll
-        for (int u = 0; u < kAhead; u++) id[u] = id_at(s + u);
-#pragma unroll
-        for (int u = 0; u < kAhead; u++) {
+        for (int u = 0; u < STEPS; u++) {
+            if (s + u >= last) break;
             const int row = (unsigned)id[u] < (unsigned)a.vocab && (id[u] & mask) == share ? id[u] >> a.shares_log2 : -1;
             unsigned long long open = __ballot(row >= 0);
             while (open) {  // the lanes that have the row of the first open one
@@ -160,7 +171,7 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(BwdArgs a)
 }
 
 // ------------------------------------------------------------------------------------------ backward: the sums
-// A wave adds up the rows of kBlock consecutive entries, 512 columns of them.
+// A wave adds up the rows of a block of entries, 512 columns of them.
 template <typename W, bool WHOLE>
 __device__ __forceinline__ void put_row(const BwdArgs &a, int id, int c, Eight v)
 {
@@ -182,12 +193,12 @@ __global__ __launch_bounds__(256) void k_embed_sum(BwdArgs a, int slabs)
     const int lane = threadIdx.x & 63;
     const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int block = (int)(unit / slabs), c = ((int)(unit % slabs) * 64 + lane) * 8, left = a.width - c;
-    const int64_t n = *a.n_real, i0 = (int64_t)block * kBlock;
+    const int64_t n = *a.n_real, i0 = (int64_t)block * a.block;
     if (i0 >= n) return;
-    const int count = (int)min((int64_t)kBlock, n - i0);
+    const int count = (int)min((int64_t)a.block, n - i0);
     // the entries and their neighbours: entry i0 + j in lane j + 1
     Entry mine = {-1, 0};
-    if (lane < kBlock + 2 && i0 - 1 + lane >= 0 && i0 - 1 + lane < n) mine = a.entries[i0 - 1 + lane];
+    if (lane < a.block + 2 && i0 - 1 + lane >= 0 && i0 - 1 + lane < n) mine = a.entries[i0 - 1 + lane];
     auto id_of = [&](int j) { return __builtin_amdgcn_readlane(mine.id, j + 1); };
     float *const part = a.parts + (size_t)block * 2 * a.width + c;
     bool begun_before = id_of(-1) == id_of(0);
@@ -229,14 +240,14 @@ __global__ __launch_bounds__(256) void k_embed_join(BwdArgs a, int slabs)
 {
     __shared__ float lds[4][512];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t block = blockIdx.x / (unsigned)slabs, n = *a.n_real, i0 = block * kBlock, i1 = i0 + kBlock;
+    const int64_t block = blockIdx.x / (unsigned)slabs, n = *a.n_real, i0 = block * a.block, i1 = i0 + a.block;
     if (i1 >= n) return;  // (no block behind it)
     const int id = a.entries[i1].id;
     if (a.entries[i1 - 1].id != id) return;
     if (a.entries[i0].id == id && i0 > 0 && a.entries[i0 - 1].id == id) return;  // begun before
     int64_t more = 1;  // blocks behind this one that have a part
     for (;;) {
-        const int64_t at = i1 + (more + lane) * kBlock;
+        const int64_t at = i1 + (more + lane) * a.block;
         const unsigned long long ends = __ballot(!(at < n && a.entries[at].id == id));
         if (ends) {
             more += __builtin_ctzll(ends);
@@ -298,7 +309,9 @@ int shares_log2(int vocab)
     while (((int64_t)kMostRows << l) < vocab) l++;
     return l;
 }
-int64_t blocks_of(int64_t tokens) { return (tokens + kBlock - 1) / kBlock; }
+// entries a block: few tokens are spread over more waves
+int block_of(int64_t tokens) { return tokens <= 16384 ? 8 : 32; }
+int64_t blocks_of(int64_t tokens) { return (tokens + block_of(tokens) - 1) / block_of(tokens); }
 size_t entries_bytes(int64_t tokens) { return ((size_t)tokens * sizeof(Entry) + 15) / 16 * 16; }
 
 #define HDT_EXPORT extern "C" __attribute__((visibility("default")))
@@ -320,7 +333,13 @@ hdt_status_t launch_bwd(const BwdArgs &a, hipStream_t st)
     {
         HdtTimer t("hdt_embed_sort", st);
         const size_t lds = (size_t)(kSortWaves + 1) * a.rows * sizeof(int);
-        hipLaunchKernelGGL(k_embed_sort<W>, dim3(1u << a.shares_log2), dim3(kSortThreads), lds, st, a);
+        const dim3 grid(1u << a.shares_log2), threads(kSortThreads);
+        if (a.tokens <= 4 * kSortThreads)
+            hipLaunchKernelGGL((k_embed_sort<W, 4, true>), grid, threads, lds, st, a);
+        else if (a.tokens <= 32 * kSortThreads)
+            hipLaunchKernelGGL((k_embed_sort<W, 32, true>), grid, threads, lds, st, a);
+        else
+            hipLaunchKernelGGL((k_embed_sort<W, 16, false>), grid, threads, lds, st, a);
         HDT_HIP_TRY(hipGetLastError());
     }
     if (blocks == 0) return HDT_OK;
@@ -388,7 +407,7 @@ HDT_EXPORT hdt_status_t hdt_embed_bwd(const void *d_out, const int32_t *d_ids, i
     a.n_real = (int32_t *)workspace;
     a.entries = (Entry *)((char *)workspace + 16);
     a.parts = (float *)((char *)workspace + 16 + entries_bytes(tokens));
-    a.tokens = (int)tokens, a.vocab = vocab, a.width = width, a.accumulate = accumulate != 0, a.scale = scale;
+    a.tokens = (int)tokens, a.vocab = vocab, a.width = width, a.accumulate = accumulate != 0, a.block = block_of(tokens), a.scale = scale;
     a.shares_log2 = shares_log2(vocab);
     a.rows = (int)(((int64_t)vocab + (1 << a.shares_log2) - 1) >> a.shares_log2);
     hipStream_t st = (hipStream_t)stream;

@@ -164,12 +164,8 @@ hdt_status_t make(const char *name, const Product *of, int products, const Sizes
         if (plan.shape == 0) return launch_tiles<KIND, Large, A_SLOW, B_SLOW>(name, of, products, plan, parts, st);
         return launch_tiles<KIND, Small, A_SLOW, B_SLOW>(name, of, products, plan, parts, st);
     }
-    for (int i = 0; i < products; i++) {
-        HdtTimer t(name, st);
-        s.dt == HDT_BF16 ? launch_plain<__bf16, KIND, A_SLOW, B_SLOW>(of[i], st) : launch_plain<float, KIND, A_SLOW, B_SLOW>(of[i], st);
-        HDT_HIP_TRY(hipGetLastError());
-    }
-    return HDT_OK;
+    HdtTimer t(name, st);
+    return s.dt == HDT_BF16 ? launch_plain<__bf16, KIND, A_SLOW, B_SLOW>(of, products, st) : launch_plain<float, KIND, A_SLOW, B_SLOW>(of, products, st);
 }
 
 #define HDT_EXPORT extern "C" __attribute__((visibility("default")))

@@ -1,4 +1,4 @@
-// The products of the gated feed-forward block for every size, type and alignment: tiles of 64 x 64, operands taken element by element.
+// The products of the gated feed-forward block for every size, type and alignment: operands taken element by element.
 #pragma once
 
 #include "hdt_ffn.h"
@@ -26,77 +26,154 @@ struct PlainOp<float> {
     }
 };
 
-// A workgroup of 2 x 2 waves, a wave 32 x 32 (two sums of them for GATE).  What is beyond m, n or k counts as zero on both sides, so that
-// nothing there, NaN or not, is met.  C^T = B A^T: a lane holds one m and rows of n.
-template <typename T, int KIND, bool A_SLOW, bool B_SLOW>
-__global__ __launch_bounds__(256) void k_ffn_plain(Product p)
+// A group of W x W waves makes a tile, a wave 32 x 32 of it (two sums of them for GATE).  GROUPS of them divide k, 32 at a time, and join at the end
+// in a fixed order: where there are few tiles a tile's walk along k is what takes the time.  A tile of k is requested before the one in
+// front of it is multiplied.  What is beyond m, n or k counts as zero on both sides, so that nothing there, NaN or not, is met.  C^T = B A^T: a
+// lane holds one m and rows of n.
+constexpr int kPlainK = 32;
+template <typename T>
+constexpr int plain_row() { return kPlainK + PlainOp<T>::PAD; }
+template <typename T, int KIND, int W, int GROUPS>
+constexpr int plain_lds() { return GROUPS * (KIND == GATE ? 3 : 2) * 32 * W * plain_row<T>() * (int)sizeof(T); }
+struct PlainArgs {
+    Product p[3];
+    unsigned first[3], tiles;  // first tile of each product; of all
+};
+
+template <typename T, int KIND, bool A_SLOW, bool B_SLOW, int W, int GROUPS>
+__global__ __launch_bounds__(64 * W * W * GROUPS) void k_ffn_plain(PlainArgs a)
 {
     using Op = PlainOp<T>;
-    constexpr int BK = 32, LD = BK + Op::PAD, NB = KIND == GATE ? 2 : 1;
-    __shared__ __attribute__((aligned(16))) T sa[64 * LD], sb[NB][64 * LD];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t tiles_n = (p.n + 63) / 64;
-    const int64_t tile = blockIdx.x;
-    const int m0 = (int)(tile / tiles_n) * 64, n0 = (int)(tile % tiles_n) * 64;
+    constexpr int LD = plain_row<T>(), NB = KIND == GATE ? 2 : 1, SIDE = 32 * W, THREADS = 64 * W * W, EACH = SIDE * kPlainK / THREADS, TILE = SIDE * LD;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int all = threadIdx.x, group = __builtin_amdgcn_readfirstlane(all / THREADS), tid = all % THREADS, lane = tid & 63, wave = tid >> 6;
+    T *const sa = reinterpret_cast<T *>(smem) + group * (1 + NB) * TILE, *const sb = sa + TILE;
+    const int which = blockIdx.x >= a.first[2] ? 2 : blockIdx.x >= a.first[1] ? 1 : 0;
+    const Product &p = a.p[which];
+    const int64_t tiles_n = (p.n + SIDE - 1) / SIDE, tile = blockIdx.x - a.first[which];
+    const int m0 = (int)(tile / tiles_n) * SIDE, n0 = (int)(tile % tiles_n) * SIDE;
     f32x16 acc[NB];
 #pragma unroll
     for (int b = 0; b < NB; b++)
 #pragma unroll
         for (int e = 0; e < 16; e++) acc[b][e] = 0.f;
 
-    auto stage = [&](T *to, const T *from, int64_t ld, bool slow, int r0, int rows, int k0) {
+    struct Part {
+        T v[EACH];
+    };
+    auto row_of = [&](bool slow, int i) { return slow ? tid % SIDE : tid / kPlainK + THREADS / kPlainK * i; };
+    auto k_of = [&](bool slow, int i) { return slow ? tid / SIDE + THREADS / SIDE * i : tid % kPlainK; };
+    auto take = [&](Part &to, const T *from, int64_t ld, bool slow, int r0, int rows, int k0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const int r = slow ? tid & 63 : (tid >> 5) + 8 * i, k = slow ? (tid >> 6) + 4 * i : tid & 31;
-            T v = (T)0.f;
-            if (r0 + r < rows && k0 + k < p.k) v = slow ? from[(int64_t)(k0 + k) * ld + r0 + r] : from[(int64_t)(r0 + r) * ld + k0 + k];
-            to[r * LD + k] = v;
+        for (int i = 0; i < EACH; i++) {
+            const int r = r0 + row_of(slow, i), k = k0 + k_of(slow, i);
+            to.v[i] = (T)0.f;
+            if (r < rows && k < p.k) to.v[i] = slow ? from[(int64_t)k * ld + r] : from[(int64_t)r * ld + k];
         }
     };
-    for (int range = 0; range < p.ranges; range++)
-        for (int k0 = 0; k0 < p.k; k0 += BK) {
-            __syncthreads();
-            stage(sa, (const T *)p.a[range], p.lda, A_SLOW, m0, p.m, k0);
+    auto put = [&](T *to, const Part &from, bool slow) __attribute__((always_inline)) {
 #pragma unroll
-            for (int b = 0; b < NB; b++) stage(sb[b], (const T *)p.b[NB == 2 ? b : range], p.ldb, B_SLOW, n0, p.n, k0);
-            __syncthreads();
-            const T *pa = sa + ((wave >> 1) * 32 + (lane & 31)) * LD;
+        for (int i = 0; i < EACH; i++) to[row_of(slow, i) * LD + k_of(slow, i)] = from.v[i];
+    };
+    const int per_range = (p.k + kPlainK - 1) / kPlainK, steps = p.ranges * per_range, rounds = (steps + GROUPS - 1) / GROUPS;
+    Part va, vb[NB];
+    auto request = [&](int t) __attribute__((always_inline)) {
+        const int range = t >= per_range, k0 = t < steps ? (t - range * per_range) * kPlainK : p.k;  // (beyond the end: zeros)
+        take(va, (const T *)(range ? p.a[1] : p.a[0]), p.lda, A_SLOW, m0, p.m, k0);
 #pragma unroll
-            for (int k = 0; k < BK; k += Op::STEP)
+        for (int b = 0; b < NB; b++) take(vb[b], (const T *)((NB == 2 ? b : range) ? p.b[1] : p.b[0]), p.ldb, B_SLOW, n0, p.n, k0);
+    };
+    if (rounds > 0) request(group);
+    for (int i = 0; i < rounds; i++) {
+        __syncthreads();
+        put(sa, va, A_SLOW);
 #pragma unroll
-                for (int b = 0; b < NB; b++) acc[b] = Op::mma(sb[b] + ((wave & 1) * 32 + (lane & 31)) * LD + k, pa + k, lane, acc[b]);
-        }
-
-    const int m = m0 + (wave >> 1) * 32 + (lane & 31);
-    if (m >= p.m) return;
+        for (int b = 0; b < NB; b++) put(sb + b * TILE, vb[b], B_SLOW);
+        __syncthreads();
+        if (i + 1 < rounds) request((i + 1) * GROUPS + group);
+        const T *pa = sa + (wave / W * 32 + (lane & 31)) * LD;
 #pragma unroll
-    for (int e = 0; e < 16; e++) {
-        const int n = n0 + (wave & 1) * 32 + (lane >> 5) * 4 + 8 * (e >> 2) + (e & 3);
-        if (n >= p.n) continue;
-        const int64_t at = (int64_t)m * p.ldo + n;
-        if (KIND == GATE) {
-            const float g = acc[0][e], u = acc[NB - 1][e];
-            Act f;
-            by_act(p.act, [&](auto act) { f = activate<true, decltype(act)::value>(g); });
-            if (p.out[0]) {
-                ((T *)p.out[0])[at] = (T)(u * f.slope);
-                ((T *)p.out[1])[at] = (T)f.value;
-            }
-            ((T *)p.out[2])[at] = (T)(f.value * u);
-        } else if (KIND == DGATE) {
-            ((T *)p.out[0])[at] = (T)(acc[0][e] * (float)((const T *)p.by_gate)[at]);
-            ((T *)p.out[1])[at] = (T)(acc[0][e] * (float)((const T *)p.by_up)[at]);
-        } else {
-            ((T *)p.out[0])[at] = (T)acc[0][e];
-        }
+        for (int k = 0; k < kPlainK; k += Op::STEP)
+#pragma unroll
+            for (int b = 0; b < NB; b++) acc[b] = Op::mma(sb + b * TILE + (wave % W * 32 + (lane & 31)) * LD + k, pa + k, lane, acc[b]);
     }
+    if (GROUPS > 1) {
+        float *const join = reinterpret_cast<float *>(smem);  // [threads][17]: one group's sums at a time
+        static_assert(GROUPS == 1 || THREADS * 17 * 4 <= plain_lds<T, KIND, W, GROUPS>(), "room for a group's sums");
+#pragma unroll
+        for (int b = 0; b < NB; b++)
+            for (int g = 1; g < GROUPS; g++) {
+                __syncthreads();
+                if (group == g)
+#pragma unroll
+                    for (int e = 0; e < 16; e++) join[tid * 17 + e] = acc[b][e];
+                __syncthreads();
+                if (group == 0)
+#pragma unroll
+                    for (int e = 0; e < 16; e++) acc[b][e] += join[tid * 17 + e];
+            }
+        if (group > 0) return;
+    }
+
+    const int m = m0 + wave / W * 32 + (lane & 31);
+    if (m >= p.m) return;
+    auto finish = [&](auto act) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 16; e++) {
+            const int n = n0 + wave % W * 32 + (lane >> 5) * 4 + 8 * (e >> 2) + (e & 3);
+            if (n >= p.n) continue;
+            const int64_t at = (int64_t)m * p.ldo + n;
+            if (KIND == GATE) {
+                const float u = acc[NB - 1][e];
+                const Act f = activate<true, decltype(act)::value>(acc[0][e]);
+                if (p.out[0]) {
+                    ((T *)p.out[0])[at] = (T)(u * f.slope);
+                    ((T *)p.out[1])[at] = (T)f.value;
+                }
+                ((T *)p.out[2])[at] = (T)(f.value * u);
+            } else if (KIND == DGATE) {
+                ((T *)p.out[0])[at] = (T)(acc[0][e] * (float)((const T *)p.by_gate)[at]);
+                ((T *)p.out[1])[at] = (T)(acc[0][e] * (float)((const T *)p.by_up)[at]);
+            } else {
+                ((T *)p.out[0])[at] = (T)acc[0][e];
+            }
+        }
+    };
+    if constexpr (KIND == GATE)
+        by_act(p.act, [&](auto act) __attribute__((always_inline)) { finish(act); });
+    else
+        finish(Constant<0>());
 }
 
-template <typename T, int KIND, bool A_SLOW, bool B_SLOW>
-void launch_plain(const Product &p, hipStream_t st)
+template <typename T, int KIND, bool A_SLOW, bool B_SLOW, int W, int GROUPS>
+hdt_status_t launch_plain_as(const Product *of, int products, hipStream_t st)
 {
-    const int64_t tiles = ((int64_t)p.m + 63) / 64 * (((int64_t)p.n + 63) / 64);
-    hipLaunchKernelGGL((k_ffn_plain<T, KIND, A_SLOW, B_SLOW>), dim3((unsigned)tiles), dim3(256), 0, st, p);
+    constexpr int SIDE = 32 * W, LDS = plain_lds<T, KIND, W, GROUPS>();
+    PlainArgs a = {};
+    for (int i = 0; i < 3; i++) {
+        a.first[i] = ~0u;
+        if (i >= products) continue;
+        a.p[i] = of[i];
+        a.first[i] = a.tiles;
+        a.tiles += (unsigned)(((int64_t)of[i].m + SIDE - 1) / SIDE * (((int64_t)of[i].n + SIDE - 1) / SIDE));
+    }
+    const auto kernel = k_ffn_plain<T, KIND, A_SLOW, B_SLOW, W, GROUPS>;
+    if (LDS > 65536) HDT_HIP_TRY(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+    hipLaunchKernelGGL(kernel, dim3(a.tiles), dim3(64 * W * W * GROUPS), LDS, st, a);
+    HDT_HIP_TRY(hipGetLastError());
+    return HDT_OK;
+}
+
+// Tiles of 64 x 64; where those do not fill the chip four groups of a workgroup divide k, and where they do not give each compute unit one,
+// tiles of 32 x 32, eight of whose waves divide k (fp32, 512 x 384 x 1000, forward and backward, us: one group 752, four 205, all three NNN)
+template <typename T, int KIND, bool A_SLOW, bool B_SLOW>
+hdt_status_t launch_plain(const Product *of, int products, hipStream_t st)
+{
+    int64_t tiles = 0;
+    for (int i = 0; i < products; i++) tiles += ((int64_t)of[i].m + 63) / 64 * (((int64_t)of[i].n + 63) / 64);
+    if (tiles <= 256) return launch_plain_as<T, KIND, A_SLOW, B_SLOW, 1, 8>(of, products, st);
+    if (tiles <= 512) return launch_plain_as<T, KIND, A_SLOW, B_SLOW, 2, 4>(of, products, st);
+    return launch_plain_as<T, KIND, A_SLOW, B_SLOW, 2, 1>(of, products, st);
 }
 
 }  // namespace hdt_ffn

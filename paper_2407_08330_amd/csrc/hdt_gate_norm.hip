@@ -69,7 +69,32 @@ __device__ __forceinline__ void statistics(Eight (&v)[NCH], const GateArgs &a, i
 constexpr int fwd_threads(int tpr) { return tpr < 256 ? 256 : tpr; }
 constexpr int bwd_threads(int tpr) { return tpr < 512 ? (tpr == 64 ? 512 : tpr) : tpr; }
 
-template <typename T, int TPR, int NCH, bool WHOLE>
+// a thread's columns of the vectors, as they are in memory: requested with a row's values, which is what a wave waits for
+template <typename W, int NCH>
+struct Vectors {
+    typename Vec<W>::V post_weight[NCH], post_bias[NCH], gate[NCH], weight[NCH], bias[NCH];
+    template <bool WHOLE>
+    __device__ __forceinline__ void load(const GateArgs &a, int u, int c, int left)
+    {
+        post_weight[u] = load8<WHOLE>((const W *)a.post_weight + c, left);
+        weight[u] = load8<WHOLE>((const W *)a.weight + c, left);
+        post_bias[u] = bias[u] = typename Vec<W>::V{};
+        if (a.post_bias) post_bias[u] = load8<WHOLE>((const W *)a.post_bias + c, left);
+        if (a.bias) bias[u] = load8<WHOLE>((const W *)a.bias + c, left);
+#pragma unroll
+        for (int e = 0; e < 8; e++) gate[u][e] = (W)1.f;
+        if (a.gate) gate[u] = load8<WHOLE>((const W *)a.gate + c, left);
+    }
+};
+
+// whether a row's registers leave room for the next row's values, which are then requested before this one's are worked on
+template <typename T>
+constexpr bool rows_ahead(int tpr, int nch)
+{
+    return tpr == 64 && nch <= 2 && sizeof(T) == 2;
+}
+
+template <typename T, typename W, int TPR, int NCH, bool WHOLE>
 __global__ __launch_bounds__(fwd_threads(TPR)) void k_gate_norm_fwd(GateArgs a)
 {
     constexpr int PER = fwd_threads(TPR) / TPR;
@@ -81,32 +106,26 @@ __global__ __launch_bounds__(fwd_threads(TPR)) void k_gate_norm_fwd(GateArgs a)
         const size_t at = (size_t)row * a.width;
         V xv[NCH];
         Eight h[NCH];
+        Vectors<W, NCH> v;
         C::each(t, a.width, [&](int u, int c, int left) {
             xv[u] = load8<WHOLE>((const T *)a.x + at + c, left);
             const V yv = load8<WHOLE>((const T *)a.y + at + c, left);
 #pragma unroll
             for (int e = 0; e < 8; e++) h[u].x[e] = (float)yv[e];
         });
+        C::each(t, a.width, [&](int u, int c, int left) { v.template load<WHOLE>(a, u, c, left); });
         float m0, r0, m1, r1;
         statistics<TPR, NCH, WHOLE>(h, a, t, lds, &m0, &r0);
         C::each(t, a.width, [&](int u, int c, int left) {
-            const Eight wp = load_weight<WHOLE>(a.post_weight, a.weight_bf16, c, left);
-            Eight bp = {}, g;
-            if (a.post_bias) bp = load_weight<WHOLE>(a.post_bias, a.weight_bf16, c, left);
 #pragma unroll
-            for (int e = 0; e < 8; e++) g.x[e] = 1.f;
-            if (a.gate) g = load_weight<WHOLE>(a.gate, a.weight_bf16, c, left);
-#pragma unroll
-            for (int e = 0; e < 8; e++) h[u].x[e] = fmaf(g.x[e], fmaf(h[u].x[e] * r0, wp.x[e], bp.x[e]), a.scale * (float)xv[u][e]);
+            for (int e = 0; e < 8; e++)
+                h[u].x[e] = fmaf((float)v.gate[u][e], fmaf(h[u].x[e] * r0, (float)v.post_weight[u][e], (float)v.post_bias[u][e]), a.scale * (float)xv[u][e]);
             store8<WHOLE>((T *)a.h_out + at + c, h[u], left);
         });
         statistics<TPR, NCH, WHOLE>(h, a, t, lds, &m1, &r1);
         C::each(t, a.width, [&](int u, int c, int left) {
-            const Eight w = load_weight<WHOLE>(a.weight, a.weight_bf16, c, left);
-            Eight b = {};
-            if (a.bias) b = load_weight<WHOLE>(a.bias, a.weight_bf16, c, left);
 #pragma unroll
-            for (int e = 0; e < 8; e++) h[u].x[e] = fmaf(h[u].x[e] * r1, w.x[e], b.x[e]);
+            for (int e = 0; e < 8; e++) h[u].x[e] = fmaf(h[u].x[e] * r1, (float)v.weight[u][e], (float)v.bias[u][e]);
             store8<WHOLE>((T *)a.n + at + c, h[u], left);
         });
         if (t == 0) {
@@ -129,25 +148,42 @@ __global__ __launch_bounds__(bwd_threads(TPR)) void k_gate_norm_bwd(GateArgs a)
     extern __shared__ __attribute__((aligned(16))) float lds[];  // 64, then (PER > 1) PER rows of `width` up to whole chunks
     const int sub = threadIdx.x / TPR, t = threadIdx.x % TPR;
     Eight sums[4][NCH] = {};
-    for (int64_t row = (int64_t)blockIdx.x * PER + sub; row < a.rows; row += (int64_t)gridDim.x * PER) {
+    constexpr bool AHEAD = rows_ahead<T>(TPR, NCH);
+    const int64_t step = (int64_t)gridDim.x * PER, first = (int64_t)blockIdx.x * PER + sub;
+    struct Row {
+        V h[NCH], y[NCH], g[NCH], d[NCH];
+        float m0, r0, m1, r1;
+    } next;
+    auto load = [&](Row &to, int64_t row) __attribute__((always_inline)) {
         const size_t at = (size_t)row * a.width;
-        const float m0 = a.stats[row], r0 = a.stats[a.rows + row], m1 = a.stats[2 * a.rows + row], r1 = a.stats[3 * a.rows + row];
-        V hv[NCH], yv[NCH], gv[NCH], dv[NCH];
+        to.m0 = a.stats[row], to.r0 = a.stats[a.rows + row], to.m1 = a.stats[2 * a.rows + row], to.r1 = a.stats[3 * a.rows + row];
         C::each(t, a.width, [&](int u, int c, int left) {
-            hv[u] = load8<WHOLE>((const T *)a.h + at + c, left);
-            gv[u] = load8<WHOLE>((const T *)a.dn + at + c, left);
-            dv[u] = V{};
-            if (a.dh) dv[u] = load8<WHOLE>((const T *)a.dh + at + c, left);
-            yv[u] = load8<WHOLE>((const T *)a.y + at + c, left);
+            to.h[u] = load8<WHOLE>((const T *)a.h + at + c, left);
+            to.g[u] = load8<WHOLE>((const T *)a.dn + at + c, left);
+            to.d[u] = V{};
+            if (a.dh) to.d[u] = load8<WHOLE>((const T *)a.dh + at + c, left);
+            to.y[u] = load8<WHOLE>((const T *)a.y + at + c, left);
         });
+    };
+    if (AHEAD && first < a.rows) load(next, first);
+    for (int64_t row = first; row < a.rows; row += step) {
+        const size_t at = (size_t)row * a.width;
+        Row now;
+        if (AHEAD) {
+            now = next;
+            if (row + step < a.rows) load(next, row + step);
+        } else {
+            load(now, row);
+        }
+        const float m0 = now.m0, r0 = now.r0, m1 = now.m1, r1 = now.r1;
         Eight hat[NCH], g[NCH];
         float s0 = 0.f, s1 = 0.f;
         C::each(t, a.width, [&](int u, int c, int left) {
             const Eight w = load_weight<WHOLE>(a.weight, a.weight_bf16, c, left);
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                const float dn = (float)gv[u][e];
-                hat[u].x[e] = WHOLE || e < left ? ((float)hv[u][e] - m1) * r1 : 0.f;
+                const float dn = (float)now.g[u][e];
+                hat[u].x[e] = WHOLE || e < left ? ((float)now.h[u][e] - m1) * r1 : 0.f;
                 sums[2][u].x[e] = fmaf(dn, hat[u].x[e], sums[2][u].x[e]);
                 sums[3][u].x[e] += dn;
                 g[u].x[e] = dn * w.x[e];
@@ -167,9 +203,9 @@ __global__ __launch_bounds__(bwd_threads(TPR)) void k_gate_norm_bwd(GateArgs a)
             Eight out;
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                const float f = d.x[e] * wp.x[e], dh = fmaf(r1, g[u].x[e] - s0 - hat[u].x[e] * s1, (float)dv[u][e]);
+                const float f = d.x[e] * wp.x[e], dh = fmaf(r1, g[u].x[e] - s0 - hat[u].x[e] * s1, (float)now.d[u][e]);
                 out.x[e] = a.scale * dh;
-                hat[u].x[e] = WHOLE || e < left ? ((float)yv[u][e] - m0) * r0 : 0.f;
+                hat[u].x[e] = WHOLE || e < left ? ((float)now.y[u][e] - m0) * r0 : 0.f;
                 sums[0][u].x[e] = fmaf(dh, hat[u].x[e], sums[0][u].x[e]);
                 sums[1][u].x[e] += dh;
                 g[u].x[e] = WHOLE || e < left ? dh * f : 0.f;
@@ -280,8 +316,11 @@ template <typename T, int TPR, int NCH, bool WHOLE>
 void launch_fwd(const GateArgs &a, hipStream_t st)
 {
     constexpr int PER = fwd_threads(TPR) / TPR;
-    const int64_t grid = std::min<int64_t>((a.rows + PER - 1) / PER, 1 << 20);
-    hipLaunchKernelGGL((k_gate_norm_fwd<T, TPR, NCH, WHOLE>), dim3((unsigned)grid), dim3(fwd_threads(TPR)), 0, st, a);
+    const dim3 grid((unsigned)std::min<int64_t>((a.rows + PER - 1) / PER, 1 << 20)), block(fwd_threads(TPR));
+    if (a.weight_bf16)
+        hipLaunchKernelGGL((k_gate_norm_fwd<T, __bf16, TPR, NCH, WHOLE>), grid, block, 0, st, a);
+    else
+        hipLaunchKernelGGL((k_gate_norm_fwd<T, float, TPR, NCH, WHOLE>), grid, block, 0, st, a);
 }
 template <typename T, int TPR, int NCH, bool WHOLE>
 void launch_bwd(const GateArgs &a, hipStream_t st)
