@@ -144,6 +144,13 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(BwdArgs a)
         }
     __syncthreads();
 
+    if (!a.accumulate)
+        for (int r = wave; r < a.rows; r += kSortWaves) {  // rows without a token
+            const int64_t v = ((int64_t)r << a.shares_log2) + share;
+            if (v >= a.vocab || totals[r] != 0) continue;
+            const Eight zero = {};
+            for (int c = lane * 8; c < a.width; c += 512) store8<false>((W *)a.grad + (size_t)v * a.width + c, zero, a.width - c);
+        }
     for (int s = first; s < last; s += STEPS) {
         if (!HELD) take(s);
 #pragma unroll
@@ -160,13 +167,6 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(BwdArgs a)
                 open &= ~same;
             }
         }
-    }
-    if (a.accumulate) return;
-    for (int r = wave; r < a.rows; r += kSortWaves) {  // rows without a token
-        const int64_t v = ((int64_t)r << a.shares_log2) + share;
-        if (v >= a.vocab || totals[r] != 0) continue;
-        const Eight zero = {};
-        for (int c = lane * 8; c < a.width; c += 512) store8<false>((W *)a.grad + (size_t)v * a.width + c, zero, a.width - c);
     }
 }
 

@@ -58,15 +58,25 @@ void consider(const Dims *of, int products, int k, int ranges, bool divisible, i
     const double rounds = (double)((tiles + slots - 1) / slots);
     offer({shape, (unsigned)tiles, (unsigned)tiles, 0, 0, 0, 0, 0, 0}, rounds * (k_tiles * step + around));
     const int64_t direct = tiles / slots * slots, cut = tiles - direct;
-    if (!divisible || cut == 0) return;
-    const int least = 256 / S::BK;  // (shorter walks are their beginning and end)
-    const int per = std::max(ceil_div(cut * k_tiles, slots), std::min(least, k_tiles)), pieces = k_tiles / per, rest = k_tiles - pieces * per;
-    if (pieces == 1 && rest == 0) return;
-    const unsigned piece_items = (unsigned)(cut * pieces + 7) / 8 * 8, sharers = (unsigned)(ceil_div(cut * rest, per) + 7) / 8 * 8;
-    // parts are written and read at about 3000 bytes a clock; and a launch
-    const size_t parts = (size_t)(cut * pieces + (rest ? sharers + cut : 0)) * S::BM * S::BN * sizeof(float);
-    offer({shape, (unsigned)direct, (unsigned)tiles, piece_items, sharers, pieces, per, rest, parts},
-          (double)(direct / slots) * (k_tiles * step + around) + per * step + 1.3 * around + parts * 2. / 3000 + 8000);
+    if (!divisible || cut == 0 || k_tiles == 0) return;
+    const int least = std::min(256 / S::BK, k_tiles);  // (shorter walks are their beginning and end)
+    const double before = (double)(direct / slots) * (k_tiles * step + around);
+    auto cut_into = [&](int pieces, int per, int rest) {
+        const int64_t sharing = rest ? ceil_div(cut * rest, per) : 0, items = cut * pieces + sharing;
+        const unsigned piece_items = (unsigned)(cut * pieces + 7) / 8 * 8, sharers = (unsigned)(sharing + 7) / 8 * 8;
+        // parts are written and read at about 3000 bytes a clock; and a launch
+        const size_t parts = (size_t)(cut * pieces + (rest ? sharers + cut : 0)) * S::BM * S::BN * sizeof(float);
+        const double tiles_of_one = rest ? per / (double)rest + 1 : 1;
+        offer({shape, (unsigned)direct, (unsigned)tiles, piece_items, sharers, pieces, per, rest, parts},
+              before + (double)ceil_div(items, slots) * (per * step + tiles_of_one * around) + parts * 2. / 3000 + 8000);
+    };
+    // the chip's share each, the rest divided anew; or equal pieces, the last a little shorter
+    const int share = std::max(ceil_div(cut * k_tiles, slots), least), pieces = k_tiles / share, rest = k_tiles - pieces * share;
+    if (rest) cut_into(pieces, share, rest);
+    for (int n = 2; n <= 32; n++) {
+        const int per = ceil_div(k_tiles, n);
+        if (per >= least && ceil_div(k_tiles, per) == n) cut_into(n, per, 0);
+    }
 }
 Plan plan_of(const Dims *of, int products, int k, int ranges, bool divisible)
 {
@@ -82,8 +92,9 @@ struct Sizes {
     int width, inner;
     hdt_dtype_t dt;
     size_t hidden_bytes() const { return padded((size_t)rows * inner * (dt == HDT_BF16 ? 2 : 4)); }
+    bool tiled() const { return dt == HDT_BF16; }
     // whether rows begin at multiples of 16 bytes, as direct loads need it
-    bool tiled() const { return dt == HDT_BF16 && width % 8 == 0 && inner % 8 == 0; }
+    bool even() const { return width % 8 == 0 && inner % 8 == 0; }
     bool few() const { return tiled() && rows <= kFew; }  // (the forward's products)
     Plan plan_gate() const
     {
@@ -114,7 +125,7 @@ struct Sizes {
     size_t bwd_bytes() const { return 2 * hidden_bytes() + (tiled() ? std::max(plan_dx().parts_bytes, plan_weights().parts_bytes) : 0); }
 };
 
-template <int KIND, typename S, bool A_SLOW, bool B_SLOW>
+template <int KIND, typename S, bool A_SLOW, bool B_SLOW, bool EVEN>
 hdt_status_t launch_tiles(const char *name, const Product *of, int products, const Plan &plan, void *parts, hipStream_t st)
 {
     TileArgs a = {};
@@ -133,7 +144,7 @@ hdt_status_t launch_tiles(const char *name, const Product *of, int products, con
                   p.lda, p.ldb, p.ldo, p.m, p.n, tiles_m, tiles_n, first};
         first += (unsigned)tiles_m * tiles_n;
     }
-    const auto kernel = k_ffn_tile<KIND, S, A_SLOW, B_SLOW>;
+    const auto kernel = k_ffn_tile<KIND, S, A_SLOW, B_SLOW, EVEN>;
     if (S::LDS > 65536) HDT_HIP_TRY(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS));
     {
         HdtTimer t(name, st);
@@ -142,16 +153,16 @@ hdt_status_t launch_tiles(const char *name, const Product *of, int products, con
     }
     if (plan.direct == plan.tiles) return HDT_OK;
     HdtTimer t("hdt_ffn_join", st);
-    hipLaunchKernelGGL(k_ffn_join<S>, dim3((plan.tiles - plan.direct) * S::MB * S::NB), dim3(S::THREADS), 0, st, a);
+    hipLaunchKernelGGL((k_ffn_join<S, EVEN>), dim3((plan.tiles - plan.direct) * S::MB * S::NB), dim3(S::THREADS), 0, st, a);
     HDT_HIP_TRY(hipGetLastError());
     return HDT_OK;
 }
 
 template <int KIND>
-hdt_status_t make_few(const char *name, const Product &p, hipStream_t st)
+hdt_status_t make_few(const char *name, const Product &p, bool even, hipStream_t st)
 {
     HdtTimer t(name, st);
-    launch_few<KIND>(p, st);
+    even ? launch_few<KIND, true>(p, st) : launch_few<KIND, false>(p, st);
     HDT_HIP_TRY(hipGetLastError());
     return HDT_OK;
 }
@@ -159,13 +170,16 @@ hdt_status_t make_few(const char *name, const Product &p, hipStream_t st)
 template <int KIND, bool A_SLOW, bool B_SLOW>
 hdt_status_t make(const char *name, const Product *of, int products, const Sizes &s, Plan (Sizes::*plan_fn)() const, void *parts, hipStream_t st)
 {
-    if (s.tiled() && of[0].m > 0 && of[0].k > 0) {
-        const Plan plan = (s.*plan_fn)();
-        if (plan.shape == 0) return launch_tiles<KIND, Large, A_SLOW, B_SLOW>(name, of, products, plan, parts, st);
-        return launch_tiles<KIND, Small, A_SLOW, B_SLOW>(name, of, products, plan, parts, st);
+    if (!s.tiled()) {
+        HdtTimer t(name, st);
+        return launch_plain<KIND, A_SLOW, B_SLOW>(of, products, st);
     }
-    HdtTimer t(name, st);
-    return s.dt == HDT_BF16 ? launch_plain<__bf16, KIND, A_SLOW, B_SLOW>(of, products, st) : launch_plain<float, KIND, A_SLOW, B_SLOW>(of, products, st);
+    const Plan plan = (s.*plan_fn)();
+    if (s.even())
+        return plan.shape == 0 ? launch_tiles<KIND, Large, A_SLOW, B_SLOW, true>(name, of, products, plan, parts, st)
+                               : launch_tiles<KIND, Small, A_SLOW, B_SLOW, true>(name, of, products, plan, parts, st);
+    return plan.shape == 0 ? launch_tiles<KIND, Large, A_SLOW, B_SLOW, false>(name, of, products, plan, parts, st)
+                           : launch_tiles<KIND, Small, A_SLOW, B_SLOW, false>(name, of, products, plan, parts, st);
 }
 
 #define HDT_EXPORT extern "C" __attribute__((visibility("default")))
@@ -209,10 +223,10 @@ HDT_EXPORT hdt_status_t hdt_ffn_fwd(const void *x, const void *w_gate, const voi
     Product p = {};
     p.a[0] = x, p.b[0] = w_gate, p.b[1] = w_up, p.lda = width, p.ldb = width, p.m = (int)rows, p.n = inner, p.k = width, p.ranges = 1;
     p.out[0] = by_gate, p.out[1] = by_up, p.out[2] = h, p.ldo = inner, p.act = act;
-    if (hdt_status_t r = s.few() ? make_few<GATE>("hdt_ffn_gate", p, st) : make<GATE, false, false>("hdt_ffn_gate", &p, 1, s, &Sizes::plan_gate, nullptr, st)) return r;
+    if (hdt_status_t r = s.few() ? make_few<GATE>("hdt_ffn_gate", p, s.even(), st) : make<GATE, false, false>("hdt_ffn_gate", &p, 1, s, &Sizes::plan_gate, nullptr, st)) return r;
     p = {};
     p.a[0] = h, p.b[0] = w_down, p.lda = inner, p.ldb = inner, p.m = (int)rows, p.n = width, p.k = inner, p.ranges = 1, p.out[0] = y, p.ldo = width;
-    return s.few() ? make_few<STORE>("hdt_ffn_down", p, st) : make<STORE, false, false>("hdt_ffn_down", &p, 1, s, &Sizes::plan_down, parts, st);
+    return s.few() ? make_few<STORE>("hdt_ffn_down", p, s.even(), st) : make<STORE, false, false>("hdt_ffn_down", &p, 1, s, &Sizes::plan_down, parts, st);
 }
 
 HDT_EXPORT size_t hdt_ffn_bwd_workspace_bytes(int64_t rows, int32_t width, int32_t inner, hdt_dtype_t dt)

@@ -5,17 +5,15 @@
 // from memory to registers: a weight is read once, by one wave.
 #pragma once
 
-#include "hdt_ffn.h"
+#include "hdt_ffn_tile.h"
 
 namespace hdt_ffn {
 
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-
 // BLOCKS: of 16 rows of x.  GATE: weights p.b[0], p.b[1]; else p.b[0].
-template <int KIND, int WAVES, int BLOCKS>
+template <int KIND, int WAVES, int BLOCKS, bool EVEN>
 __global__ __launch_bounds__(WAVES * 64) void k_ffn_few(Product p)
 {
-    constexpr int COLS = KIND == GATE ? 8 : 16, AHEAD = 4;
+    constexpr int COLS = KIND == GATE ? 8 : 16, AHEAD = BLOCKS <= 2 ? 8 : 4;
     __shared__ float lds[WAVES][BLOCKS][16][17];  // [..][row of x][sum]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15;
     const int n0 = blockIdx.x * COLS;
@@ -29,14 +27,14 @@ __global__ __launch_bounds__(WAVES * 64) void k_ffn_few(Product p)
         bf16x8 wv[AHEAD], xv[AHEAD][BLOCKS];
 #pragma unroll
         for (int u = 0; u < AHEAD; u++) {
-            const int k = k0 + u * WAVES * 32 + (lane >> 4) * 8;  // (k is a multiple of eight)
+            const int k = k0 + u * WAVES * 32 + (lane >> 4) * 8, left = p.k - k;
             wv[u] = zero_bf16x8();
 #pragma unroll
             for (int b = 0; b < BLOCKS; b++) xv[u][b] = zero_bf16x8();
-            if (k < p.k) {
-                wv[u] = *reinterpret_cast<const bf16x8 *>(w + k);
+            if (left > 0) {
+                wv[u] = load_chunk<EVEN>(w + k, left);
 #pragma unroll
-                for (int b = 0; b < BLOCKS; b++) xv[u][b] = *reinterpret_cast<const bf16x8 *>(x[b] + k);
+                for (int b = 0; b < BLOCKS; b++) xv[u][b] = load_chunk<EVEN>(x[b] + k, left);
             }
         }
 #pragma unroll
@@ -76,17 +74,17 @@ __global__ __launch_bounds__(WAVES * 64) void k_ffn_few(Product p)
 
 constexpr int kFew = 64;  // most rows
 
-template <int KIND>
+template <int KIND, bool EVEN>
 void launch_few(const Product &p, hipStream_t st)
 {
     constexpr int WAVES = KIND == GATE ? 8 : 16;
     const dim3 grid((unsigned)((p.n + (KIND == GATE ? 7 : 15)) / (KIND == GATE ? 8 : 16))), block(WAVES * 64);
     if (p.m <= 16)
-        hipLaunchKernelGGL((k_ffn_few<KIND, WAVES, 1>), grid, block, 0, st, p);
+        hipLaunchKernelGGL((k_ffn_few<KIND, WAVES, 1, EVEN>), grid, block, 0, st, p);
     else if (p.m <= 32)
-        hipLaunchKernelGGL((k_ffn_few<KIND, WAVES, 2>), grid, block, 0, st, p);
+        hipLaunchKernelGGL((k_ffn_few<KIND, WAVES, 2, EVEN>), grid, block, 0, st, p);
     else
-        hipLaunchKernelGGL((k_ffn_few<KIND, WAVES, 4>), grid, block, 0, st, p);
+        hipLaunchKernelGGL((k_ffn_few<KIND, WAVES, 4, EVEN>), grid, block, 0, st, p);
 }
 
 }  // namespace hdt_ffn

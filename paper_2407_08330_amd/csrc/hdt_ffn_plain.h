@@ -1,53 +1,30 @@
-// The products of the gated feed-forward block for every size, type and alignment: operands taken element by element.
+// The products of the gated feed-forward block in fp32.
 #pragma once
 
 #include "hdt_ffn.h"
 
 namespace hdt_ffn {
 
-template <typename T>
-struct PlainOp;
-template <>
-struct PlainOp<__bf16> {
-    static constexpr int STEP = 16, PAD = 8;
-    // row l % 32, k = (l / 32) 8 + 0 .. 7
-    static __device__ __forceinline__ f32x16 mma(const __bf16 *a, const __bf16 *b, int lane, f32x16 c)
-    {
-        const int k = (lane >> 5) * 8;
-        return mfma_32x32x16(*reinterpret_cast<const bf16x8 *>(a + k), *reinterpret_cast<const bf16x8 *>(b + k), c);
-    }
-};
-template <>
-struct PlainOp<float> {
-    static constexpr int STEP = 2, PAD = 2;
-    static __device__ __forceinline__ f32x16 mma(const float *a, const float *b, int lane, f32x16 c)
-    {
-        return __builtin_amdgcn_mfma_f32_32x32x2f32(a[lane >> 5], b[lane >> 5], c, 0, 0, 0);
-    }
-};
-
 // A group of W x W waves makes a tile, a wave 32 x 32 of it (two sums of them for GATE).  GROUPS of them divide k, 32 at a time, and join at the end
 // in a fixed order: where there are few tiles a tile's walk along k is what takes the time.  A tile of k is requested before the one in
 // front of it is multiplied.  What is beyond m, n or k counts as zero on both sides, so that nothing there, NaN or not, is met.  C^T = B A^T: a
 // lane holds one m and rows of n.
 constexpr int kPlainK = 32;
-template <typename T>
-constexpr int plain_row() { return kPlainK + PlainOp<T>::PAD; }
-template <typename T, int KIND, int W, int GROUPS>
-constexpr int plain_lds() { return GROUPS * (KIND == GATE ? 3 : 2) * 32 * W * plain_row<T>() * (int)sizeof(T); }
+constexpr int kPlainRow = kPlainK + 2;  // floats of a row in LDS
+template <int KIND, int W, int GROUPS>
+constexpr int plain_lds() { return GROUPS * (KIND == GATE ? 3 : 2) * 32 * W * kPlainRow * (int)sizeof(float); }
 struct PlainArgs {
     Product p[3];
     unsigned first[3], tiles;  // first tile of each product; of all
 };
 
-template <typename T, int KIND, bool A_SLOW, bool B_SLOW, int W, int GROUPS>
+template <int KIND, bool A_SLOW, bool B_SLOW, int W, int GROUPS>
 __global__ __launch_bounds__(64 * W * W * GROUPS) void k_ffn_plain(PlainArgs a)
 {
-    using Op = PlainOp<T>;
-    constexpr int LD = plain_row<T>(), NB = KIND == GATE ? 2 : 1, SIDE = 32 * W, THREADS = 64 * W * W, EACH = SIDE * kPlainK / THREADS, TILE = SIDE * LD;
+    constexpr int LD = kPlainRow, NB = KIND == GATE ? 2 : 1, SIDE = 32 * W, THREADS = 64 * W * W, EACH = SIDE * kPlainK / THREADS, TILE = SIDE * LD;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int all = threadIdx.x, group = __builtin_amdgcn_readfirstlane(all / THREADS), tid = all % THREADS, lane = tid & 63, wave = tid >> 6;
-    T *const sa = reinterpret_cast<T *>(smem) + group * (1 + NB) * TILE, *const sb = sa + TILE;
+    float *const sa = reinterpret_cast<float *>(smem) + group * (1 + NB) * TILE, *const sb = sa + TILE;
     const int which = blockIdx.x >= a.first[2] ? 2 : blockIdx.x >= a.first[1] ? 1 : 0;
     const Product &p = a.p[which];
     const int64_t tiles_n = (p.n + SIDE - 1) / SIDE, tile = blockIdx.x - a.first[which];
@@ -59,19 +36,19 @@ __global__ __launch_bounds__(64 * W * W * GROUPS) void k_ffn_plain(PlainArgs a)
         for (int e = 0; e < 16; e++) acc[b][e] = 0.f;
 
     struct Part {
-        T v[EACH];
+        float v[EACH];
     };
     auto row_of = [&](bool slow, int i) { return slow ? tid % SIDE : tid / kPlainK + THREADS / kPlainK * i; };
     auto k_of = [&](bool slow, int i) { return slow ? tid / SIDE + THREADS / SIDE * i : tid % kPlainK; };
-    auto take = [&](Part &to, const T *from, int64_t ld, bool slow, int r0, int rows, int k0) __attribute__((always_inline)) {
+    auto take = [&](Part &to, const float *from, int64_t ld, bool slow, int r0, int rows, int k0) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < EACH; i++) {
             const int r = r0 + row_of(slow, i), k = k0 + k_of(slow, i);
-            to.v[i] = (T)0.f;
+            to.v[i] = 0.f;
             if (r < rows && k < p.k) to.v[i] = slow ? from[(int64_t)k * ld + r] : from[(int64_t)r * ld + k];
         }
     };
-    auto put = [&](T *to, const Part &from, bool slow) __attribute__((always_inline)) {
+    auto put = [&](float *to, const Part &from, bool slow) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < EACH; i++) to[row_of(slow, i) * LD + k_of(slow, i)] = from.v[i];
     };
@@ -79,9 +56,9 @@ __global__ __launch_bounds__(64 * W * W * GROUPS) void k_ffn_plain(PlainArgs a)
     Part va, vb[NB];
     auto request = [&](int t) __attribute__((always_inline)) {
         const int range = t >= per_range, k0 = t < steps ? (t - range * per_range) * kPlainK : p.k;  // (beyond the end: zeros)
-        take(va, (const T *)(range ? p.a[1] : p.a[0]), p.lda, A_SLOW, m0, p.m, k0);
+        take(va, (const float *)(range ? p.a[1] : p.a[0]), p.lda, A_SLOW, m0, p.m, k0);
 #pragma unroll
-        for (int b = 0; b < NB; b++) take(vb[b], (const T *)((NB == 2 ? b : range) ? p.b[1] : p.b[0]), p.ldb, B_SLOW, n0, p.n, k0);
+        for (int b = 0; b < NB; b++) take(vb[b], (const float *)((NB == 2 ? b : range) ? p.b[1] : p.b[0]), p.ldb, B_SLOW, n0, p.n, k0);
     };
     if (rounds > 0) request(group);
     for (int i = 0; i < rounds; i++) {
@@ -91,15 +68,15 @@ __global__ __launch_bounds__(64 * W * W * GROUPS) void k_ffn_plain(PlainArgs a)
         for (int b = 0; b < NB; b++) put(sb + b * TILE, vb[b], B_SLOW);
         __syncthreads();
         if (i + 1 < rounds) request((i + 1) * GROUPS + group);
-        const T *pa = sa + (wave / W * 32 + (lane & 31)) * LD;
+        const float *pa = sa + (wave / W * 32 + (lane & 31)) * LD + (lane >> 5), *pb = sb + (wave % W * 32 + (lane & 31)) * LD + (lane >> 5);
 #pragma unroll
-        for (int k = 0; k < kPlainK; k += Op::STEP)
+        for (int k = 0; k < kPlainK; k += 2)
 #pragma unroll
-            for (int b = 0; b < NB; b++) acc[b] = Op::mma(sb + b * TILE + (wave % W * 32 + (lane & 31)) * LD + k, pa + k, lane, acc[b]);
+            for (int b = 0; b < NB; b++) acc[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(pb[b * TILE + k], pa[k], acc[b], 0, 0, 0);
     }
     if (GROUPS > 1) {
         float *const join = reinterpret_cast<float *>(smem);  // [threads][17]: one group's sums at a time
-        static_assert(GROUPS == 1 || THREADS * 17 * 4 <= plain_lds<T, KIND, W, GROUPS>(), "room for a group's sums");
+        static_assert(GROUPS == 1 || THREADS * 17 * 4 <= plain_lds<KIND, W, GROUPS>(), "room for a group's sums");
 #pragma unroll
         for (int b = 0; b < NB; b++)
             for (int g = 1; g < GROUPS; g++) {
@@ -127,15 +104,15 @@ __global__ __launch_bounds__(64 * W * W * GROUPS) void k_ffn_plain(PlainArgs a)
                 const float u = acc[NB - 1][e];
                 const Act f = activate<true, decltype(act)::value>(acc[0][e]);
                 if (p.out[0]) {
-                    ((T *)p.out[0])[at] = (T)(u * f.slope);
-                    ((T *)p.out[1])[at] = (T)f.value;
+                    ((float *)p.out[0])[at] = u * f.slope;
+                    ((float *)p.out[1])[at] = f.value;
                 }
-                ((T *)p.out[2])[at] = (T)(f.value * u);
+                ((float *)p.out[2])[at] = f.value * u;
             } else if (KIND == DGATE) {
-                ((T *)p.out[0])[at] = (T)(acc[0][e] * (float)((const T *)p.by_gate)[at]);
-                ((T *)p.out[1])[at] = (T)(acc[0][e] * (float)((const T *)p.by_up)[at]);
+                ((float *)p.out[0])[at] = acc[0][e] * ((const float *)p.by_gate)[at];
+                ((float *)p.out[1])[at] = acc[0][e] * ((const float *)p.by_up)[at];
             } else {
-                ((T *)p.out[0])[at] = (T)acc[0][e];
+                ((float *)p.out[0])[at] = acc[0][e];
             }
         }
     };
@@ -145,10 +122,10 @@ __global__ __launch_bounds__(64 * W * W * GROUPS) void k_ffn_plain(PlainArgs a)
         finish(Constant<0>());
 }
 
-template <typename T, int KIND, bool A_SLOW, bool B_SLOW, int W, int GROUPS>
+template <int KIND, bool A_SLOW, bool B_SLOW, int W, int GROUPS>
 hdt_status_t launch_plain_as(const Product *of, int products, hipStream_t st)
 {
-    constexpr int SIDE = 32 * W, LDS = plain_lds<T, KIND, W, GROUPS>();
+    constexpr int SIDE = 32 * W, LDS = plain_lds<KIND, W, GROUPS>();
     PlainArgs a = {};
     for (int i = 0; i < 3; i++) {
         a.first[i] = ~0u;
@@ -157,7 +134,7 @@ hdt_status_t launch_plain_as(const Product *of, int products, hipStream_t st)
         a.first[i] = a.tiles;
         a.tiles += (unsigned)(((int64_t)of[i].m + SIDE - 1) / SIDE * (((int64_t)of[i].n + SIDE - 1) / SIDE));
     }
-    const auto kernel = k_ffn_plain<T, KIND, A_SLOW, B_SLOW, W, GROUPS>;
+    const auto kernel = k_ffn_plain<KIND, A_SLOW, B_SLOW, W, GROUPS>;
     if (LDS > 65536) HDT_HIP_TRY(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
     hipLaunchKernelGGL(kernel, dim3(a.tiles), dim3(64 * W * W * GROUPS), LDS, st, a);
     HDT_HIP_TRY(hipGetLastError());
@@ -165,15 +142,15 @@ hdt_status_t launch_plain_as(const Product *of, int products, hipStream_t st)
 }
 
 // Tiles of 64 x 64; where those do not fill the chip four groups of a workgroup divide k, and where they do not give each compute unit one,
-// tiles of 32 x 32, eight of whose waves divide k (fp32, 512 x 384 x 1000, forward and backward, us: one group 752, four 205, all three NNN)
-template <typename T, int KIND, bool A_SLOW, bool B_SLOW>
+// tiles of 32 x 32, eight of whose waves divide k (fp32, 512 x 384 x 1000, forward and backward, us: one group 752, four 205, all three 160)
+template <int KIND, bool A_SLOW, bool B_SLOW>
 hdt_status_t launch_plain(const Product *of, int products, hipStream_t st)
 {
     int64_t tiles = 0;
     for (int i = 0; i < products; i++) tiles += ((int64_t)of[i].m + 63) / 64 * (((int64_t)of[i].n + 63) / 64);
-    if (tiles <= 256) return launch_plain_as<T, KIND, A_SLOW, B_SLOW, 1, 8>(of, products, st);
-    if (tiles <= 512) return launch_plain_as<T, KIND, A_SLOW, B_SLOW, 2, 4>(of, products, st);
-    return launch_plain_as<T, KIND, A_SLOW, B_SLOW, 2, 1>(of, products, st);
+    if (tiles <= 256) return launch_plain_as<KIND, A_SLOW, B_SLOW, 1, 8>(of, products, st);
+    if (tiles <= 512) return launch_plain_as<KIND, A_SLOW, B_SLOW, 2, 4>(of, products, st);
+    return launch_plain_as<KIND, A_SLOW, B_SLOW, 2, 1>(of, products, st);
 }
 
 }  // namespace hdt_ffn

@@ -11,10 +11,12 @@
 // conflict (hdt_tile.h has the rule).  Rows of "slow" operands: one k, BM or BN values, read transposed; four consecutive k at the same
 // 64 bytes are moved apart.
 //
-// Rows beyond m or n read the last one there is and are not stored; of k what is beyond the end is written as zeros, on both sides.
+// Rows beyond m or n read the last one there is and are not stored; of k what is beyond the end is written as zeros, on both sides.  Where rows do
+// not begin at multiples of 16 bytes (EVEN: they do) tiles come by way of registers, in pieces of any alignment.
 #pragma once
 
 #include "hdt_ffn.h"
+#include "hdt_rows.h"
 #include "hdt_tile.h"
 
 namespace hdt_ffn {
@@ -25,6 +27,26 @@ using hdt_tile::dma16;
 using hdt_tile::lds_addr;
 using hdt_tile::wait_vmcnt;
 using hdt_tile::wg_barrier;
+
+// eight values, `left` of which exist.  EVEN: all, at a multiple of 16 bytes; else at any element.
+template <bool EVEN>
+__device__ __forceinline__ bf16x8 load_chunk(const __bf16 *p, int left)
+{
+    if (EVEN) return *reinterpret_cast<const bf16x8 *>(p);
+    return hdt_rows::load8<false>(p, left);
+}
+template <bool EVEN>
+__device__ __forceinline__ void store_chunk(__bf16 *p, bf16x8 v, int left)
+{
+    if (EVEN) {
+        *reinterpret_cast<bf16x8 *>(p) = v;
+        return;
+    }
+    hdt_rows::Eight e;
+#pragma unroll
+    for (int i = 0; i < 8; i++) e.x[i] = (float)v[i];
+    hdt_rows::store8<false>(p, e, left);
+}
 
 // a pointer that is the same for the whole wave, in scalar registers
 __device__ __forceinline__ const __bf16 *uniform(const __bf16 *p)
@@ -47,7 +69,7 @@ struct TileArgs {
     TileProduct p[3];
     int products, k, ranges;    // k of a range
     // The first `direct` tiles have a workgroup each (`spread` of them, a multiple of 8).  Each of the others is cut along k into `pieces` of `per` tiles of
-    // k, which workgroups make side by side, all tiles' first pieces before the second: what an XCD does at a time is at one place of k, and its
+    // k (the last of fewer where that is all), which workgroups make side by side, all tiles' first pieces before the second: what an XCD does at a time is at one place of k, and its
     // tiles share what they read.  What is left of the tiles, `rest` each, one behind the other, is divided among `sharers` further
     // workgroups, `per` each.  Sums that are not all of a tile go to `parts`, and k_ffn_join adds them up.
     unsigned direct, spread, tiles, piece_items, sharers;
@@ -84,7 +106,7 @@ struct Shape {
 };
 
 // One operand of R rows: how it comes to LDS, and how its blocks of 32 rows are read.  PERMUTED: in the order of the sums' rows.
-template <int R, int NW, int BK, bool SLOW, bool PERMUTED>
+template <int R, int NW, int BK, bool SLOW, bool PERMUTED, bool EVEN>
 struct Operand {
     static constexpr int CPR = (SLOW ? R : BK) / 8;     // chunks of 16 bytes a row in LDS
     static constexpr int LOADS = R * BK / 8 / 64 / NW;  // wave-level loads of a tile, for each wave
@@ -104,11 +126,13 @@ struct Operand {
     }
     uint32_t off[LOADS];  // bytes from the tile's first row (fast) or column (slow)
     int64_t ld;
+    int columns;          // slow: how many there are from the tile's first on
 
     // rows (fast) or columns (slow) first .. of `count`
     __device__ __forceinline__ void init(int64_t ld_, int first, int count, int wave, int lane)
     {
         ld = ld_;
+        columns = count - first;
 #pragma unroll
         for (int i = 0; i < LOADS; i++) {
             int row, chunk;
@@ -116,21 +140,22 @@ struct Operand {
             if (!SLOW)
                 off[i] = (uint32_t)(min(first + row, count - 1) - first) * (uint32_t)(ld * 2) + chunk * 16;
             else
-                off[i] = (uint32_t)row * (uint32_t)(ld * 2) + (uint32_t)(min(first + chunk * 8, count - 8) - first) * 2;
+                off[i] = (uint32_t)row * (uint32_t)(ld * 2) + (uint32_t)(EVEN ? min(first + chunk * 8, count - 8) - first : chunk * 8) * 2;
         }
     }
-    // the tile without direct loads, with zeros from `left` of k on.  base: of its first row or column; other: from there to the second
-    // weight, whose rows are every second block of 32
-    __device__ __forceinline__ void fill(const __bf16 *base, int64_t other, char *to, int left, int wave, int lane) const
+    // load i of the tile by way of registers, with zeros from `left` of k on.  base: of its first row or column; other: from there to the
+    // second weight, whose rows are every second block of 32
+    __device__ __forceinline__ bf16x8 take(int i, const __bf16 *base, int64_t other, int left, int wave, int lane) const
     {
-#pragma unroll
-        for (int i = 0; i < LOADS; i++) {
-            int row, chunk;
-            place(i, wave, lane, &row, &chunk);
-            bf16x8 v = zero_bf16x8();
-            if ((SLOW ? row : chunk * 8) < left) v = *reinterpret_cast<const bf16x8 *>((const char *)(base + (row >> 5 & 1 ? other : 0)) + off[i]);
-            *reinterpret_cast<bf16x8 *>(to + (i * NW + wave) * 1024 + lane * 16) = v;
-        }
+        int row, chunk;
+        place(i, wave, lane, &row, &chunk);
+        const __bf16 *p = (const __bf16 *)((const char *)(base + (row >> 5 & 1 ? other : 0)) + off[i]);
+        const int there = SLOW ? (row >= left ? 0 : EVEN ? 8 : columns - chunk * 8) : left - chunk * 8;
+        return there > 0 ? load_chunk<EVEN>(p, there) : zero_bf16x8();
+    }
+    __device__ __forceinline__ void put(int i, bf16x8 v, char *to, int wave, int lane) const
+    {
+        *reinterpret_cast<bf16x8 *>(to + (i * NW + wave) * 1024 + lane * 16) = v;
     }
 
     // where a lane reads, at the first 16 of k; blocks: of 32 rows from `first` on
@@ -166,7 +191,7 @@ __device__ __forceinline__ int result_at(int r, int c)
 }
 
 // tiles of k t0 .. t1 - 1 of a tile; part: where sums go that are not all of it
-template <int KIND, typename S, bool A_SLOW, bool B_SLOW>
+template <int KIND, typename S, bool A_SLOW, bool B_SLOW, bool EVEN>
 __device__ __forceinline__ void make_tile(const TileArgs &a, char *smem, unsigned tile, int t0, int t1, float *part)
 {
     constexpr int MB = S::MB, NB = S::NB, NW = S::NW, BK = S::BK;
@@ -176,8 +201,8 @@ __device__ __forceinline__ void make_tile(const TileArgs &a, char *smem, unsigne
     const int m0 = at.m, n0 = at.n * (KIND == GATE ? S::BN / 2 : S::BN);
 
     const int per_range = (a.k + BK - 1) / BK, whole = a.k / BK;
-    Operand<S::BM, NW, BK, A_SLOW, false> oa;
-    Operand<S::BN, NW, BK, B_SLOW, true> ob;
+    Operand<S::BM, NW, BK, A_SLOW, false, EVEN> oa;
+    Operand<S::BN, NW, BK, B_SLOW, true, EVEN> ob;
     oa.init(p.lda, m0, p.m, wave, lane);
     if (KIND != GATE) {
         ob.init(p.ldb, n0, p.n, wave, lane);
@@ -195,7 +220,7 @@ __device__ __forceinline__ void make_tile(const TileArgs &a, char *smem, unsigne
     oa.template reader<MB>(wm, lane);
     ob.template reader<NB>(wn, lane);
 
-    auto is_whole = [&](int t) { return (t >= per_range ? t - per_range : t) < whole; };
+    auto is_whole = [&](int t) { return EVEN && (t >= per_range ? t - per_range : t) < whole; };
     struct From {
         const __bf16 *a, *b;
         int left;  // of k
@@ -217,10 +242,16 @@ __device__ __forceinline__ void make_tile(const TileArgs &a, char *smem, unsigne
                   __builtin_amdgcn_readfirstlane(to + S::A_BYTES + (uint32_t)(j * NW + wave) * 1024u));
         }
     };
-    auto fill = [&](const From &f, int stage) {
+    // a tile by way of registers: the last of k where it is not whole, and every tile where rows do not begin at multiples of 16 bytes
+    bf16x8 held[S::LOADS];
+    auto take = [&](const From &f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < S::LOADS; i++) held[i] = i < oa.LOADS ? oa.take(i, f.a, 0, f.left, wave, lane) : ob.take(i - oa.LOADS, f.b, up, f.left, wave, lane);
+    };
+    auto put = [&](int stage) __attribute__((always_inline)) {
         char *to = smem + stage * S::STAGE;
-        oa.fill(f.a, 0, to, f.left, wave, lane);
-        ob.fill(f.b, up, to + S::A_BYTES, f.left, wave, lane);
+#pragma unroll
+        for (int i = 0; i < S::LOADS; i++) i < oa.LOADS ? oa.put(i, held[i], to, wave, lane) : ob.put(i - oa.LOADS, held[i], to + S::A_BYTES, wave, lane);
     };
     auto load = [&](int t, int stage) {
         const From f = from(t);
@@ -228,7 +259,8 @@ __device__ __forceinline__ void make_tile(const TileArgs &a, char *smem, unsigne
 #pragma unroll
             for (int i = 0; i < S::LOADS; i++) request(f, stage, i);
         } else {
-            fill(f, stage);
+            take(f);
+            put(stage);
         }
     };
 
@@ -261,6 +293,7 @@ __device__ __forceinline__ void make_tile(const TileArgs &a, char *smem, unsigne
     };
     // a stage is requested STAGES - 1 ahead; before it is read, those behind it may still be on their way
     auto arrived = [&](int t) {  // tile t has, for this wave
+        if (!EVEN) return;
         constexpr int MORE = (S::STAGES - 2) * S::LOADS;
         bool direct = t + S::STAGES - 2 < t1;
 #pragma unroll
@@ -282,12 +315,16 @@ __device__ __forceinline__ void make_tile(const TileArgs &a, char *smem, unsigne
             const int next = stage + 1 == S::STAGES ? 0 : stage + 1, ahead = t + S::STAGES - 1;
             const From fr = from(min(ahead, t1 - 1));
             const bool direct = ahead < t1 && is_whole(ahead);
-            if (ahead < t1 && !direct) fill(fr, before);
+            if (ahead < t1 && !direct) {
+                take(fr);
+                if (EVEN) put(before);
+            }
 #pragma unroll
             for (int s = 0; s < S::STEPS; s++) {
                 if (s + 1 < S::STEPS) {
                     read(f[(s + 1) & 1], stage, s + 1);
                 } else if (t + 1 < t1) {
+                    if (!EVEN && ahead < t1) put(before);
                     arrived(t + 1);
                     wg_barrier();
                     read(f[0], next, 0);
@@ -361,7 +398,7 @@ __device__ __forceinline__ void make_tile(const TileArgs &a, char *smem, unsigne
                     for (int q = 0; q < GROUP * CH / S::THREADS; q++) {
                         const int r = (q * S::THREADS + tid) / CH, chunk = (q * S::THREADS + tid) % CH, m = row_of(r, i), n = n0 + chunk * 8;
                         const bf16x8 v = *reinterpret_cast<const bf16x8 *>(buf + o * BUFFER + result_at<CH>(r, chunk));
-                        if (m < p.m && n < p.n) *reinterpret_cast<bf16x8 *>(p.out[o] + (int64_t)m * p.ldo + n) = v;
+                        if (m < p.m && n < p.n) store_chunk<EVEN>(p.out[o] + (int64_t)m * p.ldo + n, v, p.n - n);
                     }
             }
         };
@@ -381,13 +418,18 @@ __device__ __forceinline__ void make_tile(const TileArgs &a, char *smem, unsigne
         struct Factors {
             bf16x8 g[EACH], u[EACH];
         } with[2];
-        auto factors = [&](int i) {
+        auto factors = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
             for (int q = 0; q < EACH; q++) {
                 const int r = (q * S::THREADS + tid) / CH, chunk = (q * S::THREADS + tid) % CH;
-                const int64_t at = (int64_t)min(row_of(r, i), p.m - 1) * p.ldo + min(n0 + chunk * 8, p.n - 8);
-                with[i & 1].g[q] = *reinterpret_cast<const bf16x8 *>(p.by_gate + at);
-                with[i & 1].u[q] = *reinterpret_cast<const bf16x8 *>(p.by_up + at);
+                const int n = n0 + chunk * 8;
+                const int64_t at = (int64_t)min(row_of(r, i), p.m - 1) * p.ldo + (EVEN ? min(n, p.n - 8) : n);
+                if (EVEN || n < p.n) {
+                    with[i & 1].g[q] = load_chunk<EVEN>(p.by_gate + at, p.n - n);
+                    with[i & 1].u[q] = load_chunk<EVEN>(p.by_up + at, p.n - n);
+                } else {
+                    with[i & 1].g[q] = with[i & 1].u[q] = zero_bf16x8();
+                }
             }
         };
         factors(0);
@@ -414,29 +456,29 @@ __device__ __forceinline__ void make_tile(const TileArgs &a, char *smem, unsigne
                     }
                 }
                 if (m < p.m && n < p.n) {
-                    *reinterpret_cast<bf16x8 *>(p.out[0] + (int64_t)m * p.ldo + n) = vg;
-                    *reinterpret_cast<bf16x8 *>(p.out[1] + (int64_t)m * p.ldo + n) = vu;
+                    store_chunk<EVEN>(p.out[0] + (int64_t)m * p.ldo + n, vg, p.n - n);
+                    store_chunk<EVEN>(p.out[1] + (int64_t)m * p.ldo + n, vu, p.n - n);
                 }
             }
         }
     }
 }
 
-template <int KIND, typename S, bool A_SLOW, bool B_SLOW>
+template <int KIND, typename S, bool A_SLOW, bool B_SLOW, bool EVEN>
 __global__ __launch_bounds__(S::THREADS, 2) void k_ffn_tile(TileArgs a)
 {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int k_tiles = a.ranges * ((a.k + S::BK - 1) / S::BK);
     if (KIND != STORE || blockIdx.x < a.spread) {
         const unsigned tile = hdt_tile::logical_block(blockIdx.x, a.chunk);
-        if (tile < a.direct) make_tile<KIND, S, A_SLOW, B_SLOW>(a, smem, tile, 0, k_tiles, nullptr);
+        if (tile < a.direct) make_tile<KIND, S, A_SLOW, B_SLOW, EVEN>(a, smem, tile, 0, k_tiles, nullptr);
         return;
     }
     const unsigned cut = a.tiles - a.direct, block = blockIdx.x - a.spread;
     constexpr size_t SIZE = (size_t)S::BM * S::BN;
     if (block < a.piece_items) {
         const unsigned item = by_xcd(block, a.piece_items), piece = item / cut, tile = item - piece * cut;
-        if (piece < (unsigned)a.pieces) make_tile<KIND, S, A_SLOW, B_SLOW>(a, smem, a.direct + tile, piece * a.per, (piece + 1) * a.per, a.parts + item * SIZE);
+        if (piece < (unsigned)a.pieces) make_tile<KIND, S, A_SLOW, B_SLOW, EVEN>(a, smem, a.direct + tile, piece * a.per, min((int)(piece + 1) * a.per, k_tiles), a.parts + item * SIZE);
         return;
     }
     const unsigned me = by_xcd(block - a.piece_items, a.sharers);
@@ -446,14 +488,14 @@ __global__ __launch_bounds__(S::THREADS, 2) void k_ffn_tile(TileArgs a)
         const int64_t tile = at / a.rest;
         const int t0 = (int)(at - tile * a.rest), t1 = (int)min((int64_t)a.rest, t0 + (end - at)), from = a.pieces * a.per;
         wg_barrier();  // (the LDS of the tile before is no longer read)
-        make_tile<KIND, S, A_SLOW, B_SLOW>(a, smem, a.direct + (unsigned)tile, from + t0, from + t1,
+        make_tile<KIND, S, A_SLOW, B_SLOW, EVEN>(a, smem, a.direct + (unsigned)tile, from + t0, from + t1,
                                            t1 - t0 == k_tiles ? nullptr : a.parts + ((size_t)a.pieces * cut + me + tile) * SIZE);
         at += t1 - t0;
     }
 }
 
 // The parts of the tiles that were cut, added up in the order of k: a workgroup has a block of each of a tile's waves.
-template <typename S>
+template <typename S, bool EVEN>
 __global__ __launch_bounds__(S::THREADS) void k_ffn_join(TileArgs a)
 {
     constexpr int MB = S::MB, NB = S::NB;
@@ -487,7 +529,7 @@ __global__ __launch_bounds__(S::THREADS) void k_ffn_join(TileArgs a)
         bf16x8 v;
 #pragma unroll
         for (int e = 0; e < 8; e++) v[e] = (__bf16)sum[2 * h + (e >> 2)][e & 3];
-        *reinterpret_cast<bf16x8 *>(p.out[0] + (int64_t)m * p.ldo + n) = v;
+        store_chunk<EVEN>(p.out[0] + (int64_t)m * p.ldo + n, v, p.n - n);
     }
 }
 
