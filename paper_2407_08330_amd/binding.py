@@ -909,7 +909,7 @@ def _check_ffn(x, w_gate, w_up, w_down):
 
 def _check_results(ts, shape, like):
     for t in ts:
-        if t.shape != shape or t.dtype != like.dtype or not (t.is_cuda and t.is_contiguous()):
+        if t is None or t.shape != shape or t.dtype != like.dtype or not (t.is_cuda and t.is_contiguous()):
             raise ValueError(f"tensors must be contiguous device tensors {tuple(shape)} of {like.dtype}")
 
 
