@@ -28,18 +28,24 @@ using hdt_tile::lds_addr;
 using hdt_tile::wait_vmcnt;
 using hdt_tile::wg_barrier;
 
-// eight values, `left` of which exist.  EVEN: all, at a multiple of 16 bytes; else at any element.
-template <bool EVEN>
+// Eight values, `left` of which exist.  EVEN: all, at a multiple of 16 bytes; else at any element.  ONCE: what nothing soon to come reads
+// again, past the caches: the derivatives that the forward keeps, there and in the backward (H then waits for its product in the last cache: down
+// projection of 32768 rows 130 -> 119 us, dG and dU 195 -> 181).
+template <bool EVEN, bool ONCE = false>
 __device__ __forceinline__ bf16x8 load_chunk(const __bf16 *p, int left)
 {
+    if (EVEN && ONCE) return __builtin_nontemporal_load(reinterpret_cast<const bf16x8 *>(p));
     if (EVEN) return *reinterpret_cast<const bf16x8 *>(p);
     return hdt_rows::load8<false>(p, left);
 }
-template <bool EVEN>
+template <bool EVEN, bool ONCE = false>
 __device__ __forceinline__ void store_chunk(__bf16 *p, bf16x8 v, int left)
 {
     if (EVEN) {
-        *reinterpret_cast<bf16x8 *>(p) = v;
+        if (ONCE)
+            __builtin_nontemporal_store(v, reinterpret_cast<bf16x8 *>(p));
+        else
+            *reinterpret_cast<bf16x8 *>(p) = v;
         return;
     }
     hdt_rows::Eight e;
@@ -398,7 +404,8 @@ __device__ __forceinline__ void make_tile(const TileArgs &a, char *smem, unsigne
                     for (int q = 0; q < GROUP * CH / S::THREADS; q++) {
                         const int r = (q * S::THREADS + tid) / CH, chunk = (q * S::THREADS + tid) % CH, m = row_of(r, i), n = n0 + chunk * 8;
                         const bf16x8 v = *reinterpret_cast<const bf16x8 *>(buf + o * BUFFER + result_at<CH>(r, chunk));
-                        if (m < p.m && n < p.n) store_chunk<EVEN>(p.out[o] + (int64_t)m * p.ldo + n, v, p.n - n);
+                        __bf16 *const to = p.out[o] + (int64_t)m * p.ldo + n;
+                        if (m < p.m && n < p.n) KIND == GATE && o < 2 ? store_chunk<EVEN, true>(to, v, p.n - n) : store_chunk<EVEN>(to, v, p.n - n);
                     }
             }
         };
@@ -417,22 +424,19 @@ __device__ __forceinline__ void make_tile(const TileArgs &a, char *smem, unsigne
         static_assert(2 * BUFFER <= S::LDS, "room for two block rows");
         struct Factors {
             bf16x8 g[EACH], u[EACH];
-        } with[2];
-        auto factors = [&](int i) __attribute__((always_inline)) {
+        } with, next;
+        auto factors = [&](Factors &to, int i) __attribute__((always_inline)) {
 #pragma unroll
             for (int q = 0; q < EACH; q++) {
                 const int r = (q * S::THREADS + tid) / CH, chunk = (q * S::THREADS + tid) % CH;
                 const int n = n0 + chunk * 8;
                 const int64_t at = (int64_t)min(row_of(r, i), p.m - 1) * p.ldo + (EVEN ? min(n, p.n - 8) : n);
-                if (EVEN || n < p.n) {
-                    with[i & 1].g[q] = load_chunk<EVEN>(p.by_gate + at, p.n - n);
-                    with[i & 1].u[q] = load_chunk<EVEN>(p.by_up + at, p.n - n);
-                } else {
-                    with[i & 1].g[q] = with[i & 1].u[q] = zero_bf16x8();
-                }
+                bf16x8 g = zero_bf16x8(), u = g;
+                if (EVEN || n < p.n) g = load_chunk<EVEN, true>(p.by_gate + at, p.n - n), u = load_chunk<EVEN, true>(p.by_up + at, p.n - n);
+                to.g[q] = g, to.u[q] = u;
             }
         };
-        factors(0);
+        factors(next, 0);
 #pragma unroll
         for (int i = 0; i < MB; i++) {
             char *buf = smem + (i & 1) * BUFFER;
@@ -440,7 +444,8 @@ __device__ __forceinline__ void make_tile(const TileArgs &a, char *smem, unsigne
             for (int c = 0; c < NB * 4; c++)  // four columns
                 *reinterpret_cast<f32x4 *>(buf + result_at<CH * 2>(my_row, wave % S::WN * (NB * 8) + (c >> 2) * 8 + (c >> 1 & 1) * 4 + hf * 2 + (c & 1))) =
                     f32x4{acc[i][c >> 2][(c & 3) * 4], acc[i][c >> 2][(c & 3) * 4 + 1], acc[i][c >> 2][(c & 3) * 4 + 2], acc[i][c >> 2][(c & 3) * 4 + 3]};
-            if (i + 1 < MB) factors(i + 1);
+            with = next;
+            if (i + 1 < MB) factors(next, i + 1);
             wg_barrier();
 #pragma unroll
             for (int q = 0; q < EACH; q++) {
@@ -451,8 +456,8 @@ __device__ __forceinline__ void make_tile(const TileArgs &a, char *smem, unsigne
                     const f32x4 dh = *reinterpret_cast<const f32x4 *>(buf + result_at<CH * 2>(r, chunk * 2 + half));
 #pragma unroll
                     for (int e = 0; e < 4; e++) {
-                        vg[half * 4 + e] = (__bf16)(dh[e] * (float)with[i & 1].g[q][half * 4 + e]);
-                        vu[half * 4 + e] = (__bf16)(dh[e] * (float)with[i & 1].u[q][half * 4 + e]);
+                        vg[half * 4 + e] = (__bf16)(dh[e] * (float)with.g[q][half * 4 + e]);
+                        vu[half * 4 + e] = (__bf16)(dh[e] * (float)with.u[q][half * 4 + e]);
                     }
                 }
                 if (m < p.m && n < p.n) {
