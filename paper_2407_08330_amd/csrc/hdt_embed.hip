@@ -4,9 +4,12 @@
 //   hdt_embed_bwd  grad[v] = scale sum of d_out[t] over the t with id[t] = v, in ascending order of blocks of them (see k_embed_sum);
 //                  0 for rows without a token, or (accumulate) added to what stands there
 //
-// Both are bound by memory.  The backward has no atomics on values: k_embed_sort puts the tokens of each row side by side, in the order in
-// which they came; k_embed_sum adds up a block of consecutive ones a wave, so that a word that is a tenth of a text keeps no workgroup longer
-// than one that comes twice; k_embed_join adds up the rows that span several blocks.  Sums are in fp32 in a fixed order.
+// Both are bound by memory.  Forward, 32768 bf16 rows of 768 columns out of 32768: 19 us with nothing in the caches (67 MB, 3.5 TB/s), 11 with the table there;
+// 16384 rows of an fp32 table to bf16: 9.2 us.  The backward has no atomics on values: k_embed_sort puts the tokens of each row side by side, in the
+// order in which they came; k_embed_sum adds up a block of consecutive ones a wave, so that a word that is a tenth of a text keeps no
+// workgroup longer than one that comes twice; k_embed_join adds up the rows that span several blocks.  Sums are in fp32 in a fixed order.
+// Same sizes, words as frequent as 1 / rank: sort 19.8 us (a third of it the zeros of rows without a token, 30 MB; else every workgroup reading all ids
+// from the L2 and placing its own), sum 15.9 (50 MB read), join 6.
 #include <algorithm>
 
 #include "hdt_internal.h"
@@ -309,8 +312,9 @@ int shares_log2(int vocab)
     while (((int64_t)kMostRows << l) < vocab) l++;
     return l;
 }
-// entries a block: few tokens are spread over more waves
-int block_of(int64_t tokens) { return tokens <= 16384 ? 8 : 32; }
+// entries a block: few tokens are spread over more waves, many have fewer rows to join (us of sum and join, blocks of 8 | 16 | 32, 768 bf16 columns, with
+// about 5 of each for the events around it: 4096 tokens 14.4 | 15.6 | 19.9, 8192 16.5 | 16.4 | 19.8, 16384 22.3 | 19.6 | 21.4, 32768 31.0 | 25.8 | 25.1)
+int block_of(int64_t tokens) { return tokens <= 4096 ? 8 : tokens <= 16384 ? 16 : 32; }
 int64_t blocks_of(int64_t tokens) { return (tokens + block_of(tokens) - 1) / block_of(tokens); }
 size_t entries_bytes(int64_t tokens) { return ((size_t)tokens * sizeof(Entry) + 15) / 16 * 16; }
 

@@ -42,7 +42,10 @@ struct Dims {
 };
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-// slots: workgroups the chip holds; step, around: clocks of 64 of k with every unit full, and of what stands around a tile's walk
+// The rule is a sum of clocks: a walk along k, what stands around it, and the parts of tiles that are cut.  slots: workgroups the chip holds; step,
+// around: clocks of 64 of k with every unit full, and of what stands around a tile's walk.  As measured (us of forward and backward, kernels, Large |
+// Small): 32768 x 768 x 2048 1184 | 1413, 8192 x 1024 x 4096 741 | 799, 1999 x 1000 x 2504 240 | 200, 512 x 768 x 2048 137 | 101.  A unit with one
+// Small workgroup is no quicker a step than with two.
 template <typename S>
 void consider(const Dims *of, int products, int k, int ranges, bool divisible, int shape, unsigned slots, double step, double around, Plan *best, double *best_cost)
 {
@@ -134,7 +137,7 @@ hdt_status_t launch_tiles(const char *name, const Product *of, int products, con
     a.chunk = hdt_tile::FastDiv(chunk);
     a.direct = plan.direct, a.spread = hdt_tile::padded_grid(plan.direct, chunk), a.tiles = plan.tiles;
     a.piece_items = plan.piece_items, a.sharers = plan.sharers, a.pieces = plan.pieces, a.per = plan.per, a.rest = plan.rest;
-    a.act = of[0].act, a.group = 4;
+    a.act = of[0].act, a.group = 4;  // (2, 4 or 8: the same but for dG and dU, 200, 196 and 215-250 us)
     unsigned first = 0;
     for (int i = 0; i < products; i++) {
         const Product &p = of[i];

@@ -2,7 +2,8 @@
 //
 // A workgroup makes 16 rows of weights' sums with all rows of x, 16 x 16 blocks of them by matrix instructions: eight columns of the gate and the
 // same eight of up, or 16 columns of the last product.  Its waves divide k, 32 at a time, and join in LDS in a fixed order.  Operands go straight
-// from memory to registers: a weight is read once, by one wave.
+// from memory to registers: a weight is read once, by one wave.  One row of 768 x 2048: 3.7 and 4.5 us, of which the 9.4 MB of weights are 1.8; 32 rows of
+// 1024 x 2816: 8.3 and 9.8 (17 MB, and every workgroup reads all of x or H from the L2).
 #pragma once
 
 #include "hdt_ffn_tile.h"
@@ -72,7 +73,8 @@ __global__ __launch_bounds__(WAVES * 64) void k_ffn_few(Product p)
     }
 }
 
-constexpr int kFew = 64;  // most rows
+// most rows (us with events around each kernel, this way | in tiles: 8 rows of 1024 x 2816 16 | 37, 32 22 | 37, 64 32 | 38; of 768 x 2048 14 | 28, 17 | 28, 22 | 28)
+constexpr int kFew = 64;
 
 template <int KIND, bool EVEN>
 void launch_few(const Product &p, hipStream_t st)

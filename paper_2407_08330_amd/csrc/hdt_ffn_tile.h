@@ -7,6 +7,14 @@
 // C^T rather than C, and the rows of B (n) that an operand holds in the order 0-3, 8-11, 4-7, 12-15: a lane's sums are then eight
 // consecutive n at a time of one m, which leave as 16 bytes, and what the epilogue multiplies them with comes as 16 bytes.
 //
+// What bounds it: the direct loads.  At 32768 x 768 x 2048 the weights' gradients take 300 us (1.03 PFLOP/s) and dX 207 (1.0), without the loads 206
+// and 174, with all of them from the L2 265 and 221; the matrix pipe alone would take 155 and 103.  Hence 256 x 256, the most a compute unit's
+// registers hold, and tiles that run at the same time at the same place of k (dX 250 -> 203 us, the gradients 352 -> 298).  The loads are
+// requested between the products of a step, three stages ahead (all of them behind the barrier, four stages of 32: dX 269 us, now 249 before the
+// cuts).  Two workgroups a compute unit with tiles of 256 x 128 take 1.5 times the loads: gate 317-336 us against 306, gradients 394 against 328.
+// The forward's gate product takes 217 us where H alone leaves and 293 where its derivatives leave too (402 MB), dG and dU 178 (537 MB in and out): stores and
+// what comes from memory at a tile's end find the other waves at the same place, and the tile's walk is only 24 stages long.
+//
 // LDS tiles.  Rows of "fast" operands: 128 bytes, 64 of k, whose 16-byte chunks are exchanged so that 16 consecutive rows read without a
 // conflict (hdt_tile.h has the rule).  Rows of "slow" operands: one k, BM or BN values, read transposed; four consecutive k at the same
 // 64 bytes are moved apart.
@@ -366,7 +374,7 @@ __device__ __forceinline__ void make_tile(const TileArgs &a, char *smem, unsigne
         return;
     }
     // Results leave by LDS, block row by block row of all waves, so that a wave stores whole rows of the tile: by itself it has 32 or 64
-    // columns of 32 rows, and as many requests of a piece of a row each.
+    // columns of 32 rows, and as many requests of a piece of a row each (dG and dU 265 -> 204 us).
     wg_barrier();  // (the stages are no longer read)
     constexpr int GROUP = S::WM * 32;  // rows of a block row
     auto row_of = [&](int r, int i) { return m0 + (r >> 5) * MB * 32 + i * 32 + (r & 31); };
