@@ -1,6 +1,6 @@
 """Binding of libhdt.so: argument marshalling only.  Every step of the method runs in the
 HIP kernels behind the C ABI declared in ``include/hdt.h``; there is no fallback path, and a
-missing library is an error.  The calls every layer makes (build, forward, backward; relative-bias attention, dropout, norm) go through native code
+missing library is an error.  The calls every layer makes (build, forward, backward; relative-bias attention, dropout, norms, embeddings, feed-forward block) go through native code
 (``csrc/hdt_pycall.cpp``) where their arguments are plain tensors and numbers, and through ctypes otherwise; that module is
 compiled for one Python and one torch, and under others, or without it, ctypes takes all calls.
 

@@ -289,7 +289,7 @@ __global__ __launch_bounds__(256) void k_embed_join(BwdArgs a, int slabs)
 
 // ------------------------------------------------------------------------------------------ host
 constexpr int kMostWidth = 32768, kMostVocab = 1 << 24;
-constexpr int64_t kMostElements = 1ll << 35, kMostTokens = 1ll << 30;
+constexpr int64_t kMostElements = 1ll << 35, kMostTokens = 1ll << 28;  // (a launch has fewer than 2^32 threads)
 
 bool misaligned(const void *p, unsigned by = 16) { return ((uintptr_t)p & (by - 1)) != 0; }
 
@@ -301,7 +301,7 @@ hdt_status_t check_sizes(const char *fn, int64_t tokens, int32_t vocab, int32_t 
     if (table_dt != HDT_BF16 && table_dt != HDT_F32) return hdt_fail(HDT_ERR_UNSUPPORTED, "%s: unknown dtype %d of the table", fn, (int)table_dt);
     if (width < 1 || width > kMostWidth) return hdt_fail(HDT_ERR_SHAPE, "%s: width %d outside [1, %d]", fn, width, kMostWidth);
     if (vocab < 1 || vocab > kMostVocab) return hdt_fail(HDT_ERR_SHAPE, "%s: vocab %d outside [1, 2^24]", fn, vocab);
-    if (tokens > kMostTokens || tokens * width > kMostElements) return hdt_fail(HDT_ERR_SHAPE, "%s: more than 2^30 tokens or 2^35 elements", fn);
+    if (tokens > kMostTokens || tokens * width > kMostElements) return hdt_fail(HDT_ERR_SHAPE, "%s: more than 2^28 tokens or 2^35 elements", fn);
     return HDT_OK;
 }
 

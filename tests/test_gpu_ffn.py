@@ -219,3 +219,26 @@ def test_a_train_step_of_many_rows():
         # three roundings of half a step at most in front of a sum of values of both signs, and the result's own: four of a root mean square of at most 2^-8 / sqrt(3)
         off = float((t.double() - want[name]).norm() / want[name].norm())
         assert off <= 2 ** -8 / 3 ** 0.5 * 4 ** 0.5, (name, off)
+
+
+def test_offsets_beyond_32_bits():
+    """Hidden rows behind 2^32 elements: the last rows against a call on them alone (width 64: sums of one order, so the same bits), gradients against
+    those of the rows that are not zero."""
+    import torch
+    import paper_2407_08330_amd as hdt
+    rows, width, inner, last = 300_000, 64, 16384, 128
+    x, dy, *w = (dev(t, "bf16") for t in problem(last, width, inner, "bf16"))
+    big, dbig = (torch.zeros(rows, width, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    big[-last:], dbig[-last:] = x, dy
+    y, *kept = hdt.hdt_ffn_fwd(big, *w)
+    want, *few = hdt.hdt_ffn_fwd(x, *w)
+    assert all(torch.equal(a[-last:], b) and not bool(a[:-last].any()) for a, b in zip(kept, few))
+    # y and the gradients: sums of up to 16384 (or 128) terms in 32 bits, in pieces that the sizes decide: within a step of bf16 and 2^-24 times their number
+    def near(a, b):
+        off = (a.double() - b.double()).norm() / b.double().norm()
+        return float(off) <= 2 ** -8
+    assert near(y[-last:], want) and not bool(y[:-last].any())
+    got = hdt.hdt_ffn_bwd(dbig, big, *w, *kept)
+    ref = hdt.hdt_ffn_bwd(dy, x, *w, *few)
+    assert near(got[0][-last:], ref[0]) and not bool(got[0][:-last].any())
+    assert all(near(a, b) for a, b in zip(got[1:], ref[1:]))

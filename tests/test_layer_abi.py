@@ -34,7 +34,7 @@ NORM_BWD = dict(dn=16, dh=32, h=48, y=64, stats=80, wp=96, bp=112, gate=128, w=1
 SIZES = [(INVALID, dict(width=-1)), (SHAPE, dict(width=0)), (UNSUPPORTED, dict(dt=2))]
 REFUSED = {
     "hdt_embed_fwd": (EMBED, [*SIZES, (INVALID, dict(tokens=-1)), (INVALID, dict(vocab=-1)), (SHAPE, dict(vocab=0)), (SHAPE, dict(vocab=(1 << 24) + 1)), (SHAPE, dict(width=32769)),
-                              (SHAPE, dict(tokens=(1 << 30) + 1)), (SHAPE, dict(tokens=1 << 30, width=64)), (UNSUPPORTED, dict(table_dt=-1)), (INVALID, dict(scale=NAN)),
+                              (SHAPE, dict(tokens=(1 << 28) + 1)), (SHAPE, dict(tokens=1 << 28, width=136)), (UNSUPPORTED, dict(table_dt=-1)), (INVALID, dict(scale=NAN)),
                               (INVALID, dict(scale=INF)), (INVALID, dict(out=16)), (INVALID, dict(ids=6))]),
     "hdt_embed_bwd": (EMBED_BWD, [*SIZES, (INVALID, dict(tokens=-1)), (SHAPE, dict(vocab=0)), (SHAPE, dict(vocab=1 << 24, width=4096)), (UNSUPPORTED, dict(table_dt=9)),
                                   (INVALID, dict(scale=-INF)), (INVALID, dict(grad=16)), (INVALID, dict(nbytes=100)), (INVALID, dict(workspace=40)), (INVALID, dict(ids=2)),
@@ -76,7 +76,7 @@ def test_nothing_to_do(lib):
 
 def test_workspace_sizes(lib):
     assert lib.hdt_embed_bwd_workspace_bytes(0, 8) == 0 and lib.hdt_embed_bwd_workspace_bytes(5, 0) == 0 and lib.hdt_embed_bwd_workspace_bytes(1 << 31, 8) == 0
-    assert lib.hdt_embed_bwd_workspace_bytes(1 << 30, 32) > (1 << 33)
+    assert lib.hdt_embed_bwd_workspace_bytes(1 << 28, 32) > (1 << 31)
     assert lib.hdt_ffn_bwd_workspace_bytes(0, 8, 8, 0) == 0 and lib.hdt_ffn_bwd_workspace_bytes(5, 8, 8, 7) == 0 and lib.hdt_ffn_bwd_workspace_bytes(5, -8, 8, 0) == 0
     assert lib.hdt_ffn_fwd_workspace_bytes(100, 8, 24, 0, 0) >= 4800 and lib.hdt_ffn_fwd_workspace_bytes(-1, 8, 24, 0, 0) == 0
     assert lib.hdt_ffn_bwd_workspace_bytes(1 << 20, 8, 32768, 0) >= 1 << 37
