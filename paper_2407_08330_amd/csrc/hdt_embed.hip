@@ -71,7 +71,7 @@ constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kMostRows = 5
 // made by frequency, go to different ones).  Its workgroup reads all ids, twice, from the caches: the first time it counts, its waves by
 // themselves and row by row, so that each wave knows where its tokens of a row go, and the second time it puts them there.  Nothing is
 // shared between workgroups.
-// HELD: a wave's STEPS x 64 ids are all it has, and stay in registers in between.
+// HELD: a wave's STEPS x 256 ids are all it has, and stay in registers in between.
 template <typename W, int STEPS, bool HELD>
 __global__ __launch_bounds__(kSortThreads) void k_embed_sort(BwdArgs a)
 {
@@ -82,26 +82,38 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(BwdArgs a)
     for (int i = threadIdx.x; i < kSortWaves * a.rows; i += kSortThreads) count[i] = 0;
     __syncthreads();
 
-    const int steps = (a.tokens + 63) / 64, per = (steps + kSortWaves - 1) / kSortWaves;
+    // a step is 256 tokens, four consecutive ones a lane (one a lane: 131072 tokens 64 us for 59, 30000 of 200 rows 18.3 for 16.3)
+    const int steps = (a.tokens + 255) / 256, per = (steps + kSortWaves - 1) / kSortWaves;
     const int first = min(wave * per, steps), last = min(first + per, steps);
     int *const mine = count + wave * a.rows, *const totals = count + kSortWaves * a.rows;
-    auto id_at = [&](int step) {
-        const int t = step * 64 + lane;
-        return t < a.tokens && step < last ? a.ids[t] : -1;
-    };
-    int id[STEPS];
+    typedef int Four __attribute__((ext_vector_type(4)));
+    typedef Four FourAnywhere __attribute__((aligned(4)));
+    Four id[STEPS];
     auto take = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < STEPS; u++) id[u] = id_at(s + u);
+        for (int u = 0; u < STEPS; u++) {
+            const int t = (s + u) * 256 + lane * 4;
+            id[u] = Four{-1, -1, -1, -1};
+            if (s + u >= last) continue;
+            if (t + 4 <= a.tokens)
+                id[u] = *reinterpret_cast<const FourAnywhere *>(a.ids + t);
+            else
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (t + e < a.tokens) id[u][e] = a.ids[t + e];
+        }
     };
     int below = 0;
     auto count_them = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < STEPS; u++) {
             if (s + u >= last) break;  // (code that is not run is not fetched)
-            const int of = (unsigned)id[u] < (unsigned)a.vocab ? id[u] & mask : mask + 1;
-            if (of < share) below++;
-            if (of == share) atomicAdd(&mine[id[u] >> a.shares_log2], 1);
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const int of = (unsigned)id[u][e] < (unsigned)a.vocab ? id[u][e] & mask : mask + 1;
+                if (of < share) below++;
+                if (of == share) atomicAdd(&mine[id[u][e] >> a.shares_log2], 1);
+            }
         }
     };
     if (HELD) {
@@ -159,15 +171,34 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(BwdArgs a)
 #pragma unroll
         for (int u = 0; u < STEPS; u++) {
             if (s + u >= last) break;
-            const int row = (unsigned)id[u] < (unsigned)a.vocab && (id[u] & mask) == share ? id[u] >> a.shares_log2 : -1;
-            unsigned long long open = __ballot(row >= 0);
-            while (open) {  // the lanes that have the row of the first open one
-                const int r = __builtin_amdgcn_readlane(row, __builtin_ctzll(open));
-                const unsigned long long same = __ballot(row == r);
+            const unsigned long long before_me = (1ull << lane) - 1;
+            int row[4];
+            unsigned long long open[4];
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                row[e] = (unsigned)id[u][e] < (unsigned)a.vocab && (id[u][e] & mask) == share ? id[u][e] >> a.shares_log2 : -1;
+                open[e] = __ballot(row[e] >= 0);
+            }
+            while (open[0] | open[1] | open[2] | open[3]) {  // the tokens that have the row of the first open one
+                const int at_lane = __builtin_ctzll(open[0] | open[1] | open[2] | open[3]);
+                int r = 0;
+#pragma unroll
+                for (int e = 3; e >= 0; e--)
+                    if (open[e] >> at_lane & 1) r = __builtin_amdgcn_readlane(row[e], at_lane);
+                unsigned long long same[4];
                 const int at = mine[r];
-                if (row == r) a.entries[at + __popcll(same & ((1ull << lane) - 1))] = {id[u], (s + u) * 64 + lane};
-                if (lane == 0) mine[r] = at + __popcll(same);
-                open &= ~same;
+                int place = at, all_same = 0;
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    same[e] = __ballot(row[e] == r);
+                    place += __popcll(same[e] & before_me);
+                    all_same += __popcll(same[e]);
+                    open[e] &= ~same[e];
+                }
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (row[e] == r) a.entries[place++] = {id[u][e], (s + u) * 256 + lane * 4 + e};
+                if (lane == 0) mine[r] = at + all_same;
             }
         }
     }
@@ -339,11 +370,11 @@ hdt_status_t launch_bwd(const BwdArgs &a, hipStream_t st)
         const size_t lds = (size_t)(kSortWaves + 1) * a.rows * sizeof(int);
         const dim3 grid(1u << a.shares_log2), threads(kSortThreads);
         if (a.tokens <= 4 * kSortThreads)
-            hipLaunchKernelGGL((k_embed_sort<W, 4, true>), grid, threads, lds, st, a);
+            hipLaunchKernelGGL((k_embed_sort<W, 1, true>), grid, threads, lds, st, a);
         else if (a.tokens <= 32 * kSortThreads)
-            hipLaunchKernelGGL((k_embed_sort<W, 32, true>), grid, threads, lds, st, a);
+            hipLaunchKernelGGL((k_embed_sort<W, 8, true>), grid, threads, lds, st, a);
         else
-            hipLaunchKernelGGL((k_embed_sort<W, 16, false>), grid, threads, lds, st, a);
+            hipLaunchKernelGGL((k_embed_sort<W, 4, false>), grid, threads, lds, st, a);
         HDT_HIP_TRY(hipGetLastError());
     }
     if (blocks == 0) return HDT_OK;

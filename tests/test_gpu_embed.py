@@ -130,6 +130,24 @@ def test_large(tokens, vocab, width):
     assert torch.equal(hdt.hdt_embed_bwd(d, ids, vocab, 2.0, grad=torch.ones(vocab, width, device="cuda"), accumulate=True).double(), want * 2 + 1)
 
 
+@pytest.mark.parametrize("tokens", [255, 257, 4095, 4096, 4097, 32767, 32768, 32769])
+def test_ids_that_begin_anywhere(tokens):
+    """Ids at every 4-byte offset, behind them ones that are not theirs; whole numbers: sums are exact in any order."""
+    import torch
+    import paper_2407_08330_amd as hdt
+    vocab, width = 777, 8
+    rng = np.random.default_rng(tokens)
+    ids = i32(word_ids(rng, tokens, vocab, "any"))
+    d = torch.randint(-3, 4, (tokens, width), device="cuda").float()
+    real = (ids >= 0) & (ids < vocab)
+    want = torch.zeros(vocab, width, device="cuda", dtype=torch.float64).index_add_(0, ids[real].long(), d[real].double())
+    for offset in range(4):
+        room = torch.full((tokens + 8,), 5, dtype=torch.int32, device="cuda")
+        here = room[offset:offset + tokens]
+        here.copy_(ids)
+        assert torch.equal(hdt.hdt_embed_bwd(d, here, vocab).double(), want)
+
+
 def test_offsets_beyond_32_bits():
     """A table and a gradient of more than 2^32 elements."""
     import torch
