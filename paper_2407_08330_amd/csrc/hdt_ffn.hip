@@ -98,7 +98,7 @@ struct Sizes {
     bool tiled() const { return dt == HDT_BF16; }
     // whether rows begin at multiples of 16 bytes, as direct loads need it
     bool even() const { return width % 8 == 0 && inner % 8 == 0; }
-    bool few() const { return tiled() && rows <= kFew; }  // (the forward's products)
+    bool few() const { return tiled() && few_rows(rows, width, inner); }  // (the forward's products)
     Plan plan_gate() const
     {
         const Dims d = {(int)rows, 2 * inner};

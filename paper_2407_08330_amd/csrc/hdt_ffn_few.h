@@ -1,9 +1,10 @@
 // The forward products of the gated feed-forward block for few rows, in bf16: what takes time is reading the weights.
 //
-// A workgroup makes 16 rows of weights' sums with all rows of x, 16 x 16 blocks of them by matrix instructions: eight columns of the gate and the
-// same eight of up, or 16 columns of the last product.  Its waves divide k, 32 at a time, and join in LDS in a fixed order.  Operands go straight
-// from memory to registers: a weight is read once, by one wave.  One row of 768 x 2048: 3.7 and 4.5 us, of which the 9.4 MB of weights are 1.8; 32 rows of
-// 1024 x 2816: 8.3 and 9.8 (17 MB, and every workgroup reads all of x or H from the L2).
+// A workgroup makes 16 rows of weights' sums with 16, 32 or 64 rows of x, 16 x 16 blocks of them by matrix instructions: eight columns of the gate and the
+// same eight of up, or 16 (8) columns of the last product.  Its waves divide k, 64 at a time, and join in LDS in a fixed order.  A load takes 128 bytes of eight
+// rows, which LDS of the wave's own turns into the instructions' operands.  (Loaded as the instructions take them, 16 neighbouring lanes meet 16 lines, and a
+// compute unit gets 16 bytes a clock: 32 rows of 1024 x 2816 17.0 us for 9.2, 64 rows of 768 x 2048 17.3 for 8.7.)  What is left at 32 rows of 1024 x 2816
+// is two launches of about 4 us, mostly latency (17 MB of weights are 3.4).
 #pragma once
 
 #include "hdt_ffn_tile.h"
@@ -11,38 +12,74 @@
 namespace hdt_ffn {
 
 // BLOCKS: of 16 rows of x.  GATE: weights p.b[0], p.b[1]; else p.b[0].
-template <int KIND, int WAVES, int BLOCKS, bool EVEN>
+template <int KIND, int WAVES, int BLOCKS, int COLS, bool EVEN>
 __global__ __launch_bounds__(WAVES * 64) void k_ffn_few(Product p)
 {
-    constexpr int COLS = KIND == GATE ? 8 : 16, AHEAD = BLOCKS <= 2 ? 8 : 4;
-    __shared__ float lds[WAVES][BLOCKS][16][17];  // [..][row of x][sum]
+    constexpr int WEIGHTS = KIND == GATE ? 16 : COLS, ROWS = WEIGHTS + 16 * BLOCKS, LOADS = ROWS / 8, FIRST = WEIGHTS / 8;
+    constexpr int CHUNKS = BLOCKS == 1 ? 4 : BLOCKS == 2 ? 3 : 2;  // of 64 of k in flight: as many as registers take
+    constexpr int kStage = WAVES * ROWS * 128, kJoin = WAVES * BLOCKS * 16 * 17 * 4;
+    __shared__ __attribute__((aligned(16))) char room[kStage > kJoin ? kStage : kJoin];
+    float(*lds)[BLOCKS][16][17] = (float(*)[BLOCKS][16][17])room;  // [wave][..][row of x][sum]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15;
-    const int n0 = blockIdx.x * COLS;
-    const int column = min(n0 + (KIND == GATE ? r & 7 : r), p.n - 1);
-    const __bf16 *w = (const __bf16 *)(KIND == GATE && r >= 8 ? p.b[1] : p.b[0]) + (int64_t)column * p.ldb;
-    const __bf16 *x[BLOCKS];
+    const int n0 = blockIdx.x * COLS, m0 = blockIdx.y * (BLOCKS * 16);
+    // load j: 128 bytes of eight rows, of the weights (j < FIRST) or x
+    const __bf16 *from[LOADS];
+    const int piece = lane & 7;
 #pragma unroll
-    for (int b = 0; b < BLOCKS; b++) x[b] = (const __bf16 *)p.a[0] + (int64_t)min(b * 16 + r, p.m - 1) * p.lda;
-    f32x4 acc[BLOCKS] = {};
-    for (int k0 = wave * 32; k0 < p.k; k0 += WAVES * 32 * AHEAD) {
-        bf16x8 wv[AHEAD], xv[AHEAD][BLOCKS];
-#pragma unroll
-        for (int u = 0; u < AHEAD; u++) {
-            const int k = k0 + u * WAVES * 32 + (lane >> 4) * 8, left = p.k - k;
-            wv[u] = zero_bf16x8();
-#pragma unroll
-            for (int b = 0; b < BLOCKS; b++) xv[u][b] = zero_bf16x8();
-            if (left > 0) {
-                wv[u] = load_chunk<EVEN>(w + k, left);
-#pragma unroll
-                for (int b = 0; b < BLOCKS; b++) xv[u][b] = load_chunk<EVEN>(x[b] + k, left);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < AHEAD; u++)
-#pragma unroll
-            for (int b = 0; b < BLOCKS; b++) acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[u], xv[u][b], acc[b], 0, 0, 0);
+    for (int j = 0; j < LOADS; j++) {
+        const int row = (j < FIRST ? j : j - FIRST) * 8 + (lane >> 3);
+        if (j < FIRST)
+            from[j] = (const __bf16 *)(KIND == GATE && j == 1 ? p.b[1] : p.b[0]) + (int64_t)min(n0 + (KIND == GATE ? row & 7 : row), p.n - 1) * p.ldb;
+        else
+            from[j] = (const __bf16 *)p.a[0] + (int64_t)min(m0 + row, p.m - 1) * p.lda;
+        from[j] += piece * 8;
     }
+    char *const mine = room + wave * (ROWS * 128);
+    // row i's piece q is at q ^ (i / 2 mod 8): 16 lanes that read a piece of 16 rows, or write two rows, meet every bank once
+    char *const put = mine + (lane >> 3) * 128;
+    const int turn = lane >> 4;
+    f32x4 acc[BLOCKS] = {};
+    bf16x8 v[CHUNKS][LOADS];
+    auto load = [&](int u, int k) __attribute__((always_inline)) {
+        const int left = p.k - k - piece * 8;
+#pragma unroll
+        for (int j = 0; j < LOADS; j++) {
+            v[u][j] = zero_bf16x8();
+            if (left > 0) v[u][j] = load_chunk<EVEN>(from[j] + k, left);
+        }
+    };
+    constexpr int STEP = WAVES * 64;
+    constexpr bool ROLLING = BLOCKS <= 2;  // a chunk's registers take the next one as soon as it is in LDS (with four blocks that spills)
+    if (ROLLING)
+#pragma unroll
+        for (int u = 0; u < CHUNKS; u++) load(u, wave * 64 + u * STEP);
+    for (int k0 = wave * 64; k0 < p.k; k0 += STEP * CHUNKS) {
+        if (!ROLLING)
+#pragma unroll
+            for (int u = 0; u < CHUNKS; u++) load(u, k0 + u * STEP);
+#pragma unroll
+        for (int u = 0; u < CHUNKS; u++) {
+            if (k0 + u * STEP >= p.k) break;
+#pragma unroll
+            for (int j = 0; j < LOADS; j++) *(bf16x8 *)(put + j * 1024 + (piece ^ ((j < FIRST ? j : j - FIRST) % 2 * 4 + turn)) * 16) = v[u][j];
+            if (ROLLING && k0 + (u + CHUNKS) * STEP < p.k) load(u, k0 + (u + CHUNKS) * STEP);
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const int q = (lane >> 4) + h * 4, i = r & (WEIGHTS - 1);
+                const bf16x8 w = *(const bf16x8 *)(mine + i * 128 + (q ^ (i >> 1)) * 16);
+                const char *const at = mine + WEIGHTS * 128 + r * 128 + (q ^ (r >> 1)) * 16;
+#pragma unroll
+                for (int b = 0; b < BLOCKS; b++) acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, *(const bf16x8 *)(at + b * 2048), acc[b], 0, 0, 0);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        }
+    }
+    __syncthreads();  // the room is the join's now
     // lane: row of x r, sums (lane / 16) 4 + 0 .. 3
 #pragma unroll
     for (int b = 0; b < BLOCKS; b++)
@@ -51,14 +88,14 @@ __global__ __launch_bounds__(WAVES * 64) void k_ffn_few(Product p)
     __syncthreads();
     for (int i = tid; i < BLOCKS * 16 * COLS; i += WAVES * 64) {
         const int m = i / COLS, c = i % COLS, n = n0 + c;
-        if (m >= p.m || n >= p.n) continue;
+        if (m0 + m >= p.m || n >= p.n) continue;
         float s[2] = {0.f, 0.f};
 #pragma unroll
         for (int v = 0; v < WAVES; v++) {
             s[0] += lds[v][m >> 4][m & 15][c];
             if (KIND == GATE) s[1] += lds[v][m >> 4][m & 15][c + 8];
         }
-        const int64_t at = (int64_t)m * p.ldo + n;
+        const int64_t at = (int64_t)(m0 + m) * p.ldo + n;
         if (KIND == GATE) {
             Act f;
             by_act(p.act, [&](auto act) { f = activate<true, decltype(act)::value>(s[0]); });
@@ -73,20 +110,34 @@ __global__ __launch_bounds__(WAVES * 64) void k_ffn_few(Product p)
     }
 }
 
-// most rows (us with events around each kernel, this way | in tiles: 8 rows of 1024 x 2816 16 | 37, 32 22 | 37, 64 32 | 38; of 768 x 2048 14 | 28, 17 | 28, 22 | 28)
-constexpr int kFew = 64;
+// How many rows are few depends on the weights, which each group of at most 64 rows reads anew (us, forward, this way | in tiles: 1024 x 2816 64 rows 11.5 | 38,
+// 128 15.3 | 31, 192 21 | 34; 768 x 2048 128 11.6 | 20, 192 15.6 | 22; 4096 x 1024 192 30 | 67; 2048 x 4096 128 32 | 45, 192 49 | 48; 2048 x 8192 64 33 | 51,
+// 128 55 | 52; 4096 x 11008 64 89 | 107, 128 146 | 109).
+inline bool few_rows(int64_t rows, int width, int inner)
+{
+    const int64_t weights = (int64_t)width * inner;
+    return rows <= 64 || (rows <= 128 && weights <= 1 << 24) || (rows <= 192 && weights <= 1 << 22);
+}
 
+// Rows a workgroup: 16 where that is not more than a workgroup a compute unit, else 32, else 64 (the last product, 64 rows of 1024 x 2816: 16 rows each, 256
+// workgroups, 4.2 us, 64 each 7.4; but 32 rows of 4096 x 11008: 16 each, 512 workgroups, 32 us, 32 each 23).  Up to 16 rows in the last product,
+// where these are few workgroups: eight columns each (one row of 768 x 2048 6.4 -> 6.2 in all, but of 4096 x 11008 46 -> 49).
 template <int KIND, bool EVEN>
 void launch_few(const Product &p, hipStream_t st)
 {
-    constexpr int WAVES = KIND == GATE ? 8 : 16;
-    const dim3 grid((unsigned)((p.n + (KIND == GATE ? 7 : 15)) / (KIND == GATE ? 8 : 16))), block(WAVES * 64);
-    if (p.m <= 16)
-        hipLaunchKernelGGL((k_ffn_few<KIND, WAVES, 1, EVEN>), grid, block, 0, st, p);
-    else if (p.m <= 32)
-        hipLaunchKernelGGL((k_ffn_few<KIND, WAVES, 2, EVEN>), grid, block, 0, st, p);
+    constexpr int WAVES = KIND == GATE ? 8 : 16, COLS = KIND == GATE ? 8 : 16;
+    const int groups = (p.m + 15) / 16, across = (p.n + COLS - 1) / COLS, most = std::max(256 / across, 1);
+    auto launch = [&](auto kernel, int cols, int blocks) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((p.n + cols - 1) / cols), (unsigned)((groups + blocks - 1) / blocks)), dim3(WAVES * 64), 0, st, p);
+    };
+    if (KIND != GATE && groups == 1 && p.n <= 2048)
+        launch(k_ffn_few<KIND, WAVES, 1, 8, EVEN>, 8, 1);
+    else if (groups <= most)
+        launch(k_ffn_few<KIND, WAVES, 1, COLS, EVEN>, COLS, 1);
+    else if ((groups + 1) / 2 <= most)
+        launch(k_ffn_few<KIND, WAVES, 2, COLS, EVEN>, COLS, 2);
     else
-        hipLaunchKernelGGL((k_ffn_few<KIND, WAVES, 4, EVEN>), grid, block, 0, st, p);
+        launch(k_ffn_few<KIND, WAVES, 4, COLS, EVEN>, COLS, 4);
 }
 
 }  // namespace hdt_ffn

@@ -82,6 +82,13 @@ def test_ffn(rows, width, inner, dtype):
     check_call(rows, width, inner, ACTS[(rows + width + inner) % 3], dtype)
 
 
+# rows on both sides of every number of rows a workgroup, with few columns and with more than a workgroup a compute unit of them; beyond 64, 128 and 192
+@pytest.mark.parametrize("rows,width,inner", [(8, 2064, 72), (15, 2049, 65), (16, 2100, 130), (48, 2056, 264), (49, 1032, 2056), (80, 520, 136), (96, 2056, 136), (100, 100, 2060),
+                                              (128, 264, 520), (129, 136, 1040), (144, 1111, 77), (177, 88, 2200), (192, 70, 200), (193, 72, 200), (40, 4104, 2056), (64, 4160, 72)])
+def test_few_rows(rows, width, inner):
+    check_call(rows, width, inner, "gelu", "bf16")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("rows,width,inner", [(4, 96, 160), (70, 96, 160), (300, 256, 512)])
@@ -130,7 +137,7 @@ def test_shapes_and_no_rows():
         assert y.shape == (0, 16) and grads[0].shape == (0, 16) and all(bool((g == 0).all()) for g in grads[1:])
 
 
-@pytest.mark.parametrize("rows,width,inner", [(20, 64, 72), (300, 256, 264), (300, 60, 100)])
+@pytest.mark.parametrize("rows,width,inner", [(20, 64, 72), (150, 80, 2056), (300, 256, 264), (300, 60, 100)])
 def test_rows_do_not_meet(rows, width, inner):
     """A row's y and dx depend on that row alone: NaN and infinities in others change nothing, whatever tile they share."""
     import torch
