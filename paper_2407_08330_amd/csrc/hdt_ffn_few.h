@@ -1,10 +1,10 @@
-// The forward products of the gated feed-forward block for few rows, in bf16: what takes time is reading the weights.
+// The forward products of the gated feed-forward block for few rows, in bf16: reading the weights is what cannot be saved.
 //
 // A workgroup makes 16 rows of weights' sums with 16, 32 or 64 rows of x, 16 x 16 blocks of them by matrix instructions: eight columns of the gate and the
 // same eight of up, or 16 (8) columns of the last product.  Its waves divide k, 64 at a time, and join in LDS in a fixed order.  A load takes 128 bytes of eight
 // rows, which LDS of the wave's own turns into the instructions' operands.  (Loaded as the instructions take them, 16 neighbouring lanes meet 16 lines, and a
-// compute unit gets 16 bytes a clock: 32 rows of 1024 x 2816 17.0 us for 9.2, 64 rows of 768 x 2048 17.3 for 8.7.)  What is left at 32 rows of 1024 x 2816
-// is two launches of about 4 us, mostly latency (17 MB of weights are 3.4).
+// compute unit gets 16 bytes a clock: 32 rows of 1024 x 2816 17.0 us for 9.2, 64 rows of 768 x 2048 17.3 for 8.7.)  Kernels: 32 rows of 1024 x 2816 5.6 and 4.7 us
+// (17 MB of weights are 3.4), one row of 768 x 2048 3.4 and 3.7 (9.4 MB, 1.8): a load's latency, a join in LDS.
 #pragma once
 
 #include "hdt_ffn_tile.h"
