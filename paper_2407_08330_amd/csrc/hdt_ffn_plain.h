@@ -35,22 +35,37 @@ __global__ __launch_bounds__(64 * W * W * GROUPS) void k_ffn_plain(PlainArgs a)
 #pragma unroll
         for (int e = 0; e < 16; e++) acc[b][e] = 0.f;
 
+    // four values a load, of k or, of operands whose k is slow, of rows (one a load, each with its bounds: 512 x 384 x 1000, forward and backward, 159 us for 126,
+    // 98 x 1024 x 3248 318 for 215, 2048 x 768 x 2048 943 for 789)
+    typedef float Four __attribute__((ext_vector_type(4)));
+    typedef Four FourAnywhere __attribute__((aligned(4)));
+    constexpr int LOADS = EACH / 4, KS = kPlainK / 4, RS = SIDE / 4;
     struct Part {
-        float v[EACH];
+        Four v[LOADS];
     };
-    auto row_of = [&](bool slow, int i) { return slow ? tid % SIDE : tid / kPlainK + THREADS / kPlainK * i; };
-    auto k_of = [&](bool slow, int i) { return slow ? tid / SIDE + THREADS / SIDE * i : tid % kPlainK; };
+    auto row_of = [&](bool slow, int i) { return slow ? tid % RS * 4 : tid / KS + THREADS / KS * i; };
+    auto k_of = [&](bool slow, int i) { return slow ? tid / RS + THREADS / RS * i : tid % KS * 4; };
     auto take = [&](Part &to, const float *from, int64_t ld, bool slow, int r0, int rows, int k0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < EACH; i++) {
+        for (int i = 0; i < LOADS; i++) {
             const int r = r0 + row_of(slow, i), k = k0 + k_of(slow, i);
-            to.v[i] = 0.f;
-            if (r < rows && k < p.k) to.v[i] = slow ? from[(int64_t)k * ld + r] : from[(int64_t)r * ld + k];
+            const int left = slow ? (k < p.k ? rows - r : 0) : p.k - k;
+            const float *const at = slow ? from + (int64_t)k * ld + r : from + (int64_t)min(r, rows - 1) * ld + k;  // (copies of the last row are not stored)
+            to.v[i] = Four{0.f, 0.f, 0.f, 0.f};
+            if (left >= 4)
+                to.v[i] = *reinterpret_cast<const FourAnywhere *>(at);
+            else if (left > 0) {
+                to.v[i][0] = at[0];
+                if (left > 1) to.v[i][1] = at[1];
+                if (left > 2) to.v[i][2] = at[2];
+            }
         }
     };
     auto put = [&](float *to, const Part &from, bool slow) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < EACH; i++) to[row_of(slow, i) * LD + k_of(slow, i)] = from.v[i];
+        for (int i = 0; i < LOADS; i++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) to[(row_of(slow, i) + (slow ? e : 0)) * LD + k_of(slow, i) + (slow ? 0 : e)] = from.v[i][e];
     };
     const int per_range = (p.k + kPlainK - 1) / kPlainK, steps = p.ranges * per_range, rounds = (steps + GROUPS - 1) / GROUPS;
     Part va, vb[NB];
@@ -142,7 +157,8 @@ hdt_status_t launch_plain_as(const Product *of, int products, hipStream_t st)
 }
 
 // Tiles of 64 x 64; where those do not fill the chip four groups of a workgroup divide k, and where they do not give each compute unit one,
-// tiles of 32 x 32, eight of whose waves divide k (fp32, 512 x 384 x 1000, forward and backward, us: one group 752, four 205, all three 160)
+// tiles of 32 x 32, eight of whose waves divide k (fp32, 512 x 384 x 1000, forward and backward, us, when a load was one value: one group 752, four 205,
+// all three 160)
 template <int KIND, bool A_SLOW, bool B_SLOW>
 hdt_status_t launch_plain(const Product *of, int products, hipStream_t st)
 {
