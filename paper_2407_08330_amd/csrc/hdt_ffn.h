@@ -25,14 +25,16 @@ enum { GATE, STORE, DGATE };
 struct Act {
     float value, slope;
 };
-// 1 / (1 + exp(-x)) and what it lacks to 1, neither by a difference.  (The exponent is bounded: an infinite exponential times zero.)
+// 1 / (1 + exp(-x)) and what it lacks to 1, neither by a difference.  Below x = -88 the exponential is infinite and the value 0, whatever g it is multiplied with
+// (held at 2^126 instead, it gave -1e36 2^-126 = -0.012 there).  What it lacks is then 0 too, not 1: it is met only as value rest.  An infinite g
+// gives what its formula gives, NaN where it meets a 0.
 struct Sigmoid {
     float value, rest;
 };
 __device__ __forceinline__ Sigmoid sigmoid(float x)
 {
-    const float t = fast_exp2(fminf(-1.4426950408889634f * x, 126.f)), s = __builtin_amdgcn_rcpf(1.f + t);
-    return {s, t * s};
+    const float t = fast_exp2(-1.4426950408889634f * x), s = __builtin_amdgcn_rcpf(1.f + t);
+    return {s, fminf(t, 3.4028235e38f) * s};
 }
 template <bool SLOPE, int ACT>
 __device__ __forceinline__ Act activate(float g)

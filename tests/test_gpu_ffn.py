@@ -119,6 +119,33 @@ def test_activations_over_their_whole_range(act, dtype):
         assert np.all(np.abs(got[big] - far) <= 2 * u * np.abs(far) + 1e-6), name
 
 
+@pytest.mark.parametrize("rows", [1, 300])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ACTS)
+def test_activations_up_to_the_types_largest_values(act, dtype, rows):
+    """G is set one by one, as above, up to the largest values of the type, in one row (few rows) and in 300 (tiles).  Out there the activation is g or 0 and
+    its slope 1 or 0: the value itself, rounded once, behind factors of 1 that are off by a few 2^-24.  Below -88 the sigmoid is 2^-126 at most (its
+    exponential may overflow, or its value be flushed to 0), and 0 below -89: with g, under 89 2^-126."""
+    import torch
+    import paper_2407_08330_amd as hdt
+    most = {"bf16": 2.0 ** 127 * (2 - 2.0 ** -7), "f32": 2.0 ** 127 * (2 - 2.0 ** -23)}[dtype]
+    sizes = [88.0, 89.0, 90.0, 100.0, 104.0, 128.0, 200.0, 1e3, 1e10, 1e20, 1e30, 1e33, 1e36, 1e37, 1e38, 3e38, most]
+    points = np.array([s * v for v in sizes for s in (1, -1)])
+    wg = host(dev(points[:, None], dtype)) if dtype == "f32" else values_of(points[:, None])
+    assert abs(wg[-1, 0]) == most
+    n, u = len(wg), half_step(dtype)
+    t = [dev(v, dtype) for v in (np.ones((rows, 1)), wg, np.ones((n, 1)), np.ones((1, n)))]
+    kept = hdt.hdt_ffn_fwd(*t, act)[1:]
+    g = wg[:, 0]
+    for name, k in zip(("by_gate", "by_up", "hidden"), kept):
+        want = (g > 0).astype(float) if name == "by_gate" else np.maximum(g, 0)
+        assert np.all(np.abs(host(k) - want) <= (u + 4 * lr.F32) * np.abs(want) + 89 * 2.0 ** -126), (name, g[np.argmax(np.abs(host(k) - want).max(0))])
+    # a NaN stays one
+    wg[:] = np.nan
+    t[1] = dev(wg, dtype)
+    assert all(bool(k.isnan().all()) for k in hdt.hdt_ffn_fwd(*t, act)[1:])
+
+
 def test_shapes_and_no_rows():
     import torch
     import paper_2407_08330_amd as hdt
