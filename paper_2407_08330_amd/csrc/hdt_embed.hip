@@ -59,7 +59,7 @@ struct BwdArgs {
     const void *d_out;
     void *grad;
     Entry *entries;   // [tokens], ordered by (id mod shares, id, token); the rest of them is not written
-    int32_t *n_real;  // how many there are
+    int32_t *n_real;  // how many there are; NULL without tokens
     float *parts;     // [blocks][2][width]: of a block's first row where that began before it, of its last where that goes on behind it
     int tokens, vocab, width, shares_log2, rows, accumulate, block;  // rows: of a share; block: entries that a wave adds up
     float scale;
@@ -439,9 +439,11 @@ HDT_EXPORT hdt_status_t hdt_embed_bwd(const void *d_out, const int32_t *d_ids, i
     }
     BwdArgs a = {};
     a.d_out = d_out, a.ids = d_ids, a.grad = grad;
-    a.n_real = (int32_t *)workspace;
-    a.entries = (Entry *)((char *)workspace + 16);
-    a.parts = (float *)((char *)workspace + 16 + entries_bytes(tokens));
+    if (tokens > 0) {  // (without tokens no workspace is needed: one that is given may be of no bytes)
+        a.n_real = (int32_t *)workspace;
+        a.entries = (Entry *)((char *)workspace + 16);
+        a.parts = (float *)((char *)workspace + 16 + entries_bytes(tokens));
+    }
     a.tokens = (int)tokens, a.vocab = vocab, a.width = width, a.accumulate = accumulate != 0, a.block = block_of(tokens), a.scale = scale;
     a.shares_log2 = shares_log2(vocab);
     a.rows = (int)(((int64_t)vocab + (1 << a.shares_log2) - 1) >> a.shares_log2);

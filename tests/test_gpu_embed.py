@@ -103,6 +103,25 @@ def test_shapes_no_tokens_and_rows_without_one():
     assert bool(hdt.hdt_embed_bwd(torch.empty(0, 12, device="cuda"), none, 50, grad=nan, accumulate=True).isnan().all())
 
 
+@pytest.mark.parametrize("offset", [0, 1, 16])
+def test_no_tokens_and_a_workspace_of_no_bytes(offset):
+    """Without tokens no workspace is needed: memory behind the address of one of no bytes, aligned or not, is not the call's."""
+    import torch
+    import paper_2407_08330_amd as hdt
+    lib = hdt.load_library()
+    assert lib.hdt_embed_bwd_workspace_bytes(0, 12) == 0
+    for dtype, code in ((torch.bfloat16, 0), (torch.float32, 1)):
+        room = torch.full((4096,), 0x5A, dtype=torch.uint8, device="cuda")
+        grad = torch.full((50, 12), float("nan"), dtype=dtype, device="cuda")
+        st = torch.cuda.current_stream().cuda_stream
+        assert lib.hdt_embed_bwd(None, None, 0, 50, 12, 1.0, 0, grad.data_ptr(), code, code, room.data_ptr() + offset, 0, st) == 0
+        assert bool((grad == 0).all()) and bool((room == 0x5A).all())
+        none = torch.empty(0, dtype=torch.int32, device="cuda")
+        grad.fill_(float("nan"))
+        hdt.hdt_embed_bwd(torch.empty(0, 12, dtype=dtype, device="cuda"), none, 50, grad=grad, workspace=room[offset:offset + 3])
+        assert bool((grad == 0).all()) and bool((room == 0x5A).all())
+
+
 def test_non_finite_values_stay_in_their_rows():
     import torch
     import paper_2407_08330_amd as hdt
