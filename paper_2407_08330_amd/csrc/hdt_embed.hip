@@ -198,7 +198,9 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(BwdArgs a)
 #pragma unroll
                 for (int e = 0; e < 4; e++)
                     if (row[e] == r) a.entries[place++] = {id[u][e], (s + u) * 256 + lane * 4 + e};
+                hdt_lanes::wave_lds_barrier();  // (all lanes have read the row's place; lane 0 moves it on for the next row and step)
                 if (lane == 0) mine[r] = at + all_same;
+                hdt_lanes::wave_lds_barrier();
             }
         }
     }

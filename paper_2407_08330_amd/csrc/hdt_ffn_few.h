@@ -63,9 +63,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_ffn_few(Product p)
 #pragma unroll
             for (int j = 0; j < LOADS; j++) *(bf16x8 *)(put + j * 1024 + (piece ^ ((j < FIRST ? j : j - FIRST) % 2 * 4 + turn)) * 16) = v[u][j];
             if (ROLLING && k0 + (u + CHUNKS) * STEP < p.k) load(u, k0 + (u + CHUNKS) * STEP);
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            hdt_lanes::wave_lds_barrier();
 #pragma unroll
             for (int h = 0; h < 2; h++) {
                 const int q = (lane >> 4) + h * 4, i = r & (WEIGHTS - 1);
@@ -74,9 +72,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_ffn_few(Product p)
 #pragma unroll
                 for (int b = 0; b < BLOCKS; b++) acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, *(const bf16x8 *)(at + b * 2048), acc[b], 0, 0, 0);
             }
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            hdt_lanes::wave_lds_barrier();
         }
     }
     __syncthreads();  // the room is the join's now

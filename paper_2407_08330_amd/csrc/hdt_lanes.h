@@ -38,6 +38,15 @@ __device__ __forceinline__ float sum_halves(float x)
     return h.lower + h.upper;
 }
 
+// What a wave's lanes have in LDS before this, its other lanes find there after it.  Their instructions are executed in order in any case; this keeps
+// the compiler, which sees one lane's program, from moving one lane's reads over another's writes.
+__device__ __forceinline__ void wave_lds_barrier()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // the sum over a wave, in every lane
 __device__ __forceinline__ float wave_sum(float x)
 {

@@ -149,6 +149,24 @@ def test_large(tokens, vocab, width):
     assert torch.equal(hdt.hdt_embed_bwd(d, ids, vocab, 2.0, grad=torch.ones(vocab, width, device="cuda"), accumulate=True).double(), want * 2 + 1)
 
 
+@pytest.mark.parametrize("tokens", [4000, 32700, 70001])
+def test_many_rows_of_one_share(tokens):
+    """All ids are congruent modulo 256: a workgroup of the sort has them all, up to 512 rows, and each wave places up to 256 of them a step, one behind the
+    other, whose places the steps before have moved on.  Whole numbers: sums are exact in any order; rows that come once show every single token."""
+    import torch
+    import paper_2407_08330_amd as hdt
+    vocab, width = 131072, 8
+    rng = np.random.default_rng(tokens)
+    for rows in (2, 100, 512):
+        ids = i32(rng.integers(0, rows, tokens) * 256 + 7)
+        d = torch.randint(-3, 4, (tokens, width), device="cuda").float()
+        want = torch.zeros(vocab, width, device="cuda", dtype=torch.float64).index_add_(0, ids.long(), d.double())
+        assert torch.equal(hdt.hdt_embed_bwd(d, ids, vocab).double(), want), rows
+    ids = i32(rng.permutation(512) * 256 + 255)
+    d = torch.randn(512, width, device="cuda")
+    assert torch.equal(hdt.hdt_embed_bwd(d, ids, vocab)[ids.long()], d)
+
+
 @pytest.mark.parametrize("tokens", [255, 257, 4095, 4096, 4097, 32767, 32768, 32769])
 def test_ids_that_begin_anywhere(tokens):
     """Ids at every 4-byte offset, behind them ones that are not theirs; whole numbers: sums are exact in any order."""
