@@ -4,6 +4,7 @@
 #include "hdt_ffn.h"
 #include "hdt_ffn_few.h"
 #include "hdt_ffn_plain.h"
+#include "hdt_ffn_plan.h"
 #include "hdt_ffn_tile.h"
 
 namespace {
@@ -14,7 +15,6 @@ constexpr int kMostSize = 65536;
 constexpr int64_t kMostElements = 1ll << 35;
 
 bool misaligned(const void *p) { return ((uintptr_t)p & 15u) != 0; }
-size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 hdt_status_t check_sizes(const char *fn, int64_t rows, int32_t width, int32_t inner, hdt_act_t act, hdt_dtype_t dt)
 {
@@ -26,107 +26,6 @@ hdt_status_t check_sizes(const char *fn, int64_t rows, int32_t width, int32_t in
     if (rows > (1 << 28) || rows * std::max(width, inner) > kMostElements) return hdt_fail(HDT_ERR_SHAPE, "%s: more than 2^28 rows or 2^35 elements", fn);
     return HDT_OK;
 }
-
-using Large = Shape<2, 4, 4, 2, 32, 4>;  // 256 x 256, a workgroup a compute unit
-using Small = Shape<2, 2, 2, 2, 64, 2>;  // 128 x 128, two
-
-// Products that one launch makes in tiles, and how (TileArgs has the meanings).
-struct Plan {
-    int shape;  // 0 Large, 1 Small
-    unsigned direct, tiles, piece_items, sharers;
-    int pieces, per, rest;
-    size_t parts_bytes;
-};
-struct Dims {
-    int m, n;  // n: columns of the tile's operand (of both weights, for GATE)
-};
-int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
-
-// The rule is a sum of clocks: a walk along k, what stands around it, and the parts of tiles that are cut.  slots: workgroups the chip holds; step,
-// around: clocks of 64 of k with every unit full, and of what stands around a tile's walk.  As measured (us of forward and backward, kernels, Large |
-// Small): 32768 x 768 x 2048 1184 | 1413, 8192 x 1024 x 4096 741 | 799, 1999 x 1000 x 2504 240 | 200, 512 x 768 x 2048 137 | 101.  A unit with one
-// Small workgroup is no quicker a step than with two.
-template <typename S>
-void consider(const Dims *of, int products, int k, int ranges, bool divisible, int shape, unsigned slots, double step, double around, Plan *best, double *best_cost)
-{
-    int64_t tiles = 0;
-    for (int i = 0; i < products; i++) tiles += (int64_t)ceil_div(of[i].m, S::BM) * ceil_div(of[i].n, S::BN);
-    const int k_tiles = ranges * ceil_div(k, S::BK);
-    step *= S::BK / 64.;
-    auto offer = [&](const Plan &plan, double cost) {
-        if (*best_cost >= 0 && cost >= *best_cost) return;
-        *best_cost = cost;
-        *best = plan;
-    };
-    const double rounds = (double)((tiles + slots - 1) / slots);
-    offer({shape, (unsigned)tiles, (unsigned)tiles, 0, 0, 0, 0, 0, 0}, rounds * (k_tiles * step + around));
-    const int64_t direct = tiles / slots * slots, cut = tiles - direct;
-    if (!divisible || cut == 0 || k_tiles == 0) return;
-    const int least = std::min(256 / S::BK, k_tiles);  // (shorter walks are their beginning and end)
-    const double before = (double)(direct / slots) * (k_tiles * step + around);
-    auto cut_into = [&](int pieces, int per, int rest) {
-        const int64_t sharing = rest ? ceil_div(cut * rest, per) : 0, items = cut * pieces + sharing;
-        const unsigned piece_items = (unsigned)(cut * pieces + 7) / 8 * 8, sharers = (unsigned)(sharing + 7) / 8 * 8;
-        // parts are written and read at about 3000 bytes a clock; and a launch
-        const size_t parts = (size_t)(cut * pieces + (rest ? sharers + cut : 0)) * S::BM * S::BN * sizeof(float);
-        const double tiles_of_one = rest ? per / (double)rest + 1 : 1;
-        offer({shape, (unsigned)direct, (unsigned)tiles, piece_items, sharers, pieces, per, rest, parts},
-              before + (double)ceil_div(items, slots) * (per * step + tiles_of_one * around) + parts * 2. / 3000 + 8000);
-    };
-    // the chip's share each, the rest divided anew; or equal pieces, the last a little shorter
-    const int share = std::max(ceil_div(cut * k_tiles, slots), least), pieces = k_tiles / share, rest = k_tiles - pieces * share;
-    if (rest) cut_into(pieces, share, rest);
-    for (int n = 2; n <= 32; n++) {
-        const int per = ceil_div(k_tiles, n);
-        if (per >= least && ceil_div(k_tiles, per) == n) cut_into(n, per, 0);
-    }
-}
-Plan plan_of(const Dims *of, int products, int k, int ranges, bool divisible)
-{
-    Plan best = {};
-    double cost = -1;
-    consider<Large>(of, products, k, ranges, divisible, 0, 256, 4000, 9000, &best, &cost);
-    consider<Small>(of, products, k, ranges, divisible, 1, 512, 2800, 7000, &best, &cost);
-    return best;
-}
-
-struct Sizes {
-    int64_t rows;
-    int width, inner;
-    hdt_dtype_t dt;
-    size_t hidden_bytes() const { return padded((size_t)rows * inner * (dt == HDT_BF16 ? 2 : 4)); }
-    bool tiled() const { return dt == HDT_BF16; }
-    // whether rows begin at multiples of 16 bytes, as direct loads need it
-    bool even() const { return width % 8 == 0 && inner % 8 == 0; }
-    bool few() const { return tiled() && few_rows(rows, width, inner); }  // (the forward's products)
-    Plan plan_gate() const
-    {
-        const Dims d = {(int)rows, 2 * inner};
-        return plan_of(&d, 1, width, 1, false);
-    }
-    Plan plan_down() const
-    {
-        const Dims d = {(int)rows, width};
-        return plan_of(&d, 1, inner, 1, true);
-    }
-    Plan plan_dgate() const
-    {
-        const Dims d = {(int)rows, inner};
-        return plan_of(&d, 1, width, 1, false);
-    }
-    Plan plan_dx() const
-    {
-        const Dims d = {(int)rows, width};
-        return plan_of(&d, 1, inner, 2, true);
-    }
-    Plan plan_weights() const
-    {
-        const Dims d[] = {{inner, width}, {inner, width}, {width, inner}};
-        return plan_of(d, 3, (int)rows, 1, true);
-    }
-    size_t fwd_bytes(bool train) const { return (train ? 0 : hidden_bytes()) + (tiled() && !few() ? plan_down().parts_bytes : 0); }
-    size_t bwd_bytes() const { return 2 * hidden_bytes() + (tiled() ? std::max(plan_dx().parts_bytes, plan_weights().parts_bytes) : 0); }
-};
 
 template <int KIND, typename S, bool A_SLOW, bool B_SLOW, bool EVEN>
 hdt_status_t launch_tiles(const char *name, const Product *of, int products, const Plan &plan, void *parts, hipStream_t st)

@@ -106,15 +106,6 @@ __global__ __launch_bounds__(WAVES * 64) void k_ffn_few(Product p)
     }
 }
 
-// How many rows are few depends on the weights, which each group of at most 64 rows reads anew (us, forward, this way | in tiles: 1024 x 2816 64 rows 11.5 | 38,
-// 128 15.3 | 31, 192 21 | 34; 768 x 2048 128 11.6 | 20, 192 15.6 | 22; 4096 x 1024 192 30 | 67; 2048 x 4096 128 32 | 45, 192 49 | 48; 2048 x 8192 64 33 | 51,
-// 128 55 | 52; 4096 x 11008 64 89 | 107, 128 146 | 109).
-inline bool few_rows(int64_t rows, int width, int inner)
-{
-    const int64_t weights = (int64_t)width * inner;
-    return rows <= 64 || (rows <= 128 && weights <= 1 << 24) || (rows <= 192 && weights <= 1 << 22);
-}
-
 // Rows a workgroup: 16 where that is not more than a workgroup a compute unit, else 32, else 64 (the last product, 64 rows of 1024 x 2816: 16 rows each, 256
 // workgroups, 4.2 us, 64 each 7.4; but 32 rows of 4096 x 11008: 16 each, 512 workgroups, 32 us, 32 each 23).  Up to 16 rows in the last product,
 // where these are few workgroups: eight columns each (one row of 768 x 2048 6.4 -> 6.2 in all, but of 4096 x 11008 46 -> 49).

@@ -2,6 +2,7 @@
 #pragma once
 
 #include "hdt_ffn.h"
+#include "hdt_ffn_plan.h"
 
 namespace hdt_ffn {
 
@@ -156,17 +157,16 @@ hdt_status_t launch_plain_as(const Product *of, int products, hipStream_t st)
     return HDT_OK;
 }
 
-// Tiles of 64 x 64; where those do not fill the chip four groups of a workgroup divide k, and where they do not give each compute unit one,
-// tiles of 32 x 32, eight of whose waves divide k (fp32, 512 x 384 x 1000, forward and backward, us, when a load was one value: one group 752, four 205,
-// all three 160)
 template <int KIND, bool A_SLOW, bool B_SLOW>
 hdt_status_t launch_plain(const Product *of, int products, hipStream_t st)
 {
     int64_t tiles = 0;
-    for (int i = 0; i < products; i++) tiles += ((int64_t)of[i].m + 63) / 64 * (((int64_t)of[i].n + 63) / 64);
-    if (tiles <= 256) return launch_plain_as<KIND, A_SLOW, B_SLOW, 1, 8>(of, products, st);
-    if (tiles <= 512) return launch_plain_as<KIND, A_SLOW, B_SLOW, 2, 4>(of, products, st);
-    return launch_plain_as<KIND, A_SLOW, B_SLOW, 2, 1>(of, products, st);
+    for (int i = 0; i < products; i++) tiles += plain_tiles({of[i].m, of[i].n});
+    switch (plain_form(tiles)) {
+    case PlainForm::kSmallDivided: return launch_plain_as<KIND, A_SLOW, B_SLOW, 1, 8>(of, products, st);
+    case PlainForm::kDivided: return launch_plain_as<KIND, A_SLOW, B_SLOW, 2, 4>(of, products, st);
+    default: return launch_plain_as<KIND, A_SLOW, B_SLOW, 2, 1>(of, products, st);
+    }
 }
 
 }  // namespace hdt_ffn

@@ -24,6 +24,7 @@
 #pragma once
 
 #include "hdt_ffn.h"
+#include "hdt_ffn_plan.h"
 #include "hdt_rows.h"
 #include "hdt_tile.h"
 
@@ -111,14 +112,6 @@ __device__ __forceinline__ TilePlace place_of(const TileArgs &a, unsigned tile)
     return at;
 }
 
-template <int WM_, int WN_, int MB_, int NB_, int BK_, int STAGES_>
-struct Shape {
-    static constexpr int WM = WM_, WN = WN_, MB = MB_, NB = NB_, NW = WM * WN, THREADS = NW * 64;
-    static constexpr int BM = WM * MB * 32, BN = WN * NB * 32, BK = BK_, STEPS = BK / 16, STAGES = STAGES_;
-    static constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE = A_BYTES + B_BYTES, LDS = STAGES * STAGE;
-    static constexpr int LOADS = (BM + BN) * BK / 8 / 64 / NW;  // direct loads of a stage, for each wave
-};
-
 // One operand of R rows: how it comes to LDS, and how its blocks of 32 rows are read.  PERMUTED: in the order of the sums' rows.
 template <int R, int NW, int BK, bool SLOW, bool PERMUTED, bool EVEN>
 struct Operand {
@@ -204,8 +197,8 @@ __device__ __forceinline__ int result_at(int r, int c)
     return (r * CH + (CH % 16 == 0 ? c ^ (r & 15) : CH == 8 ? c ^ hdt_tile::swz<8>(r) : c ^ ((r >> 1) & 7))) * 16;
 }
 
-// tiles of k t0 .. t1 - 1 of a tile; part: where sums go that are not all of it
-template <int KIND, typename S, bool A_SLOW, bool B_SLOW, bool EVEN>
+// tiles of k t0 .. t1 - 1 of a tile.  PART: not all of it, and its sums go to `part`
+template <int KIND, typename S, bool A_SLOW, bool B_SLOW, bool EVEN, bool PART>
 __device__ __forceinline__ void make_tile(const TileArgs &a, char *smem, unsigned tile, int t0, int t1, float *part)
 {
     constexpr int MB = S::MB, NB = S::NB, NW = S::NW, BK = S::BK;
@@ -361,7 +354,7 @@ __device__ __forceinline__ void make_tile(const TileArgs &a, char *smem, unsigne
 
     // a lane's sums: row m of its block, columns of eight
     const int hf = lane >> 5;
-    if (KIND == STORE && part) {
+    if constexpr (PART) {
 #pragma unroll
         for (int i = 0; i < MB; i++)
 #pragma unroll
@@ -484,26 +477,29 @@ __global__ __launch_bounds__(S::THREADS, 2) void k_ffn_tile(TileArgs a)
     const int k_tiles = a.ranges * ((a.k + S::BK - 1) / S::BK);
     if (KIND != STORE || blockIdx.x < a.spread) {
         const unsigned tile = hdt_tile::logical_block(blockIdx.x, a.chunk);
-        if (tile < a.direct) make_tile<KIND, S, A_SLOW, B_SLOW, EVEN>(a, smem, tile, 0, k_tiles, nullptr);
+        if (tile < a.direct) make_tile<KIND, S, A_SLOW, B_SLOW, EVEN, false>(a, smem, tile, 0, k_tiles, nullptr);
         return;
     }
-    const unsigned cut = a.tiles - a.direct, block = blockIdx.x - a.spread;
-    constexpr size_t SIZE = (size_t)S::BM * S::BN;
-    if (block < a.piece_items) {
-        const unsigned item = by_xcd(block, a.piece_items), piece = item / cut, tile = item - piece * cut;
-        if (piece < (unsigned)a.pieces) make_tile<KIND, S, A_SLOW, B_SLOW, EVEN>(a, smem, a.direct + tile, piece * a.per, min((int)(piece + 1) * a.per, k_tiles), a.parts + item * SIZE);
-        return;
-    }
-    const unsigned me = by_xcd(block - a.piece_items, a.sharers);
-    int64_t at = (int64_t)me * a.per;
-    const int64_t end = min(at + a.per, (int64_t)cut * a.rest);
-    while (at < end) {
-        const int64_t tile = at / a.rest;
-        const int t0 = (int)(at - tile * a.rest), t1 = (int)min((int64_t)a.rest, t0 + (end - at)), from = a.pieces * a.per;
-        wg_barrier();  // (the LDS of the tile before is no longer read)
-        make_tile<KIND, S, A_SLOW, B_SLOW, EVEN>(a, smem, a.direct + (unsigned)tile, from + t0, from + t1,
-                                           t1 - t0 == k_tiles ? nullptr : a.parts + ((size_t)a.pieces * cut + me + tile) * SIZE);
-        at += t1 - t0;
+    if constexpr (KIND == STORE) {
+        const unsigned cut = a.tiles - a.direct, block = blockIdx.x - a.spread;
+        constexpr size_t SIZE = (size_t)S::BM * S::BN;
+        if (block < a.piece_items) {
+            const unsigned item = by_xcd(block, a.piece_items), piece = item / cut, tile = item - piece * cut;
+            if (piece < (unsigned)a.pieces)
+                make_tile<KIND, S, A_SLOW, B_SLOW, EVEN, true>(a, smem, a.direct + tile, piece * a.per, min((int)(piece + 1) * a.per, k_tiles), a.parts + item * SIZE);
+            return;
+        }
+        const unsigned me = by_xcd(block - a.piece_items, a.sharers);
+        int64_t at = (int64_t)me * a.per;
+        const int64_t end = min(at + a.per, (int64_t)cut * a.rest);
+        while (at < end) {
+            const int64_t tile = at / a.rest;
+            const int t0 = (int)(at - tile * a.rest), t1 = (int)min((int64_t)a.rest, t0 + (end - at)), from = a.pieces * a.per;
+            wg_barrier();  // (the LDS of the tile before is no longer read)
+            make_tile<KIND, S, A_SLOW, B_SLOW, EVEN, true>(a, smem, a.direct + (unsigned)tile, from + t0, from + t1,
+                                                           a.parts + ((size_t)a.pieces * cut + me + tile) * SIZE);
+            at += t1 - t0;
+        }
     }
 }
 
@@ -517,8 +513,7 @@ __global__ __launch_bounds__(S::THREADS) void k_ffn_join(TileArgs a)
     const unsigned tile = blockIdx.x / (MB * NB), cut = a.tiles - a.direct;
     const int i = blockIdx.x / NB % MB, j = blockIdx.x % NB;
     const int64_t first = (int64_t)tile * a.rest / a.per, last = a.rest ? ((int64_t)(tile + 1) * a.rest - 1) / a.per : first - 1;
-    const int parts = a.pieces + (int)(last - first + 1);
-    if (parts == 1) return;  // (one workgroup had all of it)
+    const int parts = a.pieces + (int)(last - first + 1);  // two or more
     const TilePlace at = place_of<S, true>(a, a.direct + tile);
     const TileProduct &p = a.p[at.which];
     const int m = at.m + wave / S::WN * MB * 32 + i * 32 + (lane & 31), n0 = at.n * S::BN + wave % S::WN * NB * 32;
