@@ -476,7 +476,7 @@ hdt_status_t hdt_add_norm_bwd(const void *dn, const void *dh, const void *h, con
  *
  *   d_ids     device, int32 [tokens]
  *   table     device, [vocab][width] of table_dt; grad alike.  out, d_out: device, [tokens][width] of dt.  Dense, 16-byte aligned (ids: 4).
- *   workspace device, hdt_embed_bwd_workspace_bytes bytes, 16-byte aligned, scratch only
+ *   workspace device, hdt_embed_bwd_workspace_bytes bytes, 16-byte aligned, scratch only (0, without tokens: none needed)
  * width 1 .. 32768, vocab 1 .. 2^24, at most 2^28 tokens and 2^35 elements.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED (dtype), HDT_ERR_HIP.
  */
 hdt_status_t hdt_embed_fwd(const int32_t *d_ids, int64_t tokens, const void *table, int32_t vocab, int32_t width, float scale, void *out,
@@ -497,6 +497,7 @@ hdt_status_t hdt_embed_bwd(const void *d_out, const int32_t *d_ids, int64_t toke
  * aligned, scratch only (0: none needed).
  * width, inner 1 .. 65536, at most 2^28 rows and 2^35 elements a tensor.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED (dtype, act), HDT_ERR_HIP.
  */
+/* of an infinite g: what the formula gives, NaN where it meets 0 infinity */
 typedef enum {
     HDT_SILU = 0,     /* g / (1 + exp(-g)) */
     HDT_GELU = 1,     /* g Phi(g), Phi the normal distribution's */

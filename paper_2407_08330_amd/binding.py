@@ -916,7 +916,7 @@ def _check_results(ts, shape, like):
 def hdt_ffn_fwd(x, w_gate, w_up, w_down, act: str = "silu", train: bool = True, y=None, by_gate=None, by_up=None, hidden=None, workspace=None, stream=None):
     """Gated feed-forward block (hdt_ffn_fwd in include/hdt.h): y = (act(x w_gate^T) * (x w_up^T)) w_down^T.  x [..][width], w_gate, w_up
     [inner][width], w_down [width][inner]; act: "silu", "gelu" or "gelu_tanh".  Returns (y, by_gate, by_up, hidden), the last three [..][inner] for
-    hdt_ffn_bwd (the derivatives of hidden = act(..) * (..) by its two factors' products, and hidden), or None with ``train=False``."""
+    hdt_ffn_bwd (the derivatives of hidden = act(..) * (..) by its two factors' products, and hidden, rounded to x's type), or None with ``train=False``."""
     if _lib is None:
         load_library()
     r = _calls.ffn_fwd(x, w_gate, w_up, w_down, act, train, y, by_gate, by_up, hidden, workspace, None if stream is None else stream.cuda_stream)

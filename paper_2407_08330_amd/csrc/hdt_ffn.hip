@@ -1,4 +1,4 @@
-// Gated feed-forward block: checks, what kernel takes which product, the calls.  hdt_ffn.h has the mathematics.
+// Gated feed-forward block: checks, launches, the calls.  hdt_ffn.h has the mathematics, hdt_ffn_plan.h what kernel takes which product.
 #include <algorithm>
 
 #include "hdt_ffn.h"

@@ -1,7 +1,7 @@
 // The products of the gated feed-forward block in bf16, in large tiles.
 //
-// A workgroup of WM x WN waves makes a tile of BM x BN of C^T = B A^T, a wave MB x NB blocks of 32 x 32.  64 of k at a time go straight from
-// memory to LDS, two stages of them.  A wave holds the operands of 16 of k in registers and those of the next 16 on their way, over the
+// A workgroup of WM x WN waves makes a tile of BM x BN of C^T = B A^T, a wave MB x NB blocks of 32 x 32.  BK of k at a time go straight from
+// memory to LDS: 32 in tiles of 256 x 256, four stages of them, 64 in tiles of 128 x 128, two stages.  A wave holds the operands of 16 of k in registers and those of the next 16 on their way, over the
 // barrier between two stages too: the last products of a stage run while the first operands of the next arrive.
 //
 // C^T rather than C, and the rows of B (n) that an operand holds in the order 0-3, 8-11, 4-7, 12-15: a lane's sums are then eight
@@ -15,7 +15,7 @@
 // The forward's gate product takes 217 us where H alone leaves and 293 where its derivatives leave too (402 MB), dG and dU 178 (537 MB in and out): stores and
 // what comes from memory at a tile's end find the other waves at the same place, and the tile's walk is only 24 stages long.
 //
-// LDS tiles.  Rows of "fast" operands: 128 bytes, 64 of k, whose 16-byte chunks are exchanged so that 16 consecutive rows read without a
+// LDS tiles.  Rows of "fast" operands: BK of k, 64 or 128 bytes, whose 16-byte chunks are exchanged so that 16 consecutive rows read without a
 // conflict (hdt_tile.h has the rule).  Rows of "slow" operands: one k, BM or BN values, read transposed; four consecutive k at the same
 // 64 bytes are moved apart.
 //

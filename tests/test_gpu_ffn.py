@@ -146,6 +146,20 @@ def test_activations_up_to_the_types_largest_values(act, dtype, rows):
     assert all(bool(k.isnan().all()) for k in hdt.hdt_ffn_fwd(*t, act)[1:])
 
 
+@pytest.mark.parametrize("rows", [1, 300])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ACTS)
+def test_infinite_g_gives_what_the_formula_gives(act, dtype, rows):
+    import torch
+    import paper_2407_08330_amd as hdt
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    x, wg = torch.ones(rows, 1, device="cuda", dtype=t), torch.tensor([[float("inf")], [-float("inf")], [1.0]], device="cuda", dtype=t)
+    _, by_gate, by_up, hidden = hdt.hdt_ffn_fwd(x, wg, torch.ones_like(wg), torch.ones(1, 3, device="cuda", dtype=t), act)
+    for k in (by_up, hidden):
+        assert bool((k[:, 0] == float("inf")).all()) and bool(k[:, 1].isnan().all())
+    assert bool(by_gate[:, :2].isnan().all()) and all(bool(k[:, 2].isfinite().all()) for k in (by_gate, by_up, hidden))
+
+
 def test_shapes_and_no_rows():
     import torch
     import paper_2407_08330_amd as hdt
